@@ -309,6 +309,126 @@ int moe_dispatch_to_combine(const MoeShape* shape, const void* d_x, const void* 
                             void* d_out, const MoeSaved* saved, void* d_workspace, size_t workspace_bytes, int mode,
                             void* stream);
 
+/* ---- Operators around the layer in a transformer block: layer norm, dropout with residual, balance loss and the
+ *      router's backward.  Same conventions as above; sums and statistics are fp32 (or whole numbers), in a fixed
+ *      order: the same call on the same values gives the same bits.  T == 0 is a no-op unless said otherwise.
+ *      dtype (MoeDtype) is the storage type of the arrays documented as such.  1 <= H <= 262144, any T that
+ *      fits in memory.  Outputs may be the inputs of the same shape they are computed from element by element (dx = dy,
+ *      z = v, ...); two outputs of a call may not overlap. ---- */
+
+/*
+ * Layer norm of rows: mean = sum x / H, rstd = 1 / sqrt(sum (x - mean)^2 / H + eps),
+ *   y = (x - mean) * rstd * gamma + beta
+ *   d_x, d_y [T,H] dtype;  d_gamma, d_beta [H] dtype, either NULL: 1 and 0
+ *   eps      finite, >= 0
+ *   d_mean, d_rstd [T] f32   what the backward needs; NULL (inference): not stored
+ */
+int moe_layer_norm_forward(int32_t T, int32_t H, int dtype, const void* d_x, const void* d_gamma, const void* d_beta,
+                           float eps, void* d_y, float* d_mean, float* d_rstd, void* stream);
+
+/* Bytes of device workspace of the two backward calls below.  Host-only. */
+int moe_layer_norm_workspace_bytes(int32_t T, int32_t H, size_t* bytes);
+
+/*
+ * Its backward: t = dy * gamma, xh = (x - mean) * rstd,
+ *   dx = rstd * (t - sum t / H - xh * sum (t * xh) / H) + dres,  dgamma = sum over rows of dy * xh,  dbeta = sum of dy
+ *   d_dres   [T,H] dtype, NULL: 0.  The gradient that reaches x by the residual path beside the norm
+ *   d_dx     [T,H] dtype;  d_dgamma, d_dbeta [H] dtype, either NULL: not computed.  With T == 0 they are zeroed
+ *   d_workspace  >= moe_layer_norm_workspace_bytes(T, H); may be NULL if d_dgamma and d_dbeta are
+ */
+int moe_layer_norm_backward(int32_t T, int32_t H, int dtype, const void* d_dy, const void* d_x, const void* d_gamma,
+                            const float* d_mean, const float* d_rstd, const void* d_dres, void* d_dx, void* d_dgamma,
+                            void* d_dbeta, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dropout and residual: out = residual + (kept ? v * 65536 / (65536 - thr) : 0),  thr = p rounded to 1/65536, times 65536.
+ * The mask is a function of the element's place and of {seed, offset} and is never stored: element (t, h) is kept if
+ * its 16 random bits are >= thr; they are half h % 2 (0: low) of word (h % 8) / 2 of Philox4x32-10 (Salmon et al., 2011)
+ * with key (seed low, seed high) and counter (h / 8, t, offset low, offset high).  What is dropped may hold anything.
+ *   p        0 <= p <= 1 (0: everything is kept and the generator is not run; 1: everything is dropped)
+ *   d_rng    device, 8-byte aligned: {seed, offset}, u64 each, read when the call runs, so that a captured graph draws
+ *            new masks when its program changes them; may be NULL if p rounds to 0
+ *   d_residual [T,H] dtype, NULL: 0
+ * The backward takes the same p and d_rng contents: d_dv = kept ? dout * 65536 / (65536 - thr) : 0; the residual's
+ * gradient is dout.
+ */
+int moe_dropout_add_forward(int32_t T, int32_t H, int dtype, const void* d_v, const void* d_residual, float p,
+                            const uint64_t* d_rng, void* d_out, void* stream);
+int moe_dropout_add_backward(int32_t T, int32_t H, int dtype, const void* d_dout, float p, const uint64_t* d_rng,
+                             void* d_dv, void* stream);
+
+/*
+ * The two in one pass, the end of one block and the start of the next: z = residual + dropout(v), y = layer norm of z as
+ * it is stored; bit for bit what moe_dropout_add_forward and moe_layer_norm_forward give.  z and y are two buffers.
+ * Backward: dz = dres + (layer norm's backward of dy at z), which is also the residual's gradient, and dv = dropout's
+ * backward of dz (before dz is rounded to dtype).  Arguments as above.
+ */
+int moe_dropout_add_layer_norm_forward(int32_t T, int32_t H, int dtype, const void* d_v, const void* d_residual, float p,
+                                       const uint64_t* d_rng, const void* d_gamma, const void* d_beta, float eps,
+                                       void* d_z, void* d_y, float* d_mean, float* d_rstd, void* stream);
+int moe_dropout_add_layer_norm_backward(int32_t T, int32_t H, int dtype, const void* d_dy, const void* d_z,
+                                        const void* d_gamma, const float* d_mean, const float* d_rstd, const void* d_dres,
+                                        float p, const uint64_t* d_rng, void* d_dz, void* d_dv, void* d_dgamma,
+                                        void* d_dbeta, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Balance loss of the router and the selections per expert.  q[t,:] = softmax over all E logits of token t (0 in a row
+ * without a finite logit: all -inf); over the n tokens that the mask leaves
+ *   counts[e] = selections of expert e,  prob_sum[e] = sum of q[t,e],
+ *   loss = coef * E * sum over e of (counts[e] / (k n)) * (prob_sum[e] / n);  n == 0: 0
+ *   d_logits   [T,E] f32;  d_topk_idx [T,k] i32 (MoeSaved.topk_idx); ids outside 0 .. E-1 are not counted
+ *   d_mask     [T] u8, 0: the token (padding) does not count; NULL: all count
+ *   d_counts   [E+1] i32, counts[E] = n;  d_prob_sum [E] f32;  d_loss [1] f32.  Written for T == 0 as well
+ * Limits: 1 <= k <= 16, k <= E <= 256.
+ */
+int moe_balance_workspace_bytes(int32_t T, int32_t E, size_t* bytes);
+int moe_balance_forward(int32_t T, int32_t E, int32_t k, const float* d_logits, const int32_t* d_topk_idx,
+                        const uint8_t* d_mask, float coef, int32_t* d_counts, float* d_prob_sum, float* d_loss,
+                        void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradient of the router's logits: that of the routing weights (softmax over the k selected logits; moe_ffn_backward's
+ * d_dtopk_w) plus that of the balance loss (the counts carry none):
+ *   dlogits[t,e] = [e == topk_idx[t,j]] topk_w[t,j] * (dtopk_w[t,j] - sum over i of topk_w[t,i] dtopk_w[t,i])
+ *                + dloss * coef * E / n * q[t,e] * (f[e] - sum over e' of f[e'] q[t,e']),  f[e] = counts[e] / (k n)
+ *   d_topk_w, d_dtopk_w [T,k] f32   both NULL: without the first part
+ *   d_counts   [E+1] as moe_balance_forward left it (or summed over ranks: then of the loss of all their tokens);
+ *              NULL: without the second part.  Tokens off the mask have no second part
+ *   d_dloss    [1] f32 device, NULL: 1
+ *   d_dlogits  [T,E] f32, overwritten (may be d_logits)
+ */
+int moe_router_backward(int32_t T, int32_t E, int32_t k, const float* d_logits, const int32_t* d_topk_idx,
+                        const float* d_topk_w, const float* d_dtopk_w, const uint8_t* d_mask, float coef,
+                        const int32_t* d_counts, const float* d_dloss, float* d_dlogits, void* stream);
+
+/* ---- 4-bit experts (serving) ----
+ * Weights as 4-bit floats (sign, 2 exponent bits, 1 mantissa bit: 0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives) with a
+ * power-of-two scale per block of 32 consecutive k of one column, w = code * 2^(scale - 127) (the MXFP4 block format of the
+ * OCP Microscaling specification).  For a weight matrix [K,N] of each expert:
+ *   q      [E_local, K/32, N, 16] u8   byte b of a block: k = 2b in the low nibble, 2b + 1 in the high one
+ *   scale  [E_local, K/32, N]     u8   1 .. 254; 255: the block is not a number
+ */
+
+/*
+ * Blocks from weights d_w [E_local,K,N] (dtype): the scale brings the block's largest magnitude into [4, 8), each value
+ * goes to the nearest code (ties to the even one, above 6 to 6); a block of zeros has scale 127, one with an infinity
+ * or NaN 255.  K a multiple of 32, K and N up to 524288.
+ */
+int moe_quantize_w4(int32_t E_local, int32_t K, int32_t N, int dtype, const void* d_w, void* d_q, void* d_scale,
+                    void* stream);
+
+/*
+ * moe_ffn_forward (inference, serialized launches) with both weight tensors in that form: activations bf16 with fp32
+ * accumulation, weights exact.  shape->dtype must be MOE_BF16.  Made for the few rows per expert of a serving step: any T is
+ * right, but from some hundred rows per expert the bf16 weights are faster.
+ *   d_q_gate_up, d_s_gate_up  blocks and scales of w_gate_up [E_local,H,2I];  d_q_down, d_s_down of w_down [E_local,I,H]
+ * Two roundings to bf16: the SwiGLU output (GEMM-2's operand) and the layer output (GEMM-2's rows are added up in fp32).
+ *   saved      nullable, checked as for moe_ffn_forward; of its members only the routing results are written
+ */
+int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_logits, const void* d_q_gate_up,
+                       const void* d_s_gate_up, const void* d_q_down, const void* d_s_down, void* d_out,
+                       const MoeSaved* saved, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* ---- SwiGLU + Add microbenchmark (paper Section 6: tile interleaving and L2 reuse, Section 6.1;
  *      static against dynamic scheduling, Section 6.2) ----
  *   S[m,j]   = silu(X[m,j]) * X[m,N+j]      X [M,2N] bf16, S [M,N] bf16 (intermediate, written)

@@ -41,8 +41,21 @@ EXPORTS = (
     "moe_probe_mfma_bf16", "moe_probe_copy", "moe_probe_read", "moe_probe_write", "moe_microbench_swiglu_add_static_scratch",
     "moe_ffn_debug_force_device_scope", "moe_ffn_debug_layout", "moe_dispatch_to_combine",
     "moe_grouped_gemm_scatter", "moe_ffn_forward_scatter",
+    "moe_layer_norm_workspace_bytes", "moe_layer_norm_forward", "moe_layer_norm_backward", "moe_dropout_add_forward",
+    "moe_dropout_add_backward", "moe_dropout_add_layer_norm_forward", "moe_dropout_add_layer_norm_backward",
+    "moe_balance_workspace_bytes", "moe_balance_forward", "moe_router_backward", "moe_quantize_w4", "moe_ffn_forward_w4",
 )
 LAYOUT_WORDS = 25   # MOE_LAYOUT_WORDS
+
+# Argument kinds of the operators around the layer: i int, f float, p pointer, z size_t
+_KINDS = {"i": ctypes.c_int32, "f": ctypes.c_float, "p": ctypes.c_void_p, "z": ctypes.c_size_t}
+_BLOCK_ARGS = {
+    "moe_layer_norm_workspace_bytes": "iip", "moe_layer_norm_forward": "iiipppfpppp", "moe_layer_norm_backward": "iiipppppppp" "ppzp",
+    "moe_dropout_add_forward": "iiippfppp", "moe_dropout_add_backward": "iiipfppp",
+    "moe_dropout_add_layer_norm_forward": "iiippfpppf" "ppppp", "moe_dropout_add_layer_norm_backward": "iiipppppp" "fpppppp" "zp",
+    "moe_balance_workspace_bytes": "iip", "moe_balance_forward": "iiipppf" "ppppzp", "moe_router_backward": "iiippppp" "fpppp",
+    "moe_quantize_w4": "iiiipppp", "moe_ffn_forward_w4": "ppppppppppzp",
+}
 
 
 def library_path() -> str:
@@ -65,6 +78,8 @@ def load_library() -> ctypes.CDLL:
             getattr(lib, name).restype = ctypes.c_int
         lib.moe_microbench_workspace_bytes.restype = ctypes.c_size_t
         lib.moe_microbench_workspace_bytes.argtypes = [ctypes.c_int]
+        for name, kinds in _BLOCK_ARGS.items():
+            getattr(lib, name).argtypes = [_KINDS[c] for c in kinds]
         _LIB = lib
     return _LIB
 
@@ -319,3 +334,180 @@ def moe_probe_write(dst, nbytes, word=0, stream=None) -> None:
 def moe_probe_copy(src, dst, nbytes, stream=None) -> None:
     _check(load_library().moe_probe_copy(_ptr(src), _ptr(dst), ctypes.c_size_t(nbytes), _stream(stream)),
            "moe_probe_copy")
+
+
+# ---- the operators around the layer: T, H and the storage type are read off the tensors, whose shapes and types are checked ----
+
+def _arg(t: Optional[torch.Tensor], shape, dtype, name: str):
+    """Device address of a tensor of this shape and type; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous device tensor of shape {shape} and type {dtype}, got {tuple(t.shape)}, "
+                         f"{t.dtype}, {t.device}")
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, name: str):
+    """(T, H, storage type, its MoeDtype) of a [T, H] tensor."""
+    if t.dim() != 2 or t.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{name}: expected a [T, H] tensor in bfloat16 or float32, got {tuple(t.shape)}, {t.dtype}")
+    T, H = t.shape
+    return T, H, t.dtype, MOE_BF16 if t.dtype is torch.bfloat16 else MOE_F32
+
+
+def _raw_stream(stream) -> int:
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _drop_rng(rng: Optional[torch.Tensor]):
+    return _arg(rng, (2,), torch.int64, "rng")
+
+
+def _size(name: str, *args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(getattr(load_library(), name)(*args, ctypes.addressof(n)), name)
+    return n.value
+
+
+def _workspace(t: Optional[torch.Tensor]):
+    if t is None:
+        return None, 0
+    return _ptr(t).value, t.numel() * t.element_size()
+
+
+def moe_layer_norm_workspace_bytes(T: int, H: int) -> int:
+    return _size("moe_layer_norm_workspace_bytes", T, H)
+
+
+def alloc_layer_norm_workspace(T: int, H: int, device="cuda") -> torch.Tensor:
+    return torch.empty(moe_layer_norm_workspace_bytes(T, H), dtype=torch.uint8, device=device)
+
+
+def moe_layer_norm_forward(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None) -> None:
+    """y = layer norm of the rows of x [T, H]; gamma, beta [H] or None; mean, rstd [T] f32 (for the backward) or None."""
+    T, H, dt, code = _rows(x, "x")
+    f32 = torch.float32
+    _check(load_library().moe_layer_norm_forward(
+        T, H, code, _arg(x, (T, H), dt, "x"), _arg(gamma, (H,), dt, "gamma"), _arg(beta, (H,), dt, "beta"), eps,
+        _arg(y, (T, H), dt, "y"), _arg(mean, (T,), f32, "mean"), _arg(rstd, (T,), f32, "rstd"), _raw_stream(stream)),
+        "moe_layer_norm_forward")
+
+
+def moe_layer_norm_backward(dy, x, gamma, mean, rstd, dres, dx, dgamma, dbeta, workspace, stream=None) -> None:
+    """dx = gradient of x, plus dres (the residual path's) if given; dgamma, dbeta [H] or None."""
+    T, H, dt, code = _rows(x, "x")
+    f32 = torch.float32
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_layer_norm_backward(
+        T, H, code, _arg(dy, (T, H), dt, "dy"), _arg(x, (T, H), dt, "x"), _arg(gamma, (H,), dt, "gamma"),
+        _arg(mean, (T,), f32, "mean"), _arg(rstd, (T,), f32, "rstd"), _arg(dres, (T, H), dt, "dres"), _arg(dx, (T, H), dt, "dx"),
+        _arg(dgamma, (H,), dt, "dgamma"), _arg(dbeta, (H,), dt, "dbeta"), ws, wb, _raw_stream(stream)), "moe_layer_norm_backward")
+
+
+def moe_dropout_add_forward(v, residual, p: float, rng, out, stream=None) -> None:
+    """out = residual (or 0) + dropout(v); rng: device int64 {seed, offset}, None if p == 0."""
+    T, H, dt, code = _rows(v, "v")
+    _check(load_library().moe_dropout_add_forward(
+        T, H, code, _arg(v, (T, H), dt, "v"), _arg(residual, (T, H), dt, "residual"), p, _drop_rng(rng), _arg(out, (T, H), dt, "out"),
+        _raw_stream(stream)), "moe_dropout_add_forward")
+
+
+def moe_dropout_add_backward(dout, p: float, rng, dv, stream=None) -> None:
+    """dv = dropout's backward of dout, with the forward's p and rng contents."""
+    T, H, dt, code = _rows(dout, "dout")
+    _check(load_library().moe_dropout_add_backward(
+        T, H, code, _arg(dout, (T, H), dt, "dout"), p, _drop_rng(rng), _arg(dv, (T, H), dt, "dv"), _raw_stream(stream)),
+        "moe_dropout_add_backward")
+
+
+def moe_dropout_add_layer_norm_forward(v, residual, p: float, rng, gamma, beta, eps: float, z, y, mean=None, rstd=None,
+                                       stream=None) -> None:
+    """z = residual (or 0) + dropout(v), y = layer norm of z."""
+    T, H, dt, code = _rows(v, "v")
+    f32 = torch.float32
+    _check(load_library().moe_dropout_add_layer_norm_forward(
+        T, H, code, _arg(v, (T, H), dt, "v"), _arg(residual, (T, H), dt, "residual"), p, _drop_rng(rng), _arg(gamma, (H,), dt, "gamma"),
+        _arg(beta, (H,), dt, "beta"), eps, _arg(z, (T, H), dt, "z"), _arg(y, (T, H), dt, "y"), _arg(mean, (T,), f32, "mean"),
+        _arg(rstd, (T,), f32, "rstd"), _raw_stream(stream)), "moe_dropout_add_layer_norm_forward")
+
+
+def moe_dropout_add_layer_norm_backward(dy, z, gamma, mean, rstd, dres, p: float, rng, dz, dv, dgamma, dbeta, workspace,
+                                        stream=None) -> None:
+    """dz = dres (or 0) + layer norm's backward at z (the residual's gradient too), dv = dropout's backward of dz."""
+    T, H, dt, code = _rows(z, "z")
+    f32 = torch.float32
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_dropout_add_layer_norm_backward(
+        T, H, code, _arg(dy, (T, H), dt, "dy"), _arg(z, (T, H), dt, "z"), _arg(gamma, (H,), dt, "gamma"),
+        _arg(mean, (T,), f32, "mean"), _arg(rstd, (T,), f32, "rstd"), _arg(dres, (T, H), dt, "dres"), p, _drop_rng(rng),
+        _arg(dz, (T, H), dt, "dz"), _arg(dv, (T, H), dt, "dv"), _arg(dgamma, (H,), dt, "dgamma"), _arg(dbeta, (H,), dt, "dbeta"),
+        ws, wb, _raw_stream(stream)), "moe_dropout_add_layer_norm_backward")
+
+
+def moe_balance_workspace_bytes(T: int, E: int) -> int:
+    return _size("moe_balance_workspace_bytes", T, E)
+
+
+def alloc_balance_workspace(T: int, E: int, device="cuda") -> torch.Tensor:
+    return torch.empty(moe_balance_workspace_bytes(T, E), dtype=torch.uint8, device=device)
+
+
+def _mask(mask: Optional[torch.Tensor], T: int):
+    return _arg(mask, (T,), torch.bool if mask is not None and mask.dtype is torch.bool else torch.uint8, "mask")
+
+
+def _router(logits, topk_idx):
+    if logits.dim() != 2 or topk_idx.dim() != 2:
+        raise ValueError("expected logits [T, E] and topk_idx [T, k]")
+    return logits.shape[0], logits.shape[1], topk_idx.shape[1]
+
+
+def moe_balance_forward(logits, topk_idx, mask, coef: float, counts, prob_sum, loss, workspace, stream=None) -> None:
+    """counts [E + 1] i32 (the last: tokens that count), prob_sum [E] f32, loss [1] f32; mask [T] bool / uint8 or None."""
+    T, E, k = _router(logits, topk_idx)
+    f32, i32 = torch.float32, torch.int32
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_balance_forward(
+        T, E, k, _arg(logits, (T, E), f32, "logits"), _arg(topk_idx, (T, k), i32, "topk_idx"), _mask(mask, T), coef,
+        _arg(counts, (E + 1,), i32, "counts"), _arg(prob_sum, (E,), f32, "prob_sum"), _arg(loss, (1,), f32, "loss"), ws, wb,
+        _raw_stream(stream)), "moe_balance_forward")
+
+
+def moe_router_backward(logits, topk_idx, topk_w, dtopk_w, mask, coef: float, counts, dloss, dlogits, stream=None) -> None:
+    """dlogits [T, E] from the routing weights' gradient (topk_w, dtopk_w or both None) and the balance loss's (counts or None)."""
+    T, E, k = _router(logits, topk_idx)
+    f32, i32 = torch.float32, torch.int32
+    _check(load_library().moe_router_backward(
+        T, E, k, _arg(logits, (T, E), f32, "logits"), _arg(topk_idx, (T, k), i32, "topk_idx"), _arg(topk_w, (T, k), f32, "topk_w"),
+        _arg(dtopk_w, (T, k), f32, "dtopk_w"), _mask(mask, T), coef, _arg(counts, (E + 1,), i32, "counts"),
+        _arg(dloss, (1,), f32, "dloss"), _arg(dlogits, (T, E), f32, "dlogits"), _raw_stream(stream)), "moe_router_backward")
+
+
+def alloc_w4(E_local: int, K: int, N: int, device="cuda"):
+    """(q, scale) buffers of a weight tensor [E_local, K, N] in 4-bit blocks."""
+    return (torch.empty(E_local, K // 32, N, 16, dtype=torch.uint8, device=device),
+            torch.empty(E_local, K // 32, N, dtype=torch.uint8, device=device))
+
+
+def moe_quantize_w4(w, q, scale, stream=None) -> None:
+    """4-bit blocks of w [E_local, K, N] (bfloat16 or float32)."""
+    if w.dim() != 3 or w.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"w: expected an [E_local, K, N] tensor in bfloat16 or float32, got {tuple(w.shape)}, {w.dtype}")
+    E, K, N = w.shape
+    _check(load_library().moe_quantize_w4(
+        E, K, N, MOE_BF16 if w.dtype is torch.bfloat16 else MOE_F32, _arg(w, (E, K, N), w.dtype, "w"),
+        _arg(q, (E, K // 32, N, 16), torch.uint8, "q"), _arg(scale, (E, K // 32, N), torch.uint8, "scale"), _raw_stream(stream)),
+        "moe_quantize_w4")
+
+
+def moe_ffn_forward_w4(shape, x, logits, q_gate_up, s_gate_up, q_down, s_down, out, saved: Optional[Saved], workspace,
+                       stream=None) -> None:
+    T, H, I, El, bf16, u8 = shape.T, shape.H, shape.I, shape.E_local, torch.bfloat16, torch.uint8
+    sv = saved.c_struct() if saved is not None else None
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_ffn_forward_w4(
+        ctypes.addressof(shape), _arg(x, (T, H), bf16, "x"), _arg(logits, (T, shape.E), torch.float32, "logits"),
+        _arg(q_gate_up, (El, H // 32, 2 * I, 16), u8, "q_gate_up"), _arg(s_gate_up, (El, H // 32, 2 * I), u8, "s_gate_up"),
+        _arg(q_down, (El, I // 32, H, 16), u8, "q_down"), _arg(s_down, (El, I // 32, H), u8, "s_down"), _arg(out, (T, H), bf16, "out"),
+        ctypes.addressof(sv) if sv is not None else None, ws, wb, _raw_stream(stream)), "moe_ffn_forward_w4")

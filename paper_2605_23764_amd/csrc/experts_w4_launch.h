@@ -1,0 +1,23 @@
+// The grouped products with 4-bit weights (experts_w4.hip) as moe_ffn.hip launches them.
+#pragma once
+#include <stdint.h>
+
+namespace moe {
+
+struct W4Launch {
+  const void* x;
+  const int32_t* gather;         // null: rows of x in expert order
+  const void *q, *scale;
+  const int32_t* offsets;
+  void* out;
+  int E_local, K, N;
+};
+
+// swiglu: N bf16 columns from N gate and N up columns; otherwise N fp32 columns.  Returns a MoeStatus, as the next.
+__attribute__((visibility("hidden"))) int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream);
+
+// Combine of fp32 rows into bf16 [T,H].
+__attribute__((visibility("hidden"))) int launch_combine_w4(const float* y, const int32_t* row_of, const float* topk_w, void* out, int T, int H,
+                                                            int k, void* stream);
+
+}  // namespace moe

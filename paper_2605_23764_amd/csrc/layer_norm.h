@@ -1,0 +1,384 @@
+// Layer norm, dropout with residual, and the two in one pass, forward and backward.
+//
+//   z = residual + drop(v)                 (layer norm alone: z is the input)
+//   y = (z - mean) * rstd * gamma + beta   mean, rstd = 1 / sqrt(var + eps) of the row of z as it is stored
+//   backward: t = dy * gamma, xh = (z - mean) * rstd,
+//     dz = rstd * (t - mean(t) - xh * mean(t * xh)) + dres;  dv = drop'(dz);  dgamma = sum dy * xh, dbeta = sum dy over rows
+//
+// A handful of flops per element: what bounds them is the bytes, each array once.  So a row stays in the registers of the lanes that
+// read it (a vector of eight per lane, up to 16 waves a row; longer rows are read again), mean and variance are taken one after the other from
+// there (no cancellation), and the dropout bits are made again from the counter instead of stored.
+// All sums are fp32, in a fixed order.
+#pragma once
+#include "rows.h"
+
+namespace moe {
+
+constexpr int kRowMaxH = kRowMaxWaves * kWave * 8;               // longest row that stays in registers
+constexpr int kNormMaxParts = 512;                               // partial sums of dgamma / dbeta, at most
+
+// Arrays are [T, H], vectors [H]; what may be null is looked at once per launch.
+struct NormForwardParams {
+  const void *v, *x;              // v: dropped and added to x (fused form only); x may be null there
+  const void *gamma, *beta;       // null: 1, 0
+  void *z, *y;                    // z: fused form only
+  float *mean, *rstd;             // [T], may be null
+  DropParams drop;
+  float eps;
+  int T, H, group;
+};
+
+struct NormBackwardParams {
+  const void *dy, *x, *gamma, *dres;   // gamma, dres may be null
+  const float *mean, *rstd;
+  void *dx, *dv;                       // dv: fused form only
+  float* part;                         // [parts][2][H] sums of dy * xh and dy, null: not wanted
+  DropParams drop;
+  float inv_h;
+  int T, H, group, groups;             // lanes per row; rows that a workgroup has in hand at a time
+};
+
+template <typename T> __device__ __forceinline__ const T* row_of(const void* p, int t, int H) {
+  return static_cast<const T*>(p) + (size_t)t * H;
+}
+template <typename T> __device__ __forceinline__ T* row_of(void* p, int t, int H) { return static_cast<T*>(p) + (size_t)t * H; }
+
+// One row per group of lanes; rows of up to 64 vectors share a workgroup.
+template <typename T, bool TAIL, bool FUSED>
+__global__ __launch_bounds__(1024) void norm_forward_kernel(NormForwardParams p) {
+  __shared__ float s_sum[2][kRowMaxWaves];
+  const int G = p.group, H = p.H;
+  const int g = G > kWave ? (int)threadIdx.x : (int)threadIdx.x & (G - 1), at = g * 8;
+  const int rows = G > kWave ? 1 : blockDim.x / G;
+  for (long t0 = (long)blockIdx.x * rows; t0 < p.T; t0 += (long)gridDim.x * rows) {
+    const int t = (int)min(t0 + (G > kWave ? 0 : (int)threadIdx.x / G), (long)p.T);
+    const bool in = t < p.T && at < H;
+    Raw8<T> rx = raw_zero<T>(), rg = raw_zero<T>(), rb = raw_zero<T>();
+    if (in) {
+      if (p.x) rx = raw_load<T, TAIL>(row_of<T>(p.x, t, H), at, H);
+      Raw8<T> rv;
+      if (FUSED) rv = raw_load<T, TAIL>(row_of<T>(p.v, t, H), at, H);
+      if (p.gamma) rg = raw_load<T, TAIL>(static_cast<const T*>(p.gamma), at, H);
+      if (p.beta) rb = raw_load<T, TAIL>(static_cast<const T*>(p.beta), at, H);
+      if (FUSED) {
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = raw_get<T>(rv, x);
+        drop8(v, p.drop, drop_key(p.drop), (uint32_t)t, (uint32_t)g);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] += raw_get<T>(rx, x);
+        rx = raw_pack<T>(v);                                       // z is an output, and y the norm of it as it is stored
+        raw_store<T, TAIL>(row_of<T>(p.z, t, H), at, H, rx);
+      }
+    }
+    float sum[1] = {0.f}, sq[1] = {0.f};
+#pragma unroll
+    for (int x = 0; x < 8; ++x) sum[0] += raw_get<T>(rx, x);       // 0 outside the row
+    group_sum<1>(sum, G, s_sum[0]);
+    const float mean = sum[0] / (float)H;                          // not * (1 / H): a constant row then has mean x, variance 0
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const float d = raw_get<T>(rx, x) - mean;
+      if (TAIL ? at + x < H : at < H) sq[0] += d * d;
+    }
+    group_sum<1>(sq, G, s_sum[1]);
+    const float rstd = 1.0f / sqrtf(sq[0] / (float)H + p.eps);
+    if (!in) continue;
+    if (g == 0) {
+      if (p.mean) p.mean[t] = mean;
+      if (p.rstd) p.rstd[t] = rstd;
+    }
+    float o[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      o[x] = (raw_get<T>(rx, x) - mean) * rstd;
+      if (p.gamma) o[x] *= raw_get<T>(rg, x);
+      if (p.beta) o[x] += raw_get<T>(rb, x);
+    }
+    raw_store<T, TAIL>(row_of<T>(p.y, t, H), at, H, raw_pack<T>(o));
+  }
+}
+
+// A workgroup walks rows in strides with `groups` of them in hand, the next ones' loads under way while these are reduced, and keeps
+// its rows' sums of dy * xh and dy in registers: one partial per workgroup at the end.
+template <typename T, bool TAIL, bool FUSED>
+__global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackwardParams p) {
+  __shared__ float s_sum[2][2][kRowMaxWaves];
+  extern __shared__ float s_part[];                              // [groups - 1][G][16]
+  const int G = p.group, H = p.H;
+  const int rg = threadIdx.x / G, g = threadIdx.x - rg * G, at = g * 8;
+  const DropKey key = FUSED ? drop_key(p.drop) : DropKey{};
+  float acc_g[8], acc_b[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) acc_g[x] = acc_b[x] = 0.f;
+  const Raw8<T> gamma = p.gamma && at < H ? raw_load<T, TAIL>(static_cast<const T*>(p.gamma), at, H) : raw_zero<T>();
+  struct Row { Raw8<T> dy, x, dres; float mean, rstd; };
+  auto load = [&](Row& r, int t) __attribute__((always_inline)) {
+    const bool live = t < p.T;
+    r.mean = live ? p.mean[t] : 0.f;
+    r.rstd = live ? p.rstd[t] : 0.f;
+    r.dy = r.x = r.dres = raw_zero<T>();
+    if (live && at < H) {
+      r.dy = raw_load<T, TAIL>(row_of<T>(p.dy, t, H), at, H);
+      r.x = raw_load<T, TAIL>(row_of<T>(p.x, t, H), at, H);
+      if (p.dres) r.dres = raw_load<T, TAIL>(row_of<T>(p.dres, t, H), at, H);
+    }
+  };
+  const int stride = gridDim.x * p.groups;
+  Row cur;
+  load(cur, blockIdx.x * p.groups + rg);
+  // as many turns for every group of the workgroup: the barrier of a turn is reached by all.  (64 bits: t0 + stride may pass 2^31.)
+  int turn = 0;
+  for (long t0 = (long)blockIdx.x * p.groups; t0 < p.T; t0 += stride, turn ^= 1) {
+    const int t = (int)min(t0 + rg, (long)p.T);
+    Row next;
+    load(next, (int)min(t0 + rg + stride, (long)p.T));
+    float dxh[8], xh[8], sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const float d = raw_get<T>(cur.dy, x);                     // 0 outside the row
+      xh[x] = (raw_get<T>(cur.x, x) - cur.mean) * cur.rstd;
+      if (TAIL ? at + x >= H : at >= H) xh[x] = 0.f;             // there x is not, and 0 * rstd may be no number
+      dxh[x] = p.gamma ? d * raw_get<T>(gamma, x) : d;
+      acc_g[x] += d * xh[x];
+      acc_b[x] += d;
+      sum[0] += dxh[x];
+      sum[1] += dxh[x] * xh[x];
+    }
+    group_sum<2>(sum, G, &s_sum[turn][0][0]);
+    const float m1 = sum[0] * p.inv_h, m2 = sum[1] * p.inv_h;
+    if (t < p.T && at < H) {
+      float o[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) o[x] = cur.rstd * (dxh[x] - m1 - xh[x] * m2) + raw_get<T>(cur.dres, x);
+      raw_store<T, TAIL>(row_of<T>(p.dx, t, H), at, H, raw_pack<T>(o));
+      if (FUSED) {
+        drop8(o, p.drop, key, (uint32_t)t, (uint32_t)g);
+        raw_store<T, TAIL>(row_of<T>(p.dv, t, H), at, H, raw_pack<T>(o));
+      }
+    }
+    cur = next;
+  }
+  if (!p.part) return;
+  if (p.groups > 1) {
+    float* s = s_part + ((size_t)(rg - 1) * G + g) * 16;
+    if (rg > 0)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        s[x] = acc_g[x];
+        s[8 + x] = acc_b[x];
+      }
+    __syncthreads();
+    if (rg > 0) return;
+    for (int r = 1; r < p.groups; ++r) {
+      s = s_part + ((size_t)(r - 1) * G + g) * 16;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        acc_g[x] += s[x];
+        acc_b[x] += s[8 + x];
+      }
+    }
+  }
+  float* out = p.part + (size_t)blockIdx.x * 2 * H + at;
+#pragma unroll
+  for (int x = 0; x < 8; ++x)
+    if (TAIL ? at + x < H : at < H) {
+      out[x] = acc_g[x];
+      out[H + x] = acc_b[x];
+    }
+}
+
+// ---- rows longer than kRowMaxH: a workgroup of 16 waves goes over its row again instead of keeping it (from the L2) ----
+template <typename T, bool TAIL, bool FUSED>
+__global__ __launch_bounds__(1024) void norm_forward_long_kernel(NormForwardParams p) {
+  __shared__ float s_sum[2][kRowMaxWaves];
+  const int H = p.H, step = blockDim.x * 8;
+  for (long tl = blockIdx.x; tl < p.T; tl += gridDim.x) {
+    const int t = (int)tl;
+    const T* in = row_of<T>(FUSED ? (const void*)p.z : p.x, t, H);
+    const DropKey key = FUSED ? drop_key(p.drop) : DropKey{};
+    float sum[1] = {0.f}, sq[1] = {0.f};
+    for (int at = threadIdx.x * 8; at < H; at += step) {
+      Raw8<T> r = raw_zero<T>();
+      if (p.x) r = raw_load<T, TAIL>(row_of<T>(p.x, t, H), at, H);
+      if (FUSED) {
+        const Raw8<T> rv = raw_load<T, TAIL>(row_of<T>(p.v, t, H), at, H);
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = raw_get<T>(rv, x);
+        drop8(v, p.drop, key, (uint32_t)t, (uint32_t)(at / 8));
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] += raw_get<T>(r, x);
+        r = raw_pack<T>(v);
+        raw_store<T, TAIL>(row_of<T>(p.z, t, H), at, H, r);        // read again below by the same lane
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) sum[0] += raw_get<T>(r, x);
+    }
+    group_sum<1>(sum, blockDim.x, s_sum[0]);
+    const float mean = sum[0] / (float)H;                          // not * (1 / H): a constant row then has mean x, variance 0
+    for (int at = threadIdx.x * 8; at < H; at += step) {
+      const Raw8<T> r = raw_load<T, TAIL>(in, at, H);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const float d = raw_get<T>(r, x) - mean;
+        if (!TAIL || at + x < H) sq[0] += d * d;
+      }
+    }
+    group_sum<1>(sq, blockDim.x, s_sum[1]);
+    const float rstd = 1.0f / sqrtf(sq[0] / (float)H + p.eps);
+    if (threadIdx.x == 0) {
+      if (p.mean) p.mean[t] = mean;
+      if (p.rstd) p.rstd[t] = rstd;
+    }
+    for (int at = threadIdx.x * 8; at < H; at += step) {
+      const Raw8<T> r = raw_load<T, TAIL>(in, at, H);
+      Raw8<T> rg, rb;
+      if (p.gamma) rg = raw_load<T, TAIL>(static_cast<const T*>(p.gamma), at, H);
+      if (p.beta) rb = raw_load<T, TAIL>(static_cast<const T*>(p.beta), at, H);
+      float o[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        o[x] = (raw_get<T>(r, x) - mean) * rstd;
+        if (p.gamma) o[x] *= raw_get<T>(rg, x);
+        if (p.beta) o[x] += raw_get<T>(rb, x);
+      }
+      raw_store<T, TAIL>(row_of<T>(p.y, t, H), at, H, raw_pack<T>(o));
+    }
+  }
+}
+
+template <typename T, bool TAIL, bool FUSED>
+__global__ __launch_bounds__(1024) void norm_backward_long_kernel(NormBackwardParams p) {
+  __shared__ float s_sum[2][2][kRowMaxWaves];
+  const int H = p.H, step = blockDim.x * 8;
+  const DropKey key = FUSED ? drop_key(p.drop) : DropKey{};
+  int turn = 0;
+  for (long tl = blockIdx.x; tl < p.T; tl += gridDim.x, turn ^= 1) {
+    const int t = (int)tl;
+    const float mean = p.mean[t], rstd = p.rstd[t];
+    float sum[2] = {0.f, 0.f};
+    auto terms = [&](int at, float (&dxh)[8], float (&xh)[8]) __attribute__((always_inline)) {
+      const Raw8<T> rd = raw_load<T, TAIL>(row_of<T>(p.dy, t, H), at, H), rx = raw_load<T, TAIL>(row_of<T>(p.x, t, H), at, H);
+      Raw8<T> rg;
+      if (p.gamma) rg = raw_load<T, TAIL>(static_cast<const T*>(p.gamma), at, H);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        xh[x] = TAIL && at + x >= H ? 0.f : (raw_get<T>(rx, x) - mean) * rstd;
+        dxh[x] = raw_get<T>(rd, x);
+        if (p.gamma) dxh[x] *= raw_get<T>(rg, x);
+      }
+    };
+    for (int at = threadIdx.x * 8; at < H; at += step) {
+      float dxh[8], xh[8];
+      terms(at, dxh, xh);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        sum[0] += dxh[x];
+        sum[1] += dxh[x] * xh[x];
+      }
+    }
+    group_sum<2>(sum, blockDim.x, &s_sum[turn][0][0]);
+    const float m1 = sum[0] * p.inv_h, m2 = sum[1] * p.inv_h;
+    for (int at = threadIdx.x * 8; at < H; at += step) {
+      float dxh[8], xh[8], o[8];
+      terms(at, dxh, xh);
+      Raw8<T> rr = raw_zero<T>();
+      if (p.dres) rr = raw_load<T, TAIL>(row_of<T>(p.dres, t, H), at, H);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) o[x] = rstd * (dxh[x] - m1 - xh[x] * m2) + raw_get<T>(rr, x);
+      raw_store<T, TAIL>(row_of<T>(p.dx, t, H), at, H, raw_pack<T>(o));
+      if (FUSED) {
+        drop8(o, p.drop, key, (uint32_t)t, (uint32_t)(at / 8));
+        raw_store<T, TAIL>(row_of<T>(p.dv, t, H), at, H, raw_pack<T>(o));
+      }
+    }
+  }
+}
+
+// Column sums of the long rows: a lane has eight columns, a workgroup column (blockIdx.y) a share of the rows.
+template <typename T, bool TAIL>
+__global__ __launch_bounds__(256) void norm_columns_long_kernel(NormBackwardParams p) {
+  const int H = p.H, at = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (at >= H) return;
+  float acc_g[8], acc_b[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) acc_g[x] = acc_b[x] = 0.f;
+  for (long tl = blockIdx.y; tl < p.T; tl += gridDim.y) {
+    const int t = (int)tl;
+    const Raw8<T> rd = raw_load<T, TAIL>(row_of<T>(p.dy, t, H), at, H), rx = raw_load<T, TAIL>(row_of<T>(p.x, t, H), at, H);
+    const float mean = p.mean[t], rstd = p.rstd[t];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const float d = raw_get<T>(rd, x);
+      acc_g[x] += d * ((raw_get<T>(rx, x) - mean) * rstd);
+      acc_b[x] += d;
+    }
+  }
+  float* out = p.part + (size_t)blockIdx.y * 2 * H;
+#pragma unroll
+  for (int x = 0; x < 8; ++x)
+    if (!TAIL || at + x < H) {
+      out[at + x] = acc_g[x];
+      out[H + at + x] = acc_b[x];
+    }
+}
+
+// dgamma, dbeta from the partial sums: a workgroup adds 64 columns of one of the two, 16 waves a sixteenth of the partials each.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_columns_kernel(const float* part, int parts, int H, void* dgamma, void* dbeta) {
+  __shared__ float s[kRowMaxWaves][kWave];
+  const int wave = threadIdx.x / kWave, lane = lane_id();
+  const int col = blockIdx.x * kWave + lane;
+  T* out = static_cast<T*>(blockIdx.y ? dbeta : dgamma);
+  if (!out) return;
+  float a = 0.f;
+  if (col < H) {
+    const float* src = part + (size_t)blockIdx.y * H + col;
+#pragma unroll 8
+    for (int i = wave; i < parts; i += kRowMaxWaves) a += src[(size_t)i * 2 * H];
+  }
+  s[wave][lane] = a;
+  __syncthreads();
+  if (wave == 0 && col < H) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRowMaxWaves; ++w) t += s[w][lane];
+    out[col] = (T)t;
+  }
+}
+
+// ---- dropout + residual alone (and its backward: no residual): a lane per vector ----
+struct DropAddParams {
+  const void *v, *res;            // res may be null
+  void* out;
+  DropParams drop;
+  int T, H, group;                // lanes per row: a power of two up to 256
+};
+
+template <typename T, bool TAIL>
+__global__ __launch_bounds__(256) void drop_add_kernel(DropAddParams p) {
+  const int H = p.H, rows = 256 / p.group, chunks = (H + p.group * 8 - 1) / (p.group * 8);
+  const int r = threadIdx.x / p.group, g = threadIdx.x & (p.group - 1);
+  const DropKey key = drop_key(p.drop);
+  const long tasks = (long)((p.T + rows - 1) / rows) * chunks;
+  for (long task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const long rb = task / chunks;
+    const int vec = (int)(task - rb * chunks) * p.group + g, at = vec * 8;
+    const long t = rb * rows + r;
+    if (t >= p.T || at >= H) continue;
+    const Raw8<T> rv = raw_load<T, TAIL>(row_of<T>(p.v, (int)t, H), at, H);
+    Raw8<T> rr = raw_zero<T>();
+    if (p.res) rr = raw_load<T, TAIL>(row_of<T>(p.res, (int)t, H), at, H);
+    float v[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x] = raw_get<T>(rv, x);
+    drop8(v, p.drop, key, (uint32_t)t, (uint32_t)vec);
+    if (p.res)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[x] += raw_get<T>(rr, x);
+    raw_store<T, TAIL>(row_of<T>(p.out, (int)t, H), at, H, raw_pack<T>(v));
+  }
+}
+
+}  // namespace moe

@@ -10,6 +10,7 @@
 
 #include "backward.h"
 #include "common.h"
+#include "experts_w4_launch.h"
 #include "gemm_bf16.h"
 #include "gemm_f32.h"
 #include "gemm_stream.h"
@@ -947,6 +948,29 @@ int moe_ffn_forward(const MoeShape* shape, const void* d_x, const float* d_logit
   const bool copies = mode == MOE_MODE_SERIALIZED && !gathers_x(c) && c.s.T > kRouteOneT;
   if ((st = run_route(c, d_logits, mode == MOE_MODE_PERSISTENT, nullptr, copies ? d_x : nullptr)) != MOE_OK) return st;
   return run_dispatch_to_combine(c, d_x, d_w_gate_up, d_w_down, d_out, mode, copies);
+}
+
+int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_logits, const void* d_q_gate_up,
+                       const void* d_s_gate_up, const void* d_q_down, const void* d_s_down, void* d_out, const MoeSaved* saved,
+                       void* d_workspace, size_t workspace_bytes, void* stream) {
+  Ctx c;
+  int st = make_ctx(c, shape, saved, d_workspace, workspace_bytes, stream);
+  if (st != MOE_OK) return st;
+  if (c.s.dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
+  if (c.s.T == 0) return MOE_OK;
+  const void* ptrs[] = {d_x, d_logits, d_q_gate_up, d_s_gate_up, d_q_down, d_s_down, d_out};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if ((st = run_route(c, d_logits, false)) != MOE_OK) return st;
+  // GEMM-2's rows in fp32, [R_max,H], over what the bf16 layer uses for Xp and half of A and Yp behind it; A follows.  (The three are
+  // 2 R_max (2 H + I) bytes; rows of H fp32 are multiples of 256 bytes.)
+  float* y = reinterpret_cast<float*>(c.ws + c.L.Xp);
+  void* a = c.ws + c.L.Xp + (size_t)r_max(c.s) * c.s.H * 4;
+  const W4Launch g1 = {d_x, c.sv.token_of, d_q_gate_up, d_s_gate_up, c.sv.offsets, a, c.s.E_local, c.s.H, c.s.I};
+  const W4Launch g2 = {a, nullptr, d_q_down, d_s_down, c.sv.offsets, y, c.s.E_local, c.s.I, c.s.H};
+  if ((st = launch_experts_w4(g1, true, stream)) != MOE_OK) return st;
+  if ((st = launch_experts_w4(g2, false, stream)) != MOE_OK) return st;
+  return launch_combine_w4(y, c.sv.row_of, c.sv.topk_w, d_out, c.s.T, c.s.H, c.s.k, stream);
 }
 
 int moe_ffn_backward(const MoeShape* shape, const void* d_dy, const void* d_x, const void* d_w_gate_up,

@@ -29,13 +29,8 @@ TRACE_LIB = os.path.join(HERE, "libmoe_ffn_trace.so")
 
 
 def build_trace_library() -> str:
-    from .build import HIPCC_FLAGS, SOURCES
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, "-DMOE_SCHED_TRACE", *SOURCES, "-o", TRACE_LIB]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
-    return TRACE_LIB
+    from .build import build_library
+    return build_library(out=TRACE_LIB, defines=["-DMOE_SCHED_TRACE"])
 
 
 def main():
