@@ -342,10 +342,10 @@ def _arg(t: Optional[torch.Tensor], shape, dtype, name: str):
     """Device address of a tensor of this shape and type; None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or tuple(t.shape) != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous device tensor of shape {shape} and type {dtype}, got {tuple(t.shape)}, "
-                         f"{t.dtype}, {t.device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous device tensor of shape {shape} and type {dtype}, got {tuple(t.shape)}, {t.dtype}, "
+                     f"{t.device}")
 
 
 def _rows(t: torch.Tensor, name: str):
@@ -357,7 +357,7 @@ def _rows(t: torch.Tensor, name: str):
 
 
 def _raw_stream(stream) -> int:
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _drop_rng(rng: Optional[torch.Tensor]):

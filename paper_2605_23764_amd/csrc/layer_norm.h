@@ -43,59 +43,92 @@ template <typename T> __device__ __forceinline__ const T* row_of(const void* p, 
 }
 template <typename T> __device__ __forceinline__ T* row_of(void* p, int t, int H) { return static_cast<T*>(p) + (size_t)t * H; }
 
-// One row per group of lanes; rows of up to 64 vectors share a workgroup.
-template <typename T, bool TAIL, bool FUSED>
-__global__ __launch_bounds__(1024) void norm_forward_kernel(NormForwardParams p) {
+// A group of lanes per row, ITEMS vectors per lane; groups of up to a wave share a workgroup.  Workgroups walk rows in strides, the next
+// row's loads under way while this one is reduced, with gamma and beta in registers.
+template <typename T, int ITEMS, bool TAIL, bool FUSED>
+__global__ __launch_bounds__(512) void norm_forward_kernel(NormForwardParams p) {
   __shared__ float s_sum[2][kRowMaxWaves];
   const int G = p.group, H = p.H;
-  const int g = G > kWave ? (int)threadIdx.x : (int)threadIdx.x & (G - 1), at = g * 8;
-  const int rows = G > kWave ? 1 : blockDim.x / G;
-  for (long t0 = (long)blockIdx.x * rows; t0 < p.T; t0 += (long)gridDim.x * rows) {
-    const int t = (int)min(t0 + (G > kWave ? 0 : (int)threadIdx.x / G), (long)p.T);
-    const bool in = t < p.T && at < H;
-    Raw8<T> rx = raw_zero<T>(), rg = raw_zero<T>(), rb = raw_zero<T>();
-    if (in) {
-      if (p.x) rx = raw_load<T, TAIL>(row_of<T>(p.x, t, H), at, H);
-      Raw8<T> rv;
-      if (FUSED) rv = raw_load<T, TAIL>(row_of<T>(p.v, t, H), at, H);
-      if (p.gamma) rg = raw_load<T, TAIL>(static_cast<const T*>(p.gamma), at, H);
-      if (p.beta) rb = raw_load<T, TAIL>(static_cast<const T*>(p.beta), at, H);
-      if (FUSED) {
-        float v[8];
+  const int g = G > kWave ? (int)threadIdx.x : (int)threadIdx.x & (G - 1);
+  const int rows = G > kWave ? 1 : blockDim.x / G, r = G > kWave ? 0 : threadIdx.x / G;
+  const DropKey key = FUSED ? drop_key(p.drop) : DropKey{};
+  Raw8<T> gamma[ITEMS], beta[ITEMS];
 #pragma unroll
-        for (int x = 0; x < 8; ++x) v[x] = raw_get<T>(rv, x);
-        drop8(v, p.drop, drop_key(p.drop), (uint32_t)t, (uint32_t)g);
+  for (int i = 0; i < ITEMS; ++i) {
+    const int at = (i * G + g) * 8;
+    gamma[i] = p.gamma && at < H ? raw_load<T, TAIL>(static_cast<const T*>(p.gamma), at, H) : raw_zero<T>();
+    beta[i] = p.beta && at < H ? raw_load<T, TAIL>(static_cast<const T*>(p.beta), at, H) : raw_zero<T>();
+  }
+  struct Row { Raw8<T> x[ITEMS], v[FUSED ? ITEMS : 1]; };
+  auto load = [&](Row& q, long t) __attribute__((always_inline)) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) v[x] += raw_get<T>(rx, x);
-        rx = raw_pack<T>(v);                                       // z is an output, and y the norm of it as it is stored
-        raw_store<T, TAIL>(row_of<T>(p.z, t, H), at, H, rx);
+    for (int i = 0; i < ITEMS; ++i) {
+      const int at = (i * G + g) * 8;
+      q.x[i] = raw_zero<T>();
+      if (FUSED) q.v[i] = raw_zero<T>();
+      if (t < p.T && at < H) {
+        if (p.x) q.x[i] = raw_load<T, TAIL>(row_of<T>(p.x, (int)t, H), at, H);
+        if (FUSED) q.v[i] = raw_load<T, TAIL>(row_of<T>(p.v, (int)t, H), at, H);
       }
     }
+  };
+  const long stride = (long)gridDim.x * rows;
+  Row cur;
+  load(cur, (long)blockIdx.x * rows + r);
+  for (long t0 = (long)blockIdx.x * rows; t0 < p.T; t0 += stride) {
+    const int t = (int)min(t0 + r, (long)p.T);
+    Row next;
+    load(next, t0 + r + stride);
     float sum[1] = {0.f}, sq[1] = {0.f};
 #pragma unroll
-    for (int x = 0; x < 8; ++x) sum[0] += raw_get<T>(rx, x);       // 0 outside the row
-    group_sum<1>(sum, G, s_sum[0]);
-    const float mean = sum[0] / (float)H;                          // not * (1 / H): a constant row then has mean x, variance 0
+    for (int i = 0; i < ITEMS; ++i) {
+      const int vec = i * G + g, at = vec * 8;
+      if (FUSED && t < p.T && at < H) {
+        float v[8];
 #pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      const float d = raw_get<T>(rx, x) - mean;
-      if (TAIL ? at + x < H : at < H) sq[0] += d * d;
+        for (int x = 0; x < 8; ++x) v[x] = raw_get<T>(cur.v[i], x);
+        drop8(v, p.drop, key, (uint32_t)t, (uint32_t)vec);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] += raw_get<T>(cur.x[i], x);
+        cur.x[i] = raw_pack<T>(v);                               // z is an output, and y the norm of it as it is stored
+        raw_store<T, TAIL>(row_of<T>(p.z, t, H), at, H, cur.x[i]);
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) sum[0] += raw_get<T>(cur.x[i], x);                    // 0 outside the row
+    }
+    group_sum<1>(sum, G, s_sum[0]);
+    const float mean = sum[0] / (float)H;                        // not * (1 / H): a constant row then has mean x, variance 0
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int at = (i * G + g) * 8;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const float d = raw_get<T>(cur.x[i], x) - mean;
+        if (TAIL ? at + x < H : at < H) sq[0] += d * d;
+      }
     }
     group_sum<1>(sq, G, s_sum[1]);
     const float rstd = 1.0f / sqrtf(sq[0] / (float)H + p.eps);
-    if (!in) continue;
-    if (g == 0) {
-      if (p.mean) p.mean[t] = mean;
-      if (p.rstd) p.rstd[t] = rstd;
-    }
-    float o[8];
+    if (t < p.T) {
+      if (g == 0) {
+        if (p.mean) p.mean[t] = mean;
+        if (p.rstd) p.rstd[t] = rstd;
+      }
 #pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      o[x] = (raw_get<T>(rx, x) - mean) * rstd;
-      if (p.gamma) o[x] *= raw_get<T>(rg, x);
-      if (p.beta) o[x] += raw_get<T>(rb, x);
+      for (int i = 0; i < ITEMS; ++i) {
+        const int at = (i * G + g) * 8;
+        if (at >= H) continue;
+        float o[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          o[x] = (raw_get<T>(cur.x[i], x) - mean) * rstd;
+          if (p.gamma) o[x] *= raw_get<T>(gamma[i], x);
+          if (p.beta) o[x] += raw_get<T>(beta[i], x);
+        }
+        raw_store<T, TAIL>(row_of<T>(p.y, t, H), at, H, raw_pack<T>(o));
+      }
     }
-    raw_store<T, TAIL>(row_of<T>(p.y, t, H), at, H, raw_pack<T>(o));
+    cur = next;
   }
 }
 
