@@ -20,8 +20,11 @@
 namespace moe {
 
 constexpr int kW4Waves = 4;                // waves of a workgroup, each with a share of K
-constexpr int kW4Rows = 64;                // rows in hand at a time, at most
-constexpr int kW4Blocks = 2;               // 16-column blocks of an item
+// Waves per SIMD that the registers have to leave room for.  A wave has one step of its share in registers and no more (a ring of two or
+// three steps: 2 to 30 % slower), so the bytes under way come from the number of waves.
+constexpr int w4_occupancy(int row_blocks, int blocks) { return row_blocks == 2 ? 3 : blocks == 4 ? 4 : 5; }
+// Output columns of an item of `blocks` 16-column blocks; SwiGLU: half of them gate, half the matching up columns.
+constexpr int w4_columns(int blocks, bool swiglu) { return swiglu ? 8 * blocks : 16 * blocks; }
 
 struct W4Params {
   const __bf16* x;               // activations, rows of K
@@ -40,66 +43,76 @@ __device__ __forceinline__ bf16x8 w4_bf16(uint32_t w, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Rows row0 + m0 .. (up to 16 RT) of an expert with rows n_rows, times the item's columns.
-template <int RT, bool SWIGLU>
+// A buffer descriptor over `bytes` from p (the same in all lanes): what a lane asks for beyond is 0 and costs no memory access.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t w4_buffer(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000);
+}
+constexpr uint32_t kW4Beyond = 0x80000000u;   // an offset past every buffer here
+constexpr int kW4Nt = 2;                      // non-temporal: a block is read once
+
+// Rows row0 + m0 .. (up to 16 RT) of an expert with n_rows rows, times the NB column blocks of an item.
+template <int RT, int NB, bool SWIGLU>
 __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, const uint8_t* scale, int item, int row0, int m0, int n_rows,
                                         float* s_acc) {
-  constexpr int NB = kW4Blocks;
+  constexpr int kCols = w4_columns(NB, SWIGLU);
   const int lane = lane_id(), l16 = lane & 15, lq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int groups = p.K / 32;
-  // a lane's column of each block: 16 gate and the matching up columns, or 32 in a row
-  size_t at[NB];
-  const __bf16* xr[RT];
-  bool live[RT];
+  const int groups = p.K / 32, steps = (groups + 3) / 4;         // a step: 128 k, four blocks of every column
+  const int s0 = steps * wave / kW4Waves, n = steps * (wave + 1) / kW4Waves - s0;
+  // this wave's blocks: from its first step to its last, no further than the matrix (the last step may hold two blocks)
+  const int g0 = s0 * 4, n_groups = min((s0 + n) * 4, groups) - g0;
+  const __amdgpu_buffer_rsrc_t bq = w4_buffer(q + (size_t)g0 * p.cols * 16, (uint32_t)n_groups * p.cols * 16);
+  const __amdgpu_buffer_rsrc_t bs = w4_buffer(scale + (size_t)g0 * p.cols, (uint32_t)n_groups * p.cols);
+  uint32_t at[NB];                                               // block of this lane in step 0
 #pragma unroll
-  for (int b = 0; b < NB; ++b) at[b] = (SWIGLU ? b * p.N + item * 16 : item * 32 + b * 16) + l16;
+  for (int b = 0; b < NB; ++b) at[b] = lq * p.cols + item * kCols + (SWIGLU ? (b >= NB / 2 ? p.N : 0) + b % (NB / 2) * 16 : b * 16) + l16;
+  u32x4 w[NB];
+  uint32_t sc[NB];
+  bf16x8 x[RT][4];
+  auto request_w = [&](int b, int s) __attribute__((always_inline)) {   // past the wave's share: nothing
+    const uint32_t blk = at[b] + (uint32_t)s * 4 * p.cols;
+    w[b] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(bq, blk * 16, 0, kW4Nt));
+    sc[b] = __builtin_amdgcn_raw_buffer_load_b8(bs, blk, 0, 0);
+  };
+#pragma unroll
+  for (int b = 0; b < NB; ++b) request_w(b, 0);                  // ahead of the permutation's lookup
+  // activations: rows past the expert's last one, and k past the wave's share, read zeros
+  const __amdgpu_buffer_rsrc_t bx = w4_buffer(p.gather ? p.x : p.x + (size_t)(row0 + m0) * p.K, 0x7FFFFFFFu);
+  uint32_t xo[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const int m = m0 + r * 16 + l16;
-    live[r] = m < n_rows;
-    const int row = live[r] ? (p.gather ? p.gather[row0 + m] : row0 + m) : 0;
-    xr[r] = p.x + (size_t)row * p.K;
+    const int m = r * 16 + l16;
+    xo[r] = kW4Beyond;
+    if (m0 + m < n_rows) xo[r] = (uint32_t)(p.gather ? p.gather[row0 + m0 + m] : m) * (uint32_t)(p.K * 2) + (uint32_t)(g0 + lq) * 64;
   }
+  auto request_x = [&](int s) __attribute__((always_inline)) {
+    const bool in = s * 4 + lq < n_groups;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const uint32_t o = in ? xo[r] + (uint32_t)s * 256 : kW4Beyond;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[r][i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(bx, o + i * 16, 0, 0));
+    }
+  };
+  request_x(0);
   f32x4 acc[RT][NB];
 #pragma unroll
   for (int r = 0; r < RT; ++r)
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[r][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int steps = (groups + 3) / 4;
-  const int s0 = steps * wave / kW4Waves, s1 = steps * (wave + 1) / kW4Waves;
-  for (int s = s0; s < s1; ++s) {
-    const int g = s * 4 + lq;
-    const bool in = g < groups;                                  // the last step may hold two groups
-    u32x4 w[NB];
-    float sc[NB];
+  for (int s = 0; s < n; ++s) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      w[b] = u32x4{0, 0, 0, 0};
-      sc[b] = 1.f;
-      if (in) {
-        const size_t blk = (size_t)g * p.cols + at[b];
-        w[b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(q + blk * 16));
-        sc[b] = __builtin_bit_cast(float, (uint32_t)scale[blk] << 23);
-      }
+      bf16x8 wf[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wf[i] = w4_bf16(w[b][i], __builtin_bit_cast(float, sc[b] << 23));
+      request_w(b, s + 1);                                       // as soon as the registers are free
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[i], x[r][i], acc[r][b], 0, 0, 0);
     }
-    bf16x8 x[RT][4];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        u32x4 v = {0, 0, 0, 0};
-        if (live[r] && in) v = *reinterpret_cast<const u32x4*>(xr[r] + g * 32 + i * 8);
-        x[r][i] = __builtin_bit_cast(bf16x8, v);
-      }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const bf16x8 wf = w4_bf16(w[b][i], sc[b]);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) acc[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, x[r][i], acc[r][b], 0, 0, 0);
-      }
+    request_x(s + 1);
   }
   // the waves' shares of K meet: row block r is joined by wave r
 #pragma unroll
@@ -120,32 +133,36 @@ __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, con
     if (m < n_rows) {
       const size_t row = (size_t)(row0 + m) * p.N;
       if constexpr (SWIGLU) {
-        float a[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) a[c] = t[0][c] * sigmoid_bf16_(t[0][c]) * t[NB - 1][c];
-        *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.out) + row + item * 16 + lq * 4) = u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
+        for (int b = 0; b < NB / 2; ++b) {
+          float a[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) a[c] = t[b][c] * sigmoid_bf16_(t[b][c]) * t[b + NB / 2][c];
+          *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.out) + row + item * kCols + b * 16 + lq * 4) =
+              u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
+        }
       } else {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + row + item * 32 + b * 16 + lq * 4) = t[b];
+        for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + row + item * kCols + b * 16 + lq * 4) = t[b];
       }
     }
   }
 }
 
-// An item per workgroup: blockIdx.x = expert * n_items + item.
-template <bool SWIGLU>
-__global__ __launch_bounds__(kW4Waves* kWave) void experts_w4_kernel(W4Params p) {
-  __shared__ __align__(16) float s_acc[kW4Waves * (kW4Rows / 16) * kW4Blocks * kWave * 4];
-  const int e = blockIdx.x / p.n_items, item = blockIdx.x - e * p.n_items;
+// An item per workgroup.  The dispatcher deals consecutive workgroups to the eight dies in turn; consecutive items, whose blocks and above
+// all scales share lines, go to one die instead, eight at a time.
+template <int RT, int NB, bool SWIGLU>
+__global__ __launch_bounds__(kW4Waves* kWave, w4_occupancy(RT, NB)) void experts_w4_kernel(W4Params p) {
+  __shared__ __align__(16) float s_acc[kW4Waves * RT * NB * kWave * 4];
+  int id = blockIdx.x;
+  if ((id | 63) < (int)gridDim.x) id = (id & ~63) | (id & 7) << 3 | (id >> 3 & 7);
+  const int e = id / p.n_items, item = id - e * p.n_items;
   const int row0 = p.offsets[e], rows = p.offsets[e + 1] - row0;
-  if (rows <= 0) return;
   const size_t blocks = (size_t)e * (p.K / 32) * p.cols;
-  const uint8_t *q = p.q + blocks * 16, *scale = p.scale + blocks;
-  for (int m0 = 0; m0 < rows; m0 += kW4Rows) {
+#pragma unroll 1
+  for (int m0 = 0; m0 < rows; m0 += RT * 16) {                   // no rows: the weights are not touched
     if (m0) __syncthreads();                                     // s_acc has been read
-    if (rows - m0 <= 16) w4_rows<1, SWIGLU>(p, q, scale, item, row0, m0, rows, s_acc);
-    else if (rows - m0 <= 32) w4_rows<2, SWIGLU>(p, q, scale, item, row0, m0, rows, s_acc);
-    else w4_rows<4, SWIGLU>(p, q, scale, item, row0, m0, rows, s_acc);
+    w4_rows<RT, NB, SWIGLU>(p, p.q + blocks * 16, p.scale + blocks, item, row0, m0, rows, s_acc);
   }
 }
 

@@ -11,6 +11,8 @@ struct W4Launch {
   const int32_t* offsets;
   void* out;
   int E_local, K, N;
+  int experts;                   // experts with rows, at most
+  int rows;                      // of an expert, on average
 };
 
 // swiglu: N bf16 columns from N gate and N up columns; otherwise N fp32 columns.  Returns a MoeStatus, as the next.

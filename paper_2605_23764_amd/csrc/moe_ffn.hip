@@ -961,13 +961,21 @@ int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_lo
   const void* ptrs[] = {d_x, d_logits, d_q_gate_up, d_s_gate_up, d_q_down, d_s_down, d_out};
   for (const void* q : ptrs)
     if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if ((double)c.s.H * c.s.I >= 2147483648.0) return MOE_ERR_UNSUPPORTED_SHAPE;   // an expert's blocks: 31-bit offsets
   if ((st = run_route(c, d_logits, false)) != MOE_OK) return st;
   // GEMM-2's rows in fp32, [R_max,H], over what the bf16 layer uses for Xp and half of A and Yp behind it; A follows.  (The three are
   // 2 R_max (2 H + I) bytes; rows of H fp32 are multiples of 256 bytes.)
   float* y = reinterpret_cast<float*>(c.ws + c.L.Xp);
   void* a = c.ws + c.L.Xp + (size_t)r_max(c.s) * c.s.H * 4;
-  const W4Launch g1 = {d_x, c.sv.token_of, d_q_gate_up, d_s_gate_up, c.sv.offsets, a, c.s.E_local, c.s.H, c.s.I};
-  const W4Launch g2 = {a, nullptr, d_q_down, d_s_down, c.sv.offsets, y, c.s.E_local, c.s.I, c.s.H};
+  const int experts = (int)std::min((long)c.s.E_local, (long)c.s.T * c.s.k), rows = (int)((long)c.s.T * c.s.k / c.s.E);
+  W4Launch g1 = {d_x, c.sv.token_of, d_q_gate_up, d_s_gate_up, c.sv.offsets, a, c.s.E_local, c.s.H, c.s.I, experts, rows};
+  if ((size_t)c.s.T * c.s.H * 2 >= ((size_t)1 << 31)) {          // 31-bit offsets of the gathered rows: a permuted copy, read before y is written
+    c.sv.Xp = y;
+    if ((st = run_permute(c, d_x)) != MOE_OK) return st;
+    g1.x = y;
+    g1.gather = nullptr;
+  }
+  const W4Launch g2 = {a, nullptr, d_q_down, d_s_down, c.sv.offsets, y, c.s.E_local, c.s.I, c.s.H, experts, rows};
   if ((st = launch_experts_w4(g1, true, stream)) != MOE_OK) return st;
   if ((st = launch_experts_w4(g2, false, stream)) != MOE_OK) return st;
   return launch_combine_w4(y, c.sv.row_of, c.sv.topk_w, d_out, c.s.T, c.s.H, c.s.k, stream);
