@@ -55,6 +55,12 @@ template <typename F> void with_row_form(int dtype, int H, F&& f) {
   else tail(float{});
 }
 
+// Arrays that are read or written once: by way of the caches or not.
+template <typename T, typename F> void with_caching(int rows, int H, F&& f) {
+  if ((size_t)rows * H * sizeof(T) > kNormNtBytes) f(std::true_type{});
+  else f(std::false_type{});
+}
+
 // One vector per lane up to a wave's worth, two beyond.  A launch has the workgroups that run at a time (about 21 waves per CU by their
 // registers; 7, 14 and 28 waves of them: within 0.3 % of each other), which walk on in strides.
 template <bool FUSED> int run_norm_forward(NormForwardParams p, int dtype, hipStream_t s) {
@@ -69,8 +75,10 @@ template <bool FUSED> int run_norm_forward(NormForwardParams p, int dtype, hipSt
     const int rows = p.group > kWave ? 1 : 256 / p.group, threads = p.group * rows;
     const int most = 256 * (threads > 768 ? 1 : 1536 / threads), want = ceil_div(p.T, rows);
     const dim3 grid(want < most ? want : most);
-    if (vecs <= kWave) hipLaunchKernelGGL((norm_forward_kernel<T, 1, tail.value, FUSED>), grid, dim3(threads), 0, s, p);
-    else hipLaunchKernelGGL((norm_forward_kernel<T, 2, tail.value, FUSED>), grid, dim3(threads), 0, s, p);
+    with_caching<T>(p.T, p.H, [&](auto nt) {
+      if (vecs <= kWave) hipLaunchKernelGGL((norm_forward_kernel<T, 1, tail.value, FUSED, nt.value>), grid, dim3(threads), 0, s, p);
+      else hipLaunchKernelGGL((norm_forward_kernel<T, 2, tail.value, FUSED, nt.value>), grid, dim3(threads), 0, s, p);
+    });
   });
   return launched();
 }
@@ -97,8 +105,10 @@ template <bool FUSED> int run_norm_backward(NormBackwardParams p, int dtype, voi
       while (p.groups > 1 && p.groups * p.group > kWave && p.T < 256 * p.groups) p.groups /= 2;
       const int want = ceil_div(p.T, p.groups);
       parts = want < 256 ? want : 256;
-      const size_t lds = (size_t)(p.groups - 1) * p.group * 64;
-      hipLaunchKernelGGL((norm_backward_kernel<T, tail.value, FUSED>), dim3(parts), dim3(p.group * p.groups), lds, s, p);
+      const size_t lds = p.groups > 1 ? (size_t)p.groups * p.group * 64 : 0;
+      with_caching<T>(p.T, p.H, [&](auto nt) {
+        hipLaunchKernelGGL((norm_backward_kernel<T, tail.value, FUSED, nt.value>), dim3(parts), dim3(p.group * p.groups), lds, s, p);
+      });
     }
     if (sums)
       hipLaunchKernelGGL(norm_columns_kernel<T>, dim3(ceil_div(p.H, kWave), 2), dim3(1024), 0, s, p.part, parts, p.H, dgamma, dbeta);
@@ -117,17 +127,24 @@ int run_drop_add(DropAddParams p, int dtype, hipStream_t s) {
   return launched();
 }
 
-int token_lanes(int E) {
-  int l = 1;
-  while (l * 4 < E) l *= 2;
-  return l;
+// Lanes per token (four experts each, a power of two) x E % 4 != 0
+template <typename F> void with_token_form(int E, F&& f) {
+  auto tail = [&](auto lanes) {
+    if (E % 4) f(lanes, std::true_type{});
+    else f(lanes, std::false_type{});
+  };
+  if (E <= 4) tail(std::integral_constant<int, 1>{});
+  else if (E <= 8) tail(std::integral_constant<int, 2>{});
+  else if (E <= 16) tail(std::integral_constant<int, 4>{});
+  else if (E <= 32) tail(std::integral_constant<int, 8>{});
+  else if (E <= 64) tail(std::integral_constant<int, 16>{});
+  else if (E <= 128) tail(std::integral_constant<int, 32>{});
+  else tail(std::integral_constant<int, 64>{});
 }
 
 int check_router(int T, int E, int k) {
   return T < 0 || k < 1 || k > kMaxK || E < k || E > kMaxE ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
 }
-
-constexpr size_t kBalPartN = (size_t)kBalMaxParts * (kMaxE + 4) * 4;   // the counts in front, the probabilities behind
 
 }  // namespace
 
@@ -241,7 +258,7 @@ int moe_balance_workspace_bytes(int32_t T, int32_t E, size_t* bytes) {
   const int st = check_router(T, E, 1);
   if (st != MOE_OK) return st;
   if (!bytes) return MOE_ERR_INVALID_ARG;
-  *bytes = kBalPartN + (size_t)kBalMaxParts * kMaxE * 4;
+  *bytes = (size_t)kBalMaxParts * (kMaxE + 1) * 8;
   return MOE_OK;
 }
 
@@ -257,13 +274,14 @@ int moe_balance_forward(int32_t T, int32_t E, int32_t k, const float* d_logits, 
   if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
   BalanceParams p{};
   p.logits = d_logits; p.topk_idx = d_topk_idx; p.mask = d_mask; p.counts = d_counts; p.prob_sum = d_prob_sum; p.loss = d_loss;
-  p.part_n = static_cast<int32_t*>(d_workspace);
-  p.part_p = reinterpret_cast<float*>(static_cast<char*>(d_workspace) + kBalPartN);
-  p.coef = coef; p.T = T; p.E = E; p.k = k; p.lanes = token_lanes(E);
-  const int want = ceil_div(T, kBalThreads / p.lanes);
-  p.parts = T <= kBalOneT ? 1 : want < kBalMaxParts ? want : kBalMaxParts;
+  p.part = static_cast<u32x2*>(d_workspace);
+  p.coef = coef; p.T = T; p.E = E; p.k = k;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(balance_kernel, dim3(p.parts), dim3(kBalThreads), 0, s, p);
+  with_token_form(E, [&](auto lanes, auto tail) {
+    const int want = ceil_div(T, kBalThreads / lanes.value);
+    p.parts = T <= kBalOneT ? 1 : want < kBalMaxParts ? want : kBalMaxParts;
+    hipLaunchKernelGGL((balance_kernel<lanes.value, tail.value>), dim3(p.parts), dim3(kBalThreads), 0, s, p);
+  });
   if (p.parts > 1) hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(1024), 0, s, p);
   return launched();
 }
@@ -280,9 +298,14 @@ int moe_router_backward(int32_t T, int32_t E, int32_t k, const float* d_logits, 
     return MOE_ERR_INVALID_ARG;
   RouterBackwardParams p{};
   p.logits = d_logits; p.topk_idx = d_topk_idx; p.topk_w = d_topk_w; p.dtopk_w = d_dtopk_w; p.mask = d_mask; p.counts = d_counts;
-  p.dloss = d_dloss; p.dlogits = d_dlogits; p.coef = coef; p.T = T; p.E = E; p.k = k; p.lanes = token_lanes(E);
-  const int want = ceil_div(T, kBalThreads / p.lanes);
-  hipLaunchKernelGGL(router_backward_kernel, dim3(want < 2048 ? want : 2048), dim3(kBalThreads), 0, static_cast<hipStream_t>(stream), p);
+  p.dloss = d_dloss; p.dlogits = d_dlogits; p.coef = coef; p.T = T; p.E = E; p.k = k;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  with_token_form(E, [&](auto lanes, auto tail) {
+    const int want = ceil_div(T, kRouterThreads / lanes.value * kRouterAhead);
+    const dim3 grid(want < 2048 ? want : 2048);
+    if (p.topk_w) hipLaunchKernelGGL((router_backward_kernel<lanes.value, tail.value, true>), grid, dim3(kRouterThreads), 0, s, p);
+    else hipLaunchKernelGGL((router_backward_kernel<lanes.value, tail.value, false>), grid, dim3(kRouterThreads), 0, s, p);
+  });
   return launched();
 }
 
