@@ -26,21 +26,60 @@ template <typename T> __device__ __forceinline__ Raw8<T> raw_zero() {
   return r;
 }
 
-// Elements i .. i + 7 of a row of H; those past the end are zero.
-template <typename T, bool TAIL> __device__ __forceinline__ Raw8<T> raw_load(const T* row, int i, int H) {
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element's address
+
+// Elements i .. i + 7 of a row of H; those past the end are zero.  A short last vector is the row's last eight elements moved down, one
+// load like the others' (in rows of fewer than eight, element by element).  NT: non-temporal, for what is read once and larger than the
+// caches.
+template <typename T, bool TAIL, bool NT = false> __device__ __forceinline__ Raw8<T> raw_load(const T* row, int i, int H) {
   Raw8<T> r;
-  if (!TAIL || i + 8 <= H) {
-    __builtin_memcpy(&r, row + i, sizeof(r));
-  } else {
+  constexpr int kWords = sizeof(r) / 4;
+  if (TAIL && H < 8) {
     r = raw_zero<T>();
 #pragma unroll
     for (int x = 0; x < 7; ++x)
-      if (i + x < H) {
-        if constexpr (sizeof(T) == 2) r.w[x >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, row[i + x]) << (16 * (x & 1));
-        else r.w[x] = __builtin_bit_cast(uint32_t, row[i + x]);
+      if (x < H) {
+        if constexpr (sizeof(T) == 2) r.w[x >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, row[x]) << (16 * (x & 1));
+        else r.w[x] = __builtin_bit_cast(uint32_t, row[x]);
       }
+    return r;
+  }
+  const u32x4_any* src = reinterpret_cast<const u32x4_any*>(row + (TAIL ? min(i, H - 8) : i));
+#pragma unroll
+  for (int v = 0; v < kWords / 4; ++v) {
+    const u32x4_any a = NT ? __builtin_nontemporal_load(src + v) : src[v];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) r.w[4 * v + w] = a[w];
+  }
+  if (TAIL && i + 8 > H) {
+    const int down = i + 8 - H;                                  // elements, 1 .. 7
+#pragma unroll
+    for (int bit = 4; bit >= 1; bit >>= 1) {
+      const bool on = (down & bit) != 0;
+      if (sizeof(T) == 2 && bit == 1) {
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+          const uint32_t up = w + 1 < kWords ? r.w[w + 1] : 0;
+          r.w[w] = on ? r.w[w] >> 16 | up << 16 : r.w[w];
+        }
+      } else {
+        const int step = sizeof(T) == 2 ? bit / 2 : bit;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+          const uint32_t up = w + step < kWords ? r.w[w + step] : 0;
+          r.w[w] = on ? up : r.w[w];
+        }
+      }
+    }
   }
   return r;
+}
+
+// Waits for a load here.  Placed ahead of a turn's stores: waiting behind them would be for them as well, as loads and stores are counted
+// together and the compiler cannot tell how many of these (lanes past the row have none) follow the load.
+template <typename T> __device__ __forceinline__ void raw_settle(Raw8<T>& r) {
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) asm volatile("" : "+v"(r.w[i]));
 }
 
 // Rounded to T, once.
@@ -56,9 +95,15 @@ template <typename T> __device__ __forceinline__ Raw8<T> raw_pack(const float (&
   return r;
 }
 
-template <typename T, bool TAIL> __device__ __forceinline__ void raw_store(T* row, int i, int H, const Raw8<T>& r) {
+template <typename T, bool TAIL, bool NT = false> __device__ __forceinline__ void raw_store(T* row, int i, int H, const Raw8<T>& r) {
   if (!TAIL || i + 8 <= H) {
-    __builtin_memcpy(row + i, &r, sizeof(r));
+    u32x4_any* dst = reinterpret_cast<u32x4_any*>(row + i);
+#pragma unroll
+    for (int v = 0; v < (int)sizeof(r) / 16; ++v) {
+      const u32x4_any a = {r.w[4 * v], r.w[4 * v + 1], r.w[4 * v + 2], r.w[4 * v + 3]};
+      if (NT) __builtin_nontemporal_store(a, dst + v);
+      else dst[v] = a;
+    }
   } else {
 #pragma unroll
     for (int x = 0; x < 7; ++x)
