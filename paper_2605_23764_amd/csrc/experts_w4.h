@@ -27,12 +27,12 @@ constexpr int w4_occupancy(int row_blocks, int blocks) { return row_blocks == 2 
 constexpr int w4_columns(int blocks, bool swiglu) { return swiglu ? 8 * blocks : 16 * blocks; }
 
 struct W4Params {
-  const __bf16* x;               // activations, rows of K
-  const int32_t* gather;         // row r of the experts' rows is row gather[r] of x; null: r
+  const __bf16* x;               // activations: rows of K (gather), or the experts' rows in tiles (w4_tile_at)
+  const int32_t* gather;         // row r of the experts' rows is row gather[r] of x; null: tiles
   const uint8_t* q;              // [E_local][K / 32][cols][16]
   const uint8_t* scale;          // [E_local][K / 32][cols]
   const int32_t* offsets;        // [E_local + 1]
-  void* out;                     // rows of N: bf16 (SwiGLU) or fp32
+  void* out;                     // bf16 in tiles (SwiGLU), or rows of N fp32
   int K, N, cols, n_items;       // N: output columns (cols = 2 N with the gate and up halves)
 };
 
@@ -42,6 +42,11 @@ __device__ __forceinline__ bf16x8 w4_bf16(uint32_t w, float scale) {
   const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+
+// Activations in tiles: up to 16 rows of an expert (n of them) as [K / 8][n][8], so that what the 64 lanes of a load want, eight k of 16 rows
+// from four blocks, lies in four runs of 256 bytes; in rows it lies in 32 pieces of 64 bytes, and the L1 takes a load line by line.
+// Tiles follow each other like the rows in them.  Element of (row r of the tile, k):
+__device__ __forceinline__ uint32_t w4_tile_at(int r, int k, int n) { return (uint32_t)(((k >> 3) * n + r) * 8 + (k & 7)); }
 
 // A buffer descriptor over `bytes` from p (the same in all lanes): what a lane asks for beyond is 0 and costs no memory access.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t w4_buffer(const void* p, uint32_t bytes) {
@@ -78,20 +83,25 @@ __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, con
   for (int b = 0; b < NB; ++b) request_w(b, 0);                  // ahead of the permutation's lookup
   // activations: rows past the expert's last one, and k past the wave's share, read zeros
   const __amdgpu_buffer_rsrc_t bx = w4_buffer(p.gather ? p.x : p.x + (size_t)(row0 + m0) * p.K, 0x7FFFFFFFu);
-  uint32_t xo[RT];
+  uint32_t xo[RT];                                               // byte of this lane's block in step 0
+  int n_tile[RT];
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const int m = r * 16 + l16;
+    n_tile[r] = min(max(n_rows - m0 - r * 16, 0), 16);
     xo[r] = kW4Beyond;
-    if (m0 + m < n_rows) xo[r] = (uint32_t)(p.gather ? p.gather[row0 + m0 + m] : m) * (uint32_t)(p.K * 2) + (uint32_t)(g0 + lq) * 64;
+    if (l16 < n_tile[r]) {
+      if (p.gather) xo[r] = (uint32_t)p.gather[row0 + m0 + r * 16 + l16] * (uint32_t)(p.K * 2) + (uint32_t)(g0 + lq) * 64;
+      else xo[r] = (uint32_t)(r * 16) * (uint32_t)(p.K * 2) + 2 * w4_tile_at(l16, (g0 + lq) * 32, n_tile[r]);
+    }
   }
   auto request_x = [&](int s) __attribute__((always_inline)) {
     const bool in = s * 4 + lq < n_groups;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const uint32_t o = in ? xo[r] + (uint32_t)s * 256 : kW4Beyond;
+      const uint32_t eight = p.gather ? 16 : n_tile[r] * 16;     // bytes from eight k to the next
+      const uint32_t o = in ? xo[r] + (uint32_t)s * 16 * eight : kW4Beyond;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[r][i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(bx, o + i * 16, 0, 0));
+      for (int i = 0; i < 4; ++i) x[r][i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(bx, o + i * eight, 0, 0));
     }
   };
   request_x(0);
@@ -131,19 +141,21 @@ __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, con
     // lane: row l16 of the block, columns 4 lq .. 4 lq + 3 of each 16
     const int m = m0 + wave * 16 + l16;
     if (m < n_rows) {
-      const size_t row = (size_t)(row0 + m) * p.N;
       if constexpr (SWIGLU) {
+        const int n = min(n_rows - m0 - wave * 16, 16);
+        __bf16* tile = static_cast<__bf16*>(p.out) + (size_t)(row0 + m0 + wave * 16) * p.N;
 #pragma unroll
         for (int b = 0; b < NB / 2; ++b) {
           float a[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) a[c] = t[b][c] * sigmoid_bf16_(t[b][c]) * t[b + NB / 2][c];
-          *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.out) + row + item * kCols + b * 16 + lq * 4) =
+          *reinterpret_cast<u32x2*>(tile + w4_tile_at(l16, item * kCols + b * 16 + lq * 4, n)) =
               u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
         }
       } else {
+        float* row = static_cast<float*>(p.out) + (size_t)(row0 + m) * p.N;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + row + item * kCols + b * 16 + lq * 4) = t[b];
+        for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4*>(row + item * kCols + b * 16 + lq * 4) = t[b];
       }
     }
   }
@@ -163,6 +175,19 @@ __global__ __launch_bounds__(kW4Waves* kWave, w4_occupancy(RT, NB)) void experts
   for (int m0 = 0; m0 < rows; m0 += RT * 16) {                   // no rows: the weights are not touched
     if (m0) __syncthreads();                                     // s_acc has been read
     w4_rows<RT, NB, SWIGLU>(p, p.q + blocks * 16, p.scale + blocks, item, row0, m0, rows, s_acc);
+  }
+}
+
+// Token rows into tiles: blockIdx.x an expert, blockIdx.y a share of its tiles' 16-byte pieces.
+__global__ __launch_bounds__(256) void tiles_w4_kernel(const __bf16* x, const int32_t* token_of, const int32_t* offsets, __bf16* tiles, int K) {
+  const int row0 = offsets[blockIdx.x], rows = offsets[blockIdx.x + 1] - row0;
+  for (int m0 = 0; m0 < rows; m0 += 16) {
+    const int n = min(rows - m0, 16);
+    __bf16* tile = tiles + (size_t)(row0 + m0) * K;
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < K / 8 * n; i += gridDim.y * 256) {
+      const int k8 = i / n, r = i - k8 * n;
+      reinterpret_cast<u32x4*>(tile)[i] = *reinterpret_cast<const u32x4*>(x + (size_t)token_of[row0 + m0 + r] * K + k8 * 8);
+    }
   }
 }
 

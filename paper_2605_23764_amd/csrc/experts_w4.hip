@@ -22,9 +22,9 @@ int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream) {
   p.K = l.K; p.N = l.N; p.cols = swiglu ? 2 * l.N : l.N;
   // 32 rows at a time where experts have more than 8 on average (T = 100, 10 of 24 experts, k = 3: 28 -> 24 us); otherwise 16, which
   // leaves room for more waves, and the few experts above read their weights again.  Items of four column blocks, whose activations
-  // are fetched half as often, as long as there are four of them per CU (32 tokens, H = 7168, I = 2048, 32 of 256 experts: 117 -> 97
-  // us; one token, H = 2048, I = 1408: 20.8 us with two blocks, 22.7 with four).
-  const bool rows32 = l.rows > 8, wide = (long)l.experts * (l.N / w4_columns(4, swiglu)) >= 1024;
+  // are fetched half as often, as long as there are two of them per CU (32 tokens, H = 7168, I = 2048, 32 of 256 experts: 117 -> 97
+  // us; 64 tokens, H = 2048, I = 1408, 16 experts: 47 -> 38; but one token there 20.8 -> 22.7).
+  const bool rows32 = l.rows > 8, wide = (long)l.experts * (l.N / w4_columns(4, swiglu)) >= 512;
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto with_blocks = [&](auto rt, auto nb) {
     if (swiglu) launch<rt.value, nb.value, true>(p, l.E_local, s);
@@ -36,6 +36,12 @@ int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream) {
   };
   if (rows32) with_rows(std::integral_constant<int, 2>{});
   else with_rows(std::integral_constant<int, 1>{});
+  return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_LAUNCH;
+}
+
+int launch_tiles_w4(const void* x, const int32_t* token_of, const int32_t* offsets, void* tiles, int E_local, int K, void* stream) {
+  hipLaunchKernelGGL(tiles_w4_kernel, dim3(E_local, 32), dim3(256), 0, static_cast<hipStream_t>(stream), static_cast<const __bf16*>(x),
+                     token_of, offsets, static_cast<__bf16*>(tiles), K);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_LAUNCH;
 }
 

@@ -6,7 +6,7 @@ namespace moe {
 
 struct W4Launch {
   const void* x;
-  const int32_t* gather;         // null: rows of x in expert order
+  const int32_t* gather;         // token of each row; null: x holds the rows in tiles
   const void *q, *scale;
   const int32_t* offsets;
   void* out;
@@ -15,8 +15,12 @@ struct W4Launch {
   int rows;                      // of an expert, on average
 };
 
-// swiglu: N bf16 columns from N gate and N up columns; otherwise N fp32 columns.  Returns a MoeStatus, as the next.
+// swiglu: N bf16 columns from N gate and N up columns, in tiles; otherwise rows of N fp32.  Returns a MoeStatus, as the next two.
 __attribute__((visibility("hidden"))) int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream);
+
+// Token rows of K in the tiles that the products read fastest.
+__attribute__((visibility("hidden"))) int launch_tiles_w4(const void* x, const int32_t* token_of, const int32_t* offsets, void* tiles, int E_local,
+                                                          int K, void* stream);
 
 // Combine of fp32 rows into bf16 [T,H].
 __attribute__((visibility("hidden"))) int launch_combine_w4(const float* y, const int32_t* row_of, const float* topk_w, void* out, int T, int H,
