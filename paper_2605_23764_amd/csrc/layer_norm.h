@@ -72,8 +72,8 @@ __global__ __launch_bounds__(512) void norm_forward_kernel(NormForwardParams p) 
       q.x[i] = raw_zero<T>();
       if (FUSED) q.v[i] = raw_zero<T>();
       if (t < p.T && at < H) {
-        if (p.x) q.x[i] = raw_load<T, TAIL>(row_of<T>(p.x, (int)t, H), at, H);
-        if (FUSED) q.v[i] = raw_load<T, TAIL, NT>(row_of<T>(p.v, (int)t, H), at, H);
+        if (p.x) q.x[i] = raw_request<T, TAIL>(row_of<T>(p.x, (int)t, H), at, H);
+        if (FUSED) q.v[i] = raw_request<T, TAIL, NT>(row_of<T>(p.v, (int)t, H), at, H);
       }
     }
   };
@@ -88,6 +88,8 @@ __global__ __launch_bounds__(512) void norm_forward_kernel(NormForwardParams p) 
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int vec = i * G + g, at = vec * 8;
+      raw_trim<T, TAIL>(cur.x[i], at, H);
+      if (FUSED) raw_trim<T, TAIL>(cur.v[i], at, H);
       if (FUSED && t < p.T && at < H) {
         float v[8];
 #pragma unroll
@@ -162,9 +164,9 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackwardParams 
     r.rstd = live ? p.rstd[t] : 0.f;
     r.dy = r.x = r.dres = raw_zero<T>();
     if (live && at < H) {
-      r.dy = raw_load<T, TAIL, NT>(row_of<T>(p.dy, t, H), at, H);
-      r.x = raw_load<T, TAIL>(row_of<T>(p.x, t, H), at, H);
-      if (p.dres) r.dres = raw_load<T, TAIL, NT>(row_of<T>(p.dres, t, H), at, H);
+      r.dy = raw_request<T, TAIL, NT>(row_of<T>(p.dy, t, H), at, H);
+      r.x = raw_request<T, TAIL>(row_of<T>(p.x, t, H), at, H);
+      if (p.dres) r.dres = raw_request<T, TAIL, NT>(row_of<T>(p.dres, t, H), at, H);
     }
   };
   const int stride = gridDim.x * p.groups;
@@ -176,6 +178,9 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackwardParams 
     const int t = (int)min(t0 + rg, (long)p.T);
     Row next;
     load(next, (int)min(t0 + rg + stride, (long)p.T));
+    raw_trim<T, TAIL>(cur.dy, at, H);
+    raw_trim<T, TAIL>(cur.x, at, H);
+    raw_trim<T, TAIL>(cur.dres, at, H);
     float dxh[8], xh[8], sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 8; ++x) {

@@ -28,12 +28,11 @@ template <typename T> __device__ __forceinline__ Raw8<T> raw_zero() {
 
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element's address
 
-// Elements i .. i + 7 of a row of H; those past the end are zero.  A short last vector is the row's last eight elements moved down, one
-// load like the others' (in rows of fewer than eight, element by element).  NT: non-temporal, for what is read once and larger than the
-// caches.
-template <typename T, bool TAIL, bool NT = false> __device__ __forceinline__ Raw8<T> raw_load(const T* row, int i, int H) {
+// Elements i .. i + 7 of a row of H; those past the end are zero.  A short last vector is the row's last eight elements moved down: one
+// load like the others' (in rows of fewer than eight, element by element).  The load alone, whose result nothing waits for yet, and the
+// rest of it.  NT: non-temporal, for what is read once and larger than the caches.
+template <typename T, bool TAIL, bool NT = false> __device__ __forceinline__ Raw8<T> raw_request(const T* row, int i, int H) {
   Raw8<T> r;
-  constexpr int kWords = sizeof(r) / 4;
   if (TAIL && H < 8) {
     r = raw_zero<T>();
 #pragma unroll
@@ -46,32 +45,39 @@ template <typename T, bool TAIL, bool NT = false> __device__ __forceinline__ Raw
   }
   const u32x4_any* src = reinterpret_cast<const u32x4_any*>(row + (TAIL ? min(i, H - 8) : i));
 #pragma unroll
-  for (int v = 0; v < kWords / 4; ++v) {
+  for (int v = 0; v < (int)sizeof(r) / 16; ++v) {
     const u32x4_any a = NT ? __builtin_nontemporal_load(src + v) : src[v];
 #pragma unroll
     for (int w = 0; w < 4; ++w) r.w[4 * v + w] = a[w];
   }
-  if (TAIL && i + 8 > H) {
-    const int down = i + 8 - H;                                  // elements, 1 .. 7
+  return r;
+}
+template <typename T, bool TAIL> __device__ __forceinline__ void raw_trim(Raw8<T>& r, int i, int H) {
+  constexpr int kWords = sizeof(r) / 4;
+  if (!TAIL || H < 8) return;
+  const int down = max(i + 8 - H, 0);                            // elements, 0 .. 7 in lanes with a part of the row
 #pragma unroll
-    for (int bit = 4; bit >= 1; bit >>= 1) {
-      const bool on = (down & bit) != 0;
-      if (sizeof(T) == 2 && bit == 1) {
+  for (int bit = 4; bit >= 1; bit >>= 1) {
+    const bool on = (down & bit) != 0;
+    if (sizeof(T) == 2 && bit == 1) {
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-          const uint32_t up = w + 1 < kWords ? r.w[w + 1] : 0;
-          r.w[w] = on ? r.w[w] >> 16 | up << 16 : r.w[w];
-        }
-      } else {
-        const int step = sizeof(T) == 2 ? bit / 2 : bit;
+      for (int w = 0; w < kWords; ++w) {
+        const uint32_t up = w + 1 < kWords ? r.w[w + 1] : 0;
+        r.w[w] = on ? r.w[w] >> 16 | up << 16 : r.w[w];
+      }
+    } else {
+      const int step = sizeof(T) == 2 ? bit / 2 : bit;
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-          const uint32_t up = w + step < kWords ? r.w[w + step] : 0;
-          r.w[w] = on ? up : r.w[w];
-        }
+      for (int w = 0; w < kWords; ++w) {
+        const uint32_t up = w + step < kWords ? r.w[w + step] : 0;
+        r.w[w] = on ? up : r.w[w];
       }
     }
   }
+}
+template <typename T, bool TAIL, bool NT = false> __device__ __forceinline__ Raw8<T> raw_load(const T* row, int i, int H) {
+  Raw8<T> r = raw_request<T, TAIL, NT>(row, i, H);
+  raw_trim<T, TAIL>(r, i, H);
   return r;
 }
 
