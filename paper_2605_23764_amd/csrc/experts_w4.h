@@ -15,7 +15,8 @@
 // Products are exact in fp32 (bf16 x 2 bits), sums fp32.  GEMM-1's results are rounded to bf16 (they are an MFMA's operand next), GEMM-2's
 // stay fp32 until Combine has added them up, which rounds the layer's output once: 8 bytes of traffic per value of few rows.
 #pragma once
-#include "common.h"
+#include "experts_w4_launch.h"
+#include "route_select.h"
 
 namespace moe {
 
@@ -34,7 +35,12 @@ struct W4Params {
   const int32_t* offsets;        // [E_local + 1]
   void* out;                     // bf16 in tiles (SwiGLU), or rows of N fp32
   int K, N, cols, n_items;       // N: output columns (cols = 2 N with the gate and up halves)
+  RouteParams route;             // up to kW4RoutedT tokens: see experts_w4_kernel
 };
+
+// Rows of an expert, for the routed form: where each comes from and goes to.
+constexpr int kW4RoutedT = kW4MaxRoutedT;
+struct W4Rows { int32_t in[kW4RoutedT], out[kW4RoutedT]; };
 
 __device__ __forceinline__ bf16x8 w4_bf16(uint32_t w, float scale) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -56,9 +62,9 @@ constexpr uint32_t kW4Beyond = 0x80000000u;   // an offset past every buffer her
 constexpr int kW4Nt = 2;                      // non-temporal: a block is read once
 
 // Rows row0 + m0 .. (up to 16 RT) of an expert with n_rows rows, times the NB column blocks of an item.
-template <int RT, int NB, bool SWIGLU>
+template <int RT, int NB, bool SWIGLU, bool ROUTED>
 __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, const uint8_t* scale, int item, int row0, int m0, int n_rows,
-                                        float* s_acc) {
+                                        const W4Rows* s_rows, float* s_acc) {
   constexpr int kCols = w4_columns(NB, SWIGLU);
   const int lane = lane_id(), l16 = lane & 15, lq = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -82,7 +88,8 @@ __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, con
 #pragma unroll
   for (int b = 0; b < NB; ++b) request_w(b, 0);                  // ahead of the permutation's lookup
   // activations: rows past the expert's last one, and k past the wave's share, read zeros
-  const __amdgpu_buffer_rsrc_t bx = w4_buffer(p.gather ? p.x : p.x + (size_t)(row0 + m0) * p.K, 0x7FFFFFFFu);
+  const bool by_row = ROUTED || p.gather;
+  const __amdgpu_buffer_rsrc_t bx = w4_buffer(by_row ? p.x : p.x + (size_t)(row0 + m0) * p.K, 0x7FFFFFFFu);
   uint32_t xo[RT];                                               // byte of this lane's block in step 0
   int n_tile[RT];
 #pragma unroll
@@ -90,7 +97,8 @@ __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, con
     n_tile[r] = min(max(n_rows - m0 - r * 16, 0), 16);
     xo[r] = kW4Beyond;
     if (l16 < n_tile[r]) {
-      if (p.gather) xo[r] = (uint32_t)p.gather[row0 + m0 + r * 16 + l16] * (uint32_t)(p.K * 2) + (uint32_t)(g0 + lq) * 64;
+      const int m = m0 + r * 16 + l16;
+      if (by_row) xo[r] = (uint32_t)(ROUTED ? s_rows->in[m] : p.gather[row0 + m]) * (uint32_t)(p.K * 2) + (uint32_t)(g0 + lq) * 64;
       else xo[r] = (uint32_t)(r * 16) * (uint32_t)(p.K * 2) + 2 * w4_tile_at(l16, (g0 + lq) * 32, n_tile[r]);
     }
   }
@@ -98,7 +106,7 @@ __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, con
     const bool in = s * 4 + lq < n_groups;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      const uint32_t eight = p.gather ? 16 : n_tile[r] * 16;     // bytes from eight k to the next
+      const uint32_t eight = by_row ? 16 : n_tile[r] * 16;      // bytes from eight k to the next
       const uint32_t o = in ? xo[r] + (uint32_t)s * 16 * eight : kW4Beyond;
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[r][i] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(bx, o + i * eight, 0, 0));
@@ -141,19 +149,20 @@ __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, con
     // lane: row l16 of the block, columns 4 lq .. 4 lq + 3 of each 16
     const int m = m0 + wave * 16 + l16;
     if (m < n_rows) {
+      const size_t to = (size_t)(ROUTED ? s_rows->out[m] : row0 + m) * p.N;
       if constexpr (SWIGLU) {
         const int n = min(n_rows - m0 - wave * 16, 16);
-        __bf16* tile = static_cast<__bf16*>(p.out) + (size_t)(row0 + m0 + wave * 16) * p.N;
+        __bf16* tile = static_cast<__bf16*>(p.out) + (ROUTED ? to : to - (size_t)l16 * p.N);
 #pragma unroll
         for (int b = 0; b < NB / 2; ++b) {
           float a[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) a[c] = t[b][c] * sigmoid_bf16_(t[b][c]) * t[b + NB / 2][c];
-          *reinterpret_cast<u32x2*>(tile + w4_tile_at(l16, item * kCols + b * 16 + lq * 4, n)) =
-              u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
+          const int c = item * kCols + b * 16 + lq * 4;
+          *reinterpret_cast<u32x2*>(tile + (ROUTED ? c : w4_tile_at(l16, c, n))) = u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])};
         }
       } else {
-        float* row = static_cast<float*>(p.out) + (size_t)(row0 + m) * p.N;
+        float* row = static_cast<float*>(p.out) + to;
 #pragma unroll
         for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4*>(row + item * kCols + b * 16 + lq * 4) = t[b];
       }
@@ -161,20 +170,113 @@ __device__ __forceinline__ void w4_rows(const W4Params& p, const uint8_t* q, con
   }
 }
 
+// The routed form, for up to kW4RoutedT tokens: no routing launch ahead.  Every workgroup of GEMM-1 finds its expert's tokens itself, one
+// more workgroup routes all tokens for what follows, and the row of (token, slot) is token * k + slot, which nobody has to add up.
+//
+// GEMM-1: the expert's slot in a token's selection is the number of experts ahead of it: larger logit, or equal and lower id (the router's
+// order); a slot if that is less than k.  Returns the number of rows.
+__device__ __forceinline__ int w4_select(const RouteParams& p, int e, W4Rows* s_rows, int32_t* s_slot) {
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), id = p.expert_base + e;
+  constexpr int kTokens = kW4RoutedT / kW4Waves, kPieces = kMaxE / kWave;
+  float mine[kTokens], other[kTokens][kPieces];
+#pragma unroll
+  for (int q = 0; q < kTokens; ++q) {                            // all requested together
+    if (wave + q * kW4Waves >= p.T) break;
+    const float* row = p.logits + (size_t)(wave + q * kW4Waves) * p.E;
+    mine[q] = row[id];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (i * kWave < p.E) other[q][i] = row[min(i * kWave + lane, p.E - 1)];
+  }
+#pragma unroll
+  for (int q = 0; q < kTokens; ++q) {
+    if (wave + q * kW4Waves >= p.T) break;
+    const uint32_t key = float_order_key(mine[q]);
+    int ahead = 0;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      if (i * kWave < p.E) {
+        const int e2 = i * kWave + lane;
+        const uint32_t key2 = float_order_key(other[q][i]);
+        ahead += __popcll(__ballot(e2 < p.E && (key2 > key || (key2 == key && e2 < id))));
+      }
+    if (lane == 0) s_slot[wave + q * kW4Waves] = ahead < p.k ? ahead : -1;
+  }
+  __syncthreads();
+  const int slot = lane < p.T ? s_slot[lane] : -1;
+  const uint64_t members = __ballot(slot >= 0);
+  if (wave == 0 && slot >= 0) {
+    const int m = __popcll(members & ((1ull << lane) - 1));
+    s_rows->in[m] = lane;
+    s_rows->out[m] = lane * p.k + slot;
+  }
+  __syncthreads();
+  return __popcll(members);
+}
+// GEMM-2: from the selections that GEMM-1's launch has left.
+__device__ __forceinline__ int w4_selected(const RouteParams& p, int e, W4Rows* s_rows) {
+  const int lane = lane_id(), id = p.expert_base + e;
+  int slot = -1;
+  if (lane < p.T)
+    for (int j = 0; j < p.k; ++j)
+      if (p.topk_idx[lane * p.k + j] == id) slot = j;
+  const uint64_t members = __ballot(slot >= 0);
+  if (threadIdx.x < kWave && slot >= 0) {
+    const int m = __popcll(members & ((1ull << lane) - 1));
+    s_rows->in[m] = s_rows->out[m] = lane * p.k + slot;
+  }
+  __syncthreads();
+  return __popcll(members);
+}
+// topk_idx, topk_w and row_of of all tokens by one workgroup.
+__device__ __forceinline__ void w4_route(const RouteParams& p, int32_t* s_idx, float* s_val) {
+  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  s_idx += wave * kRouteTokensPerWave * kMaxK;
+  s_val += wave * kRouteTokensPerWave * kMaxK;
+  for (int t0 = wave * kRouteTokensPerWave; t0 < p.T; t0 += kW4Waves * kRouteTokensPerWave) {
+    with_route_keys(p.E, [&](auto kp) __attribute__((always_inline)) {
+      uint32_t key[decltype(kp)::value];
+      route_load(p, t0, lane, key);
+      route_select(p, t0, lane, key, s_idx, s_val);
+    });
+    const int r = lane >> 4, j = lane & 15, t = t0 + r;
+    if (t < p.T && j < p.k) {
+      const int local = s_idx[r * kMaxK + j] - p.expert_base;
+      p.row_of[t * p.k + j] = local >= 0 && local < p.E_local ? t * p.k + j : -1;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");        // read before the next tokens' selection is filed
+  }
+}
+
 // An item per workgroup.  The dispatcher deals consecutive workgroups to the eight dies in turn; consecutive items, whose blocks and above
 // all scales share lines, go to one die instead, eight at a time.
-template <int RT, int NB, bool SWIGLU>
+template <int RT, int NB, bool SWIGLU, bool ROUTED>
 __global__ __launch_bounds__(kW4Waves* kWave, w4_occupancy(RT, NB)) void experts_w4_kernel(W4Params p) {
+  constexpr int kRouting = ROUTED && SWIGLU;                     // workgroup 0 routes
   __shared__ __align__(16) float s_acc[kW4Waves * RT * NB * kWave * 4];
-  int id = blockIdx.x;
-  if ((id | 63) < (int)gridDim.x) id = (id & ~63) | (id & 7) << 3 | (id >> 3 & 7);
+  __shared__ W4Rows s_rows[1];                                   // the routed form alone
+  static_assert(!kRouting || sizeof(s_acc) >= 2 * kW4Waves * kRouteTokensPerWave * kMaxK * 4, "the selection's words");
+  int id = (int)blockIdx.x - kRouting;
+  if (kRouting && id < 0) {
+    w4_route(p.route, reinterpret_cast<int32_t*>(s_acc), s_acc + kW4Waves * kRouteTokensPerWave * kMaxK);
+    return;
+  }
+  if ((id | 63) < (int)gridDim.x - kRouting) id = (id & ~63) | (id & 7) << 3 | (id >> 3 & 7);
   const int e = id / p.n_items, item = id - e * p.n_items;
-  const int row0 = p.offsets[e], rows = p.offsets[e + 1] - row0;
+  int row0 = 0, rows;
+  if constexpr (!ROUTED) {
+    row0 = p.offsets[e];
+    rows = p.offsets[e + 1] - row0;
+  } else if constexpr (SWIGLU) {
+    rows = w4_select(p.route, e, s_rows, reinterpret_cast<int32_t*>(s_acc));
+  } else {
+    rows = w4_selected(p.route, e, s_rows);
+  }
   const size_t blocks = (size_t)e * (p.K / 32) * p.cols;
 #pragma unroll 1
   for (int m0 = 0; m0 < rows; m0 += RT * 16) {                   // no rows: the weights are not touched
     if (m0) __syncthreads();                                     // s_acc has been read
-    w4_rows<RT, NB, SWIGLU>(p, p.q + blocks * 16, p.scale + blocks, item, row0, m0, rows, s_acc);
+    w4_rows<RT, NB, SWIGLU, ROUTED>(p, p.q + blocks * 16, p.scale + blocks, item, row0, m0, rows, s_rows, s_acc);
   }
 }
 

@@ -9,9 +9,10 @@ using namespace moe;
 
 namespace moe {
 
-template <int RT, int NB, bool SWIGLU> static void launch(W4Params p, int E_local, hipStream_t s) {
+template <int RT, int NB, bool SWIGLU, bool ROUTED> static void launch(W4Params p, int E_local, hipStream_t s) {
   p.n_items = p.N / w4_columns(NB, SWIGLU);
-  hipLaunchKernelGGL((experts_w4_kernel<RT, NB, SWIGLU>), dim3((unsigned)E_local * (unsigned)p.n_items), dim3(kW4Waves * kWave), 0, s, p);
+  const unsigned grid = (unsigned)E_local * (unsigned)p.n_items + (ROUTED && SWIGLU ? 1 : 0);
+  hipLaunchKernelGGL((experts_w4_kernel<RT, NB, SWIGLU, ROUTED>), dim3(grid), dim3(kW4Waves * kWave), 0, s, p);
 }
 
 int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream) {
@@ -24,18 +25,25 @@ int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream) {
   // leaves room for more waves, and the few experts above read their weights again.  Items of four column blocks, whose activations
   // are fetched half as often, as long as there are two of them per CU (32 tokens, H = 7168, I = 2048, 32 of 256 experts: 117 -> 97
   // us; 64 tokens, H = 2048, I = 1408, 16 experts: 47 -> 38; but one token there 20.8 -> 22.7).
-  const bool rows32 = l.rows > 8, wide = (long)l.experts * (l.N / w4_columns(4, swiglu)) >= 512;
+  const bool rows32 = l.rows > kW4FewRows, wide = (long)l.experts * (l.N / w4_columns(4, swiglu)) >= 512;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto with_blocks = [&](auto rt, auto nb) {
-    if (swiglu) launch<rt.value, nb.value, true>(p, l.E_local, s);
-    else launch<rt.value, nb.value, false>(p, l.E_local, s);
+  auto with_blocks = [&](auto rt, auto nb, auto routed) {
+    if (swiglu) launch<rt.value, nb.value, true, routed.value>(p, l.E_local, s);
+    else launch<rt.value, nb.value, false, routed.value>(p, l.E_local, s);
   };
-  auto with_rows = [&](auto rt) {
-    if (wide) with_blocks(rt, std::integral_constant<int, 4>{});
-    else with_blocks(rt, std::integral_constant<int, 2>{});
+  auto with_rows = [&](auto rt, auto routed) {
+    if (wide) with_blocks(rt, std::integral_constant<int, 4>{}, routed);
+    else with_blocks(rt, std::integral_constant<int, 2>{}, routed);
   };
-  if (rows32) with_rows(std::integral_constant<int, 2>{});
-  else with_rows(std::integral_constant<int, 1>{});
+  if (l.logits) {
+    p.route.logits = l.logits; p.route.topk_idx = l.topk_idx; p.route.topk_w = l.topk_w; p.route.row_of = l.row_of;
+    p.route.T = l.T; p.route.E = l.E; p.route.E_local = l.E_local; p.route.expert_base = l.expert_base; p.route.k = l.k;
+    with_rows(std::integral_constant<int, 1>{}, std::true_type{});
+  } else if (rows32) {
+    with_rows(std::integral_constant<int, 2>{}, std::false_type{});
+  } else {
+    with_rows(std::integral_constant<int, 1>{}, std::false_type{});
+  }
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_LAUNCH;
 }
 

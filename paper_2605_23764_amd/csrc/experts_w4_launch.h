@@ -11,9 +11,17 @@ struct W4Launch {
   const int32_t* offsets;
   void* out;
   int E_local, K, N;
-  int experts;                   // experts with rows, at most
+  int experts;                   // experts with rows, expected
   int rows;                      // of an expert, on average
+  // The routed form (T up to kW4MaxRoutedT, rows up to kW4FewRows, k <= E_local): no routing launch has run, `gather` and `offsets`
+  // are null; GEMM-1 leaves topk_idx, topk_w and row_of, a row is token * k + slot, activations between the two are rows, not tiles.
+  const float* logits;           // null: not routed
+  int32_t* topk_idx;
+  float* topk_w;
+  int32_t* row_of;
+  int T, E, expert_base, k;
 };
+constexpr int kW4MaxRoutedT = 16, kW4FewRows = 8;
 
 // swiglu: N bf16 columns from N gate and N up columns, in tiles; otherwise rows of N fp32.  Returns a MoeStatus, as the next two.
 __attribute__((visibility("hidden"))) int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream);

@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 
 #include "backward.h"
@@ -962,22 +963,40 @@ int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_lo
   for (const void* q : ptrs)
     if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
   if ((double)c.s.H * c.s.I >= 2147483648.0) return MOE_ERR_UNSUPPORTED_SHAPE;   // an expert's blocks: 31-bit offsets
-  if ((st = run_route(c, d_logits, false)) != MOE_OK) return st;
   // GEMM-2's rows in fp32, [R_max,H], over what the bf16 layer uses for Xp and half of A and Yp behind it; A follows.  (The three are
   // 2 R_max (2 H + I) bytes; rows of H fp32 are multiples of 256 bytes.)
   float* y = reinterpret_cast<float*>(c.ws + c.L.Xp);
   void* a = c.ws + c.L.Xp + (size_t)r_max(c.s) * c.s.H * 4;
-  const int experts = (int)std::min((long)c.s.E_local, (long)c.s.T * c.s.k), rows = (int)((long)c.s.T * c.s.k / c.s.E);
-  W4Launch g1 = {d_x, c.sv.token_of, d_q_gate_up, d_s_gate_up, c.sv.offsets, a, c.s.E_local, c.s.H, c.s.I, experts, rows};
-  // Token rows are read through the permutation, except where experts have many of them, whose fetches then bound GEMM-1 (H = 2048,
-  // I = 1408, 16 experts, k = 4: T = 128, 32 rows on average, 61 -> 56 us, T = 256 89 -> 76, but T = 64 38 -> 39), and beyond its 31-bit
-  // offsets: put into tiles first, where y will be.
-  if (rows > 16 || (size_t)c.s.T * c.s.H * 2 >= ((size_t)1 << 31)) {
-    if ((st = launch_tiles_w4(d_x, c.sv.token_of, c.sv.offsets, y, c.s.E_local, c.s.H, stream)) != MOE_OK) return st;
-    g1.x = y;
-    g1.gather = nullptr;
+  const int rows = (int)((long)c.s.T * c.s.k / c.s.E);
+  const int experts = (int)std::min((double)c.s.E_local, ceil((double)c.s.T * c.s.k * c.s.E_local / c.s.E));
+  W4Launch g1 = {}, g2 = {};
+  g1.x = d_x; g1.q = d_q_gate_up; g1.scale = d_s_gate_up; g1.out = a; g1.K = c.s.H; g1.N = c.s.I;
+  g2.x = a; g2.q = d_q_down; g2.scale = d_s_down; g2.out = y; g2.K = c.s.I; g2.N = c.s.H;
+  for (W4Launch* g : {&g1, &g2}) {
+    g->E_local = c.s.E_local; g->experts = experts; g->rows = rows;
+    g->T = c.s.T; g->E = c.s.E; g->expert_base = c.s.expert_base; g->k = c.s.k;
   }
-  const W4Launch g2 = {a, nullptr, d_q_down, d_s_down, c.sv.offsets, y, c.s.E_local, c.s.I, c.s.H, experts, rows};
+  // Few tokens: without a routing launch, which costs more than every workgroup's own look at the logits as long as these are few: a load
+  // each for 64 logits of a token (H = 2048, I = 1408, 16 experts, k = 4: T = 1 23.4 -> 18.9 us, T = 16 29.2 -> 25.4; H = 7168, I = 2048, 32 of
+  // 256 experts, k = 8: T = 1 29.1 -> 27.3, T = 4 44.4 -> 42.0, but T = 8 57.5 -> 58.2).  A caller's MoeSaved wants everything that launch
+  // leaves.
+  if (!saved && (long)c.s.T * ceil_div(c.s.E, kWave) <= kW4MaxRoutedT && rows <= kW4FewRows && c.s.k <= c.s.E_local) {
+    for (W4Launch* g : {&g1, &g2}) {
+      g->logits = d_logits; g->topk_idx = c.sv.topk_idx; g->topk_w = c.sv.topk_w; g->row_of = c.sv.row_of;
+    }
+  } else {
+    if ((st = run_route(c, d_logits, false)) != MOE_OK) return st;
+    g1.offsets = g2.offsets = c.sv.offsets;
+    g1.gather = c.sv.token_of;
+    // Token rows are read through the permutation, except where experts have many of them, whose fetches then bound GEMM-1 (H = 2048,
+    // I = 1408, 16 experts, k = 4: T = 128, 32 rows on average, 61 -> 56 us, T = 256 89 -> 76, but T = 64 38 -> 39), and beyond its 31-bit
+    // offsets: put into tiles first, where y will be.
+    if (rows > 16 || (size_t)c.s.T * c.s.H * 2 >= ((size_t)1 << 31)) {
+      if ((st = launch_tiles_w4(d_x, c.sv.token_of, c.sv.offsets, y, c.s.E_local, c.s.H, stream)) != MOE_OK) return st;
+      g1.x = y;
+      g1.gather = nullptr;
+    }
+  }
   if ((st = launch_experts_w4(g1, true, stream)) != MOE_OK) return st;
   if ((st = launch_experts_w4(g2, false, stream)) != MOE_OK) return st;
   return launch_combine_w4(y, c.sv.row_of, c.sv.topk_w, d_out, c.s.T, c.s.H, c.s.k, stream);

@@ -118,6 +118,26 @@ def test_every_code_and_scale():
             np.testing.assert_array_equal(f64(out), 96.0 * values * 2.0 ** (s - 127), err_msg=str(s))
 
 
+@pytest.mark.parametrize("T,E,El,base,k", [(1, 256, 32, 0, 8), (4, 250, 100, 150, 16), (5, 130, 130, 0, 3), (16, 64, 64, 0, 2), (16, 5, 5, 0, 1),
+                                           (8, 100, 60, 17, 9), (17, 64, 20, 3, 4)])
+def test_few_tokens_route_alike(T, E, El, base, k):
+    """Few tokens take no routing launch unless a MoeSaved asks for its results: the same bits both ways, ties, zeros of both signs,
+    infinities and NaN among the logits included."""
+    cfg = MoeConfig("w4", T, 128, 64, E, El, base, k, "bf16", 70 + T)
+    inp = make_inputs(cfg)
+    r = np.random.default_rng(E)
+    lg = np.round(inp["logits"] * 2) / 2                             # many ties
+    lg[r.random(lg.shape) < 0.1] = -0.0
+    if k < E // 2:
+        lg[r.random(lg.shape) < 0.05] = -np.inf
+        lg[r.random(lg.shape) < 0.05] = np.nan
+    inp["logits"] = lg
+    dev = _device(inp)
+    shape, out = _run(cfg, dev)
+    _, want = _run(cfg, dev, moe.alloc_saved(shape))
+    assert torch.equal(out, want) and not torch.isnan(out.float()).any()
+
+
 def test_tokens_without_a_local_expert():
     cfg = MoeConfig("w4", 40, 64, 64, 16, 2, 14, 1, "bf16", 3)
     inp = make_inputs(cfg)
