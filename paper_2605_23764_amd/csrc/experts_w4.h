@@ -12,6 +12,9 @@
 //     contiguous bytes per lane), so that neither side is ever shuffled.
 //   * The waves of a workgroup split K, so that an item is narrow (16 gate + 16 up columns, or 32 columns) and even one token's few
 //     experts give several items per CU; their sums meet in LDS, in wave order.
+// Bound by that read: 32 tokens, H = 7168, I = 2048, 32 of 256 experts, k = 8 (about 20 with rows, 482 MB): GEMM-1 57 us, GEMM-2 30, 5.5 TB/s
+// where a loop that only loads pieces of 256 bytes reaches 6.2; with few weights (one token, H = 2048, I = 1408: 18 MB, 7.4 + 5.7 us) by
+// the latency of a workgroup's start, four steps and a join; with many rows by the activations' fetches.
 // Products are exact in fp32 (bf16 x 2 bits), sums fp32.  GEMM-1's results are rounded to bf16 (they are an MFMA's operand next), GEMM-2's
 // stay fp32 until Combine has added them up, which rounds the layer's output once: 8 bytes of traffic per value of few rows.
 #pragma once
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(256) void tiles_w4_kernel(const __bf16* x, const in
   }
 }
 
-// out[t,:] = sum over the local slots j of topk_w[t,j] * y[row_of[t,j],:], in slot order: a lane per eight columns of a token.
+// Combine (4.7 us for 32 tokens of H = 7168, latency): out[t,:] = sum over the local slots j of topk_w[t,j] * y[row_of[t,j],:], in slot order: a lane per eight columns of a token.
 __global__ __launch_bounds__(256) void combine_w4_kernel(const float* y, const int32_t* row_of, const float* topk_w, __bf16* out, int T, int H,
                                                          int k) {
   const int per = H / 8;
