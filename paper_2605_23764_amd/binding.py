@@ -338,30 +338,34 @@ def moe_probe_copy(src, dst, nbytes, stream=None) -> None:
 
 # ---- the operators around the layer: T, H and the storage type are read off the tensors, whose shapes and types are checked ----
 
-def _arg(t: Optional[torch.Tensor], shape, dtype, name: str):
-    """Device address of a tensor of this shape and type; None for None."""
-    if t is None:
-        return None
-    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError(f"{name}: expected a contiguous device tensor of shape {shape} and type {dtype}, got {tuple(t.shape)}, {t.dtype}, "
-                     f"{t.device}")
+def _args(shape, dtype, names: str, *tensors):
+    """Device addresses of tensors of this shape and type; None for None.  (One call per group: a launch is 3 us of the host's time, and each
+    tensor's checks a quarter of one.)"""
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+        elif t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
+            raise ValueError(f"{names.split()[len(out)]}: expected a contiguous device tensor of shape {tuple(shape)} and type {dtype}, got "
+                             f"{tuple(t.shape)}, {t.dtype}, {t.device}")
+    return out
+
+
+_STORAGE = {torch.bfloat16: MOE_BF16, torch.float32: MOE_F32}
 
 
 def _rows(t: torch.Tensor, name: str):
-    """(T, H, storage type, its MoeDtype) of a [T, H] tensor."""
-    if t.dim() != 2 or t.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"{name}: expected a [T, H] tensor in bfloat16 or float32, got {tuple(t.shape)}, {t.dtype}")
-    T, H = t.shape
-    return T, H, t.dtype, MOE_BF16 if t.dtype is torch.bfloat16 else MOE_F32
+    """(shape, storage type, its MoeDtype) of a [T, H] tensor."""
+    shape, dtype = t.shape, t.dtype
+    if len(shape) != 2 or dtype not in _STORAGE:
+        raise ValueError(f"{name}: expected a [T, H] tensor in bfloat16 or float32, got {tuple(shape)}, {dtype}")
+    return shape, dtype, _STORAGE[dtype]
 
 
 def _raw_stream(stream) -> int:
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-
-
-def _drop_rng(rng: Optional[torch.Tensor]):
-    return _arg(rng, (2,), torch.int64, "rng")
 
 
 def _size(name: str, *args) -> int:
@@ -386,63 +390,70 @@ def alloc_layer_norm_workspace(T: int, H: int, device="cuda") -> torch.Tensor:
 
 def moe_layer_norm_forward(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None) -> None:
     """y = layer norm of the rows of x [T, H]; gamma, beta [H] or None; mean, rstd [T] f32 (for the backward) or None."""
-    T, H, dt, code = _rows(x, "x")
-    f32 = torch.float32
-    _check(load_library().moe_layer_norm_forward(
-        T, H, code, _arg(x, (T, H), dt, "x"), _arg(gamma, (H,), dt, "gamma"), _arg(beta, (H,), dt, "beta"), eps,
-        _arg(y, (T, H), dt, "y"), _arg(mean, (T,), f32, "mean"), _arg(rstd, (T,), f32, "rstd"), _raw_stream(stream)),
-        "moe_layer_norm_forward")
+    shape, dt, code = _rows(x, "x")
+    T, H = shape
+    x, y = _args(shape, dt, "x y", x, y)
+    gamma, beta = _args((H,), dt, "gamma beta", gamma, beta)
+    mean, rstd = _args((T,), torch.float32, "mean rstd", mean, rstd)
+    _check(load_library().moe_layer_norm_forward(T, H, code, x, gamma, beta, eps, y, mean, rstd, _raw_stream(stream)),
+           "moe_layer_norm_forward")
 
 
 def moe_layer_norm_backward(dy, x, gamma, mean, rstd, dres, dx, dgamma, dbeta, workspace, stream=None) -> None:
     """dx = gradient of x, plus dres (the residual path's) if given; dgamma, dbeta [H] or None."""
-    T, H, dt, code = _rows(x, "x")
-    f32 = torch.float32
+    shape, dt, code = _rows(x, "x")
+    T, H = shape
+    dy, x, dres, dx = _args(shape, dt, "dy x dres dx", dy, x, dres, dx)
+    gamma, dgamma, dbeta = _args((H,), dt, "gamma dgamma dbeta", gamma, dgamma, dbeta)
+    mean, rstd = _args((T,), torch.float32, "mean rstd", mean, rstd)
     ws, wb = _workspace(workspace)
-    _check(load_library().moe_layer_norm_backward(
-        T, H, code, _arg(dy, (T, H), dt, "dy"), _arg(x, (T, H), dt, "x"), _arg(gamma, (H,), dt, "gamma"),
-        _arg(mean, (T,), f32, "mean"), _arg(rstd, (T,), f32, "rstd"), _arg(dres, (T, H), dt, "dres"), _arg(dx, (T, H), dt, "dx"),
-        _arg(dgamma, (H,), dt, "dgamma"), _arg(dbeta, (H,), dt, "dbeta"), ws, wb, _raw_stream(stream)), "moe_layer_norm_backward")
+    _check(load_library().moe_layer_norm_backward(T, H, code, dy, x, gamma, mean, rstd, dres, dx, dgamma, dbeta, ws, wb,
+                                                  _raw_stream(stream)), "moe_layer_norm_backward")
 
 
 def moe_dropout_add_forward(v, residual, p: float, rng, out, stream=None) -> None:
     """out = residual (or 0) + dropout(v); rng: device int64 {seed, offset}, None if p == 0."""
-    T, H, dt, code = _rows(v, "v")
-    _check(load_library().moe_dropout_add_forward(
-        T, H, code, _arg(v, (T, H), dt, "v"), _arg(residual, (T, H), dt, "residual"), p, _drop_rng(rng), _arg(out, (T, H), dt, "out"),
-        _raw_stream(stream)), "moe_dropout_add_forward")
+    shape, dt, code = _rows(v, "v")
+    T, H = shape
+    v, residual, out = _args(shape, dt, "v residual out", v, residual, out)
+    rng, = _args((2,), torch.int64, "rng", rng)
+    _check(load_library().moe_dropout_add_forward(T, H, code, v, residual, p, rng, out, _raw_stream(stream)), "moe_dropout_add_forward")
 
 
 def moe_dropout_add_backward(dout, p: float, rng, dv, stream=None) -> None:
     """dv = dropout's backward of dout, with the forward's p and rng contents."""
-    T, H, dt, code = _rows(dout, "dout")
-    _check(load_library().moe_dropout_add_backward(
-        T, H, code, _arg(dout, (T, H), dt, "dout"), p, _drop_rng(rng), _arg(dv, (T, H), dt, "dv"), _raw_stream(stream)),
-        "moe_dropout_add_backward")
+    shape, dt, code = _rows(dout, "dout")
+    T, H = shape
+    dout, dv = _args(shape, dt, "dout dv", dout, dv)
+    rng, = _args((2,), torch.int64, "rng", rng)
+    _check(load_library().moe_dropout_add_backward(T, H, code, dout, p, rng, dv, _raw_stream(stream)), "moe_dropout_add_backward")
 
 
 def moe_dropout_add_layer_norm_forward(v, residual, p: float, rng, gamma, beta, eps: float, z, y, mean=None, rstd=None,
                                        stream=None) -> None:
     """z = residual (or 0) + dropout(v), y = layer norm of z."""
-    T, H, dt, code = _rows(v, "v")
-    f32 = torch.float32
-    _check(load_library().moe_dropout_add_layer_norm_forward(
-        T, H, code, _arg(v, (T, H), dt, "v"), _arg(residual, (T, H), dt, "residual"), p, _drop_rng(rng), _arg(gamma, (H,), dt, "gamma"),
-        _arg(beta, (H,), dt, "beta"), eps, _arg(z, (T, H), dt, "z"), _arg(y, (T, H), dt, "y"), _arg(mean, (T,), f32, "mean"),
-        _arg(rstd, (T,), f32, "rstd"), _raw_stream(stream)), "moe_dropout_add_layer_norm_forward")
+    shape, dt, code = _rows(v, "v")
+    T, H = shape
+    v, residual, z, y = _args(shape, dt, "v residual z y", v, residual, z, y)
+    gamma, beta = _args((H,), dt, "gamma beta", gamma, beta)
+    mean, rstd = _args((T,), torch.float32, "mean rstd", mean, rstd)
+    rng, = _args((2,), torch.int64, "rng", rng)
+    _check(load_library().moe_dropout_add_layer_norm_forward(T, H, code, v, residual, p, rng, gamma, beta, eps, z, y, mean, rstd,
+                                                             _raw_stream(stream)), "moe_dropout_add_layer_norm_forward")
 
 
 def moe_dropout_add_layer_norm_backward(dy, z, gamma, mean, rstd, dres, p: float, rng, dz, dv, dgamma, dbeta, workspace,
                                         stream=None) -> None:
     """dz = dres (or 0) + layer norm's backward at z (the residual's gradient too), dv = dropout's backward of dz."""
-    T, H, dt, code = _rows(z, "z")
-    f32 = torch.float32
+    shape, dt, code = _rows(z, "z")
+    T, H = shape
+    dy, z, dres, dz, dv = _args(shape, dt, "dy z dres dz dv", dy, z, dres, dz, dv)
+    gamma, dgamma, dbeta = _args((H,), dt, "gamma dgamma dbeta", gamma, dgamma, dbeta)
+    mean, rstd = _args((T,), torch.float32, "mean rstd", mean, rstd)
+    rng, = _args((2,), torch.int64, "rng", rng)
     ws, wb = _workspace(workspace)
-    _check(load_library().moe_dropout_add_layer_norm_backward(
-        T, H, code, _arg(dy, (T, H), dt, "dy"), _arg(z, (T, H), dt, "z"), _arg(gamma, (H,), dt, "gamma"),
-        _arg(mean, (T,), f32, "mean"), _arg(rstd, (T,), f32, "rstd"), _arg(dres, (T, H), dt, "dres"), p, _drop_rng(rng),
-        _arg(dz, (T, H), dt, "dz"), _arg(dv, (T, H), dt, "dv"), _arg(dgamma, (H,), dt, "dgamma"), _arg(dbeta, (H,), dt, "dbeta"),
-        ws, wb, _raw_stream(stream)), "moe_dropout_add_layer_norm_backward")
+    _check(load_library().moe_dropout_add_layer_norm_backward(T, H, code, dy, z, gamma, mean, rstd, dres, p, rng, dz, dv, dgamma, dbeta,
+                                                              ws, wb, _raw_stream(stream)), "moe_dropout_add_layer_norm_backward")
 
 
 def moe_balance_workspace_bytes(T: int, E: int) -> int:
@@ -453,35 +464,40 @@ def alloc_balance_workspace(T: int, E: int, device="cuda") -> torch.Tensor:
     return torch.empty(moe_balance_workspace_bytes(T, E), dtype=torch.uint8, device=device)
 
 
-def _mask(mask: Optional[torch.Tensor], T: int):
-    return _arg(mask, (T,), torch.bool if mask is not None and mask.dtype is torch.bool else torch.uint8, "mask")
-
-
-def _router(logits, topk_idx):
+def _router(logits, topk_idx, mask):
+    """T, E, k and the mask's type (bool or uint8)."""
     if logits.dim() != 2 or topk_idx.dim() != 2:
         raise ValueError("expected logits [T, E] and topk_idx [T, k]")
-    return logits.shape[0], logits.shape[1], topk_idx.shape[1]
+    return *logits.shape, topk_idx.shape[1], torch.bool if mask is not None and mask.dtype is torch.bool else torch.uint8
 
 
 def moe_balance_forward(logits, topk_idx, mask, coef: float, counts, prob_sum, loss, workspace, stream=None) -> None:
     """counts [E + 1] i32 (the last: tokens that count), prob_sum [E] f32, loss [1] f32; mask [T] bool / uint8 or None."""
-    T, E, k = _router(logits, topk_idx)
+    T, E, k, mask_type = _router(logits, topk_idx, mask)
     f32, i32 = torch.float32, torch.int32
+    logits, = _args((T, E), f32, "logits", logits)
+    topk_idx, = _args((T, k), i32, "topk_idx", topk_idx)
+    mask, = _args((T,), mask_type, "mask", mask)
+    counts, = _args((E + 1,), i32, "counts", counts)
+    prob_sum, = _args((E,), f32, "prob_sum", prob_sum)
+    loss, = _args((1,), f32, "loss", loss)
     ws, wb = _workspace(workspace)
-    _check(load_library().moe_balance_forward(
-        T, E, k, _arg(logits, (T, E), f32, "logits"), _arg(topk_idx, (T, k), i32, "topk_idx"), _mask(mask, T), coef,
-        _arg(counts, (E + 1,), i32, "counts"), _arg(prob_sum, (E,), f32, "prob_sum"), _arg(loss, (1,), f32, "loss"), ws, wb,
-        _raw_stream(stream)), "moe_balance_forward")
+    _check(load_library().moe_balance_forward(T, E, k, logits, topk_idx, mask, coef, counts, prob_sum, loss, ws, wb, _raw_stream(stream)),
+           "moe_balance_forward")
 
 
 def moe_router_backward(logits, topk_idx, topk_w, dtopk_w, mask, coef: float, counts, dloss, dlogits, stream=None) -> None:
     """dlogits [T, E] from the routing weights' gradient (topk_w, dtopk_w or both None) and the balance loss's (counts or None)."""
-    T, E, k = _router(logits, topk_idx)
+    T, E, k, mask_type = _router(logits, topk_idx, mask)
     f32, i32 = torch.float32, torch.int32
-    _check(load_library().moe_router_backward(
-        T, E, k, _arg(logits, (T, E), f32, "logits"), _arg(topk_idx, (T, k), i32, "topk_idx"), _arg(topk_w, (T, k), f32, "topk_w"),
-        _arg(dtopk_w, (T, k), f32, "dtopk_w"), _mask(mask, T), coef, _arg(counts, (E + 1,), i32, "counts"),
-        _arg(dloss, (1,), f32, "dloss"), _arg(dlogits, (T, E), f32, "dlogits"), _raw_stream(stream)), "moe_router_backward")
+    logits, dlogits = _args((T, E), f32, "logits dlogits", logits, dlogits)
+    topk_idx, = _args((T, k), i32, "topk_idx", topk_idx)
+    topk_w, dtopk_w = _args((T, k), f32, "topk_w dtopk_w", topk_w, dtopk_w)
+    mask, = _args((T,), mask_type, "mask", mask)
+    counts, = _args((E + 1,), i32, "counts", counts)
+    dloss, = _args((1,), f32, "dloss", dloss)
+    _check(load_library().moe_router_backward(T, E, k, logits, topk_idx, topk_w, dtopk_w, mask, coef, counts, dloss, dlogits,
+                                              _raw_stream(stream)), "moe_router_backward")
 
 
 def alloc_w4(E_local: int, K: int, N: int, device="cuda"):
@@ -492,22 +508,27 @@ def alloc_w4(E_local: int, K: int, N: int, device="cuda"):
 
 def moe_quantize_w4(w, q, scale, stream=None) -> None:
     """4-bit blocks of w [E_local, K, N] (bfloat16 or float32)."""
-    if w.dim() != 3 or w.dtype not in (torch.bfloat16, torch.float32):
+    if w.dim() != 3 or w.dtype not in _STORAGE:
         raise ValueError(f"w: expected an [E_local, K, N] tensor in bfloat16 or float32, got {tuple(w.shape)}, {w.dtype}")
     E, K, N = w.shape
-    _check(load_library().moe_quantize_w4(
-        E, K, N, MOE_BF16 if w.dtype is torch.bfloat16 else MOE_F32, _arg(w, (E, K, N), w.dtype, "w"),
-        _arg(q, (E, K // 32, N, 16), torch.uint8, "q"), _arg(scale, (E, K // 32, N), torch.uint8, "scale"), _raw_stream(stream)),
-        "moe_quantize_w4")
+    code = _STORAGE[w.dtype]
+    w, = _args((E, K, N), w.dtype, "w", w)
+    q, = _args((E, K // 32, N, 16), torch.uint8, "q", q)
+    scale, = _args((E, K // 32, N), torch.uint8, "scale", scale)
+    _check(load_library().moe_quantize_w4(E, K, N, code, w, q, scale, _raw_stream(stream)), "moe_quantize_w4")
 
 
 def moe_ffn_forward_w4(shape, x, logits, q_gate_up, s_gate_up, q_down, s_down, out, saved: Optional[Saved], workspace,
                        stream=None) -> None:
-    T, H, I, El, bf16, u8 = shape.T, shape.H, shape.I, shape.E_local, torch.bfloat16, torch.uint8
+    T, H, I, El, u8 = shape.T, shape.H, shape.I, shape.E_local, torch.uint8
     sv = saved.c_struct() if saved is not None else None
+    x, out = _args((T, H), torch.bfloat16, "x out", x, out)
+    logits, = _args((T, shape.E), torch.float32, "logits", logits)
+    q_gate_up, = _args((El, H // 32, 2 * I, 16), u8, "q_gate_up", q_gate_up)
+    s_gate_up, = _args((El, H // 32, 2 * I), u8, "s_gate_up", s_gate_up)
+    q_down, = _args((El, I // 32, H, 16), u8, "q_down", q_down)
+    s_down, = _args((El, I // 32, H), u8, "s_down", s_down)
     ws, wb = _workspace(workspace)
-    _check(load_library().moe_ffn_forward_w4(
-        ctypes.addressof(shape), _arg(x, (T, H), bf16, "x"), _arg(logits, (T, shape.E), torch.float32, "logits"),
-        _arg(q_gate_up, (El, H // 32, 2 * I, 16), u8, "q_gate_up"), _arg(s_gate_up, (El, H // 32, 2 * I), u8, "s_gate_up"),
-        _arg(q_down, (El, I // 32, H, 16), u8, "q_down"), _arg(s_down, (El, I // 32, H), u8, "s_down"), _arg(out, (T, H), bf16, "out"),
-        ctypes.addressof(sv) if sv is not None else None, ws, wb, _raw_stream(stream)), "moe_ffn_forward_w4")
+    _check(load_library().moe_ffn_forward_w4(ctypes.addressof(shape), x, logits, q_gate_up, s_gate_up, q_down, s_down, out,
+                                             ctypes.addressof(sv) if sv is not None else None, ws, wb, _raw_stream(stream)),
+           "moe_ffn_forward_w4")

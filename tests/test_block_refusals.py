@@ -109,7 +109,7 @@ def test_quantize(lib, want, change):
 
 
 @pytest.mark.parametrize("want,change,shape", [
-    (SHAPE, {}, dict(H=96)), (SHAPE, {}, dict(E=300)), (INVALID, {}, dict(dtype=0)), (SMALL, dict(size=1000), {}),
+    (SHAPE, {}, dict(H=96)), (SHAPE, {}, dict(E=300)), (SHAPE, dict(size=1 << 40), dict(H=65536, I=32768)), (INVALID, {}, dict(dtype=0)), (SMALL, dict(size=1000), {}),
     *[(INVALID, {n: None}, {}) for n in ("x", "logits", "q1", "s1", "q2", "s2", "out", "ws")],
     *[(INVALID, {n: at(12, 8)}, {}) for n in ("x", "logits", "q1", "s1", "q2", "s2", "out", "ws")]])
 def test_forward_w4(lib, want, change, shape):

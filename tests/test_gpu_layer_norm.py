@@ -85,6 +85,23 @@ def test_many_rows(T, H, dtype):
     assert all(torch.equal(a, b) for a, b in zip((dx, dg, db), again))      # a fixed order of every sum
 
 
+@pytest.mark.parametrize("T,H", [(30000, 72), (5300, 520), (5200, 1001), (3000, 2048), (1601, 7168)])
+def test_forward_walks_rows(T, H):
+    """More rows than a launch has workgroups for: several turns in the forward too, alone and with dropout."""
+    print(f"walk T={T} H={H}", flush=True)
+    x, gamma, beta, _, _, v = _inputs(T, H, "bf16", H + T)
+    y, mean, rstd = _forward(x, gamma, beta)
+    want, m, s, e_y, e_m, e_s, _ = norm_bounds(f64(x), f64(gamma), f64(beta), EPS, "bf16")
+    close(y, want, e_y, "y")
+    close(mean, m, e_m, "mean")
+    close(rstd, s, e_s, "rstd")
+    rng, z, z2 = _rng(3, 4), torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    moe.moe_dropout_add_layer_norm_forward(v, x, 0.4, rng, gamma, beta, EPS, z, y, mean, rstd)
+    moe.moe_dropout_add_forward(v, x, 0.4, rng, z2)
+    y2, mean2, rstd2 = _forward(z2, gamma, beta)
+    assert torch.equal(z, z2) and torch.equal(y, y2) and torch.equal(mean, mean2) and torch.equal(rstd, rstd2)
+
+
 def test_gradient_against_differences():
     """Central differences of the oracle's forward, in 64 bits (they are good to 1e-8), against the kernel's fp32 gradient."""
     T, H = 3, 21
@@ -227,6 +244,31 @@ def test_dropout_add_layer_norm(T, H, dtype):
         close(db, wb, e_b, "dbeta")
         f = bo.dropout_factor(T, H, p, 42 + H, 1000)
         close(dv, wz * f, f * e_raw + (HALF[dtype] + 2 * U) * (np.abs(wz) + e_raw) * f, "dv")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H", [(9, 61), (40, 520), (300, 1001), (5, 4099), (3, 9001)])
+def test_dropout_add_layer_norm_in_place(T, H, dtype):
+    """Every output over an input of its shape: the same bits (short last vectors read past neighbours that are being written)."""
+    x, gamma, beta, dy, dres, v = _inputs(T, H, dtype, H)
+    rng, p = _rng(7, 8), 0.3
+    stats = [torch.empty(T, device="cuda") for _ in range(2)]
+    z, y = torch.empty_like(x), torch.empty_like(x)
+    moe.moe_dropout_add_layer_norm_forward(v, x, p, rng, gamma, beta, EPS, z, y, *stats)
+    for zi, yi in (("v", "x"), ("x", "v"), ("x", None), (None, "v")):
+        a = dict(v=v.clone(), x=x.clone())
+        zo, yo = (a[n] if n else torch.empty_like(x) for n in (zi, yi))
+        moe.moe_dropout_add_layer_norm_forward(a["v"], a["x"], p, rng, gamma, beta, EPS, zo, yo, *(torch.empty_like(s) for s in stats))
+        assert torch.equal(zo, z) and torch.equal(yo, y), (zi, yi)
+    ws, dg, db = moe.alloc_layer_norm_workspace(T, H), torch.empty_like(gamma), torch.empty_like(gamma)
+
+    def backward(a, dz, dv):
+        moe.moe_dropout_add_layer_norm_backward(a["dy"], a["z"], gamma, *stats, a["dres"], p, rng, dz, dv, dg, db, ws)
+        return dz.clone(), dv.clone(), dg.clone(), db.clone()
+    want = backward(dict(dy=dy, z=z, dres=dres), torch.empty_like(x), torch.empty_like(x))
+    for zi, vi in (("dy", "z"), ("z", "dres"), ("dres", "dy")):
+        a = dict(dy=dy.clone(), z=z.clone(), dres=dres.clone())
+        assert all(torch.equal(p_, q_) for p_, q_ in zip(backward(a, a[zi], a[vi]), want)), (zi, vi)
 
 
 def test_graph_replays_draw_new_masks():
