@@ -122,7 +122,9 @@ int run_drop_add(DropAddParams p, int dtype, hipStream_t s) {
   p.group = g;
   const unsigned grid = row_grid((long)ceil_div(p.T, 256 / g) * ceil_div(p.H, g * 8));
   with_row_form(dtype, p.H, [&](auto t, auto tail) {
-    hipLaunchKernelGGL((drop_add_kernel<decltype(t), tail.value>), dim3(grid), dim3(256), 0, s, p);
+    with_caching<decltype(t)>(p.T, p.H, [&](auto nt) {
+      hipLaunchKernelGGL((drop_add_kernel<decltype(t), tail.value, nt.value>), dim3(grid), dim3(256), 0, s, p);
+    });
   });
   return launched();
 }

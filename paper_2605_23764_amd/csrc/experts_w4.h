@@ -296,22 +296,43 @@ __global__ __launch_bounds__(256) void tiles_w4_kernel(const __bf16* x, const in
   }
 }
 
-// Combine (4.7 us for 32 tokens of H = 7168, latency): out[t,:] = sum over the local slots j of topk_w[t,j] * y[row_of[t,j],:], in slot order: a lane per eight columns of a token.
+// Combine: out[t,:] = sum over the local slots j of topk_w[t,j] * y[row_of[t,j],:], in slot order: a workgroup per 2048 columns of a token, a
+// lane per eight.  The token's local slots are listed first, so that the rows of four of them are under way together.
 __global__ __launch_bounds__(256) void combine_w4_kernel(const float* y, const int32_t* row_of, const float* topk_w, __bf16* out, int T, int H,
                                                          int k) {
-  const int per = H / 8;
-  const long n = (long)T * per;
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
-    const long t = i / per;
-    const int c = (int)(i - t * per) * 8;
+  __shared__ int32_t s_row[kMaxK];
+  __shared__ float s_w[kMaxK];
+  const int chunks = (H + 2047) / 2048, lane = lane_id();
+  for (long task = blockIdx.x; task < (long)T * chunks; task += gridDim.x) {
+    const long t = task / chunks;
+    const int c = ((int)(task - t * chunks) * 256 + threadIdx.x) * 8;
+    const int r = lane < k ? row_of[t * k + lane] : -1;
+    const float w = lane < k ? topk_w[t * k + lane] : 0.f;
+    const uint64_t local = __ballot(r >= 0);
+    const int n = __popcll(local);
+    __syncthreads();                                             // the list of the task before has been read
+    if (threadIdx.x < kWave && r >= 0) {
+      const int m = __popcll(local & ((1ull << lane) - 1));
+      s_row[m] = r;
+      s_w[m] = w;
+    }
+    __syncthreads();
+    if (c >= H) continue;
     f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-    for (int j = 0; j < k; ++j) {
-      const int r = row_of[t * k + j];
-      if (r < 0) continue;
-      const float w = topk_w[t * k + j];
-      const f32x4* src = reinterpret_cast<const f32x4*>(y + (size_t)r * H + c);
-      lo += w * src[0];
-      hi += w * src[1];
+    for (int j = 0; j < n; j += 4) {
+      f32x4 a[4], b[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4* src = reinterpret_cast<const f32x4*>(y + (size_t)s_row[min(j + q, n - 1)] * H + c);
+        a[q] = src[0];
+        b[q] = src[1];
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (j + q < n) {
+          lo += s_w[j + q] * a[q];
+          hi += s_w[j + q] * b[q];
+        }
     }
     *reinterpret_cast<u32x4*>(out + (size_t)t * H + c) =
         u32x4{pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};

@@ -54,7 +54,7 @@ int launch_tiles_w4(const void* x, const int32_t* token_of, const int32_t* offse
 }
 
 int launch_combine_w4(const float* y, const int32_t* row_of, const float* topk_w, void* out, int T, int H, int k, void* stream) {
-  const long want = ((long)T * (H / 8) + 255) / 256;
+  const long want = (long)T * ((H + 2047) / 2048);
   hipLaunchKernelGGL(combine_w4_kernel, dim3((unsigned)(want < (1 << 16) ? want : 1 << 16)), dim3(256), 0, static_cast<hipStream_t>(stream), y,
                      row_of, topk_w, static_cast<__bf16*>(out), T, H, k);
   return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_LAUNCH;

@@ -43,9 +43,9 @@ template <typename T> __device__ __forceinline__ const T* row_of(const void* p, 
 }
 template <typename T> __device__ __forceinline__ T* row_of(void* p, int t, int H) { return static_cast<T*>(p) + (size_t)t * H; }
 
-// NT (both kernels below; arrays above kNormNtBytes): what is read or written once in the training step (y, v, dy, dres, dx, dv) passes the
-// caches by, which leaves them to x or z, read again by the backward.  T = 8192, H = 7168 bf16 (117 MB an array): forward + backward
-// 147 -> 140 us, with dropout and residual 209 -> 200; where everything fits into the caches it costs up to a fifth.
+// NT (these kernels and drop_add; arrays above kNormNtBytes): what is read or written once in the training step (y, v and the residual, dy,
+// dres, dx, dv) passes the caches by, which leaves them to x or z, read again by the backward.  T = 8192, H = 7168 bf16 (117 MB an array): forward + backward
+// 147 -> 140 us, with dropout and residual 209 -> 200, and 184 -> 182 with the residual; where everything fits into the caches it costs up to a fifth.
 constexpr size_t kNormNtBytes = 64u << 20;
 
 // A group of lanes per row, ITEMS vectors per lane; groups of up to a wave share a workgroup.  Workgroups walk rows in strides, the next
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(512) void norm_forward_kernel(NormForwardParams p) 
       q.x[i] = raw_zero<T>();
       if (FUSED) q.v[i] = raw_zero<T>();
       if (t < p.T && at < H) {
-        if (p.x) q.x[i] = raw_request<T, TAIL>(row_of<T>(p.x, (int)t, H), at, H);
+        if (p.x) q.x[i] = raw_request<T, TAIL, NT && FUSED>(row_of<T>(p.x, (int)t, H), at, H);
         if (FUSED) q.v[i] = raw_request<T, TAIL, NT>(row_of<T>(p.v, (int)t, H), at, H);
       }
     }
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(1024) void norm_columns_kernel(const float* part, i
 
 // ---- dropout + residual alone (and its backward: no residual): a lane per vector ----
 // The generator takes 20 products of 32 x 32 bits per vector, some 150 instructions, which hide behind the three arrays: T = 8192, H = 7168
-// bf16, both directions, 118 us (5.0 TB/s), with p = 0 108.
+// bf16, both directions, 106 us (5.5 TB/s; 116 by way of the caches), with p = 0 98.
 struct DropAddParams {
   const void *v, *res;            // res may be null
   void* out;
@@ -411,7 +411,7 @@ struct DropAddParams {
   int T, H, group;                // lanes per row: a power of two up to 256
 };
 
-template <typename T, bool TAIL>
+template <typename T, bool TAIL, bool NT>
 __global__ __launch_bounds__(256) void drop_add_kernel(DropAddParams p) {
   const int H = p.H, rows = 256 / p.group, chunks = (H + p.group * 8 - 1) / (p.group * 8);
   const int r = threadIdx.x / p.group, g = threadIdx.x & (p.group - 1);
@@ -422,9 +422,9 @@ __global__ __launch_bounds__(256) void drop_add_kernel(DropAddParams p) {
     const int vec = (int)(task - rb * chunks) * p.group + g, at = vec * 8;
     const long t = rb * rows + r;
     if (t >= p.T || at >= H) continue;
-    const Raw8<T> rv = raw_load<T, TAIL>(row_of<T>(p.v, (int)t, H), at, H);
+    const Raw8<T> rv = raw_load<T, TAIL, NT>(row_of<T>(p.v, (int)t, H), at, H);
     Raw8<T> rr = raw_zero<T>();
-    if (p.res) rr = raw_load<T, TAIL>(row_of<T>(p.res, (int)t, H), at, H);
+    if (p.res) rr = raw_load<T, TAIL, NT>(row_of<T>(p.res, (int)t, H), at, H);
     float v[8];
 #pragma unroll
     for (int x = 0; x < 8; ++x) v[x] = raw_get<T>(rv, x);
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(256) void drop_add_kernel(DropAddParams p) {
     if (p.res)
 #pragma unroll
       for (int x = 0; x < 8; ++x) v[x] += raw_get<T>(rr, x);
-    raw_store<T, TAIL>(row_of<T>(p.out, (int)t, H), at, H, raw_pack<T>(v));
+    raw_store<T, TAIL, NT>(row_of<T>(p.out, (int)t, H), at, H, raw_pack<T>(v));
   }
 }
 
