@@ -118,9 +118,9 @@ template <bool FUSED> int run_norm_backward(NormBackwardParams p, int dtype, voi
 
 int run_drop_add(DropAddParams p, int dtype, hipStream_t s) {
   int g = 8;
-  while (g < 256 && g * 8 < p.H) g *= 2;
+  while (g < kDropGroup && g * 8 * kDropItems < p.H) g *= 2;
   p.group = g;
-  const unsigned grid = row_grid((long)ceil_div(p.T, 256 / g) * ceil_div(p.H, g * 8));
+  const unsigned grid = row_grid((long)ceil_div(p.T, 256 / g) * ceil_div(p.H, g * 8 * kDropItems));
   with_row_form(dtype, p.H, [&](auto t, auto tail) {
     with_caching<decltype(t)>(p.T, p.H, [&](auto nt) {
       hipLaunchKernelGGL((drop_add_kernel<decltype(t), tail.value, nt.value>), dim3(grid), dim3(256), 0, s, p);
@@ -281,7 +281,7 @@ int moe_balance_forward(int32_t T, int32_t E, int32_t k, const float* d_logits, 
   hipStream_t s = static_cast<hipStream_t>(stream);
   with_token_form(E, [&](auto lanes, auto tail) {
     const int want = ceil_div(T, kBalThreads / lanes.value);
-    p.parts = T <= kBalOneT ? 1 : want < kBalMaxParts ? want : kBalMaxParts;
+    p.parts = (long)T * lanes.value <= kBalOneLanes ? 1 : want < kBalMaxParts ? want : kBalMaxParts;
     hipLaunchKernelGGL((balance_kernel<lanes.value, tail.value>), dim3(p.parts), dim3(kBalThreads), 0, s, p);
   });
   if (p.parts > 1) hipLaunchKernelGGL(balance_join_kernel, dim3(1), dim3(1024), 0, s, p);

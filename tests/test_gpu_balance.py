@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 # lanes per token 1, 2, 4, 8, 16, 32, 64; E not a multiple of 4; one workgroup, two launches
 SHAPES = [(1, 1, 1), (1, 256, 8), (5, 3, 3), (64, 4, 1), (65, 8, 2), (200, 7, 7), (1000, 16, 4), (333, 24, 3), (4097, 60, 6), (777, 64, 8),
-          (500, 127, 5), (300, 128, 16), (900, 250, 8), (3001, 256, 8), (20000, 33, 2), (20003, 256, 8), (70000, 9, 3)]
+          (500, 127, 5), (300, 128, 16), (900, 250, 8), (3001, 256, 8), (20000, 33, 2), (20003, 256, 8), (70000, 9, 3), (128, 256, 8), (129, 256, 8), (8192, 4, 1), (8193, 3, 2)]
 
 
 def _inputs(T, E, k, seed, masked=None, hole=0.0):
