@@ -85,13 +85,39 @@ template <bool FUSED> int run_norm_forward(NormForwardParams p, int dtype, hipSt
 
 int norm_parts(int T) { return T < kNormMaxParts ? T : kNormMaxParts; }
 
+// Whether arrays of n bytes share any.
+bool overlap(const void* a, const void* b, size_t n) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + n && y < x + n;
+}
+
 template <bool FUSED> int run_norm_backward(NormBackwardParams p, int dtype, void* dgamma, void* dbeta, hipStream_t s) {
   const bool sums = dgamma || dbeta;
+  const size_t bytes = (size_t)p.T * p.H * (dtype == MOE_BF16 ? 2 : 4);
+  const bool in_place = overlap(p.dx, p.dy, bytes) || overlap(p.dx, p.x, bytes) ||
+                        (FUSED && (overlap(p.dv, p.dy, bytes) || overlap(p.dv, p.x, bytes)));
   if (!sums) p.part = nullptr;
   p.inv_h = 1.0f / (float)p.H;
   with_row_form(dtype, p.H, [&](auto t, auto tail) {
     using T = decltype(t);
     int parts = 0;
+    if (sums && p.T > 0 && p.T <= kNormFewRows && bytes <= kNormFewBytes && p.H <= kRowMaxH) {
+      p.part = nullptr;
+      p.dgamma = dgamma; p.dbeta = dbeta;
+      p.group = row_group(p.H);
+      p.groups = kNormFewLanes / p.group;
+      p.row_groups = ceil_div(p.T, p.groups);
+      const auto few = norm_backward_few_kernel<T, tail.value, FUSED>;
+      const int rows = p.row_groups, columns = ceil_div(p.H, kWave);
+      const dim3 lanes(p.group * p.groups);
+      if (in_place) {                                            // the columns' sums before anything lies over what they read
+        p.row_groups = 0;
+        hipLaunchKernelGGL(few, dim3(columns), lanes, 0, s, p);
+        p.row_groups = rows;
+      }
+      hipLaunchKernelGGL(few, dim3(in_place ? rows : rows + columns), lanes, 0, s, p);
+      return;
+    }
     if (p.T > 0 && p.H > kRowMaxH) {
       if (sums) {                                                // ahead of the launch that writes dx, which may be dy or x
         parts = norm_parts(p.T) < 64 ? norm_parts(p.T) : 64;

@@ -16,6 +16,10 @@ namespace moe {
 
 constexpr int kRowMaxH = kRowMaxWaves * kWave * 8;               // longest row that stays in registers
 constexpr int kNormMaxParts = 512;                               // partial sums of dgamma / dbeta, at most
+// norm_backward_few_kernel takes up to so many rows, in arrays of up to so many bytes, in workgroups of up to so many lanes
+constexpr int kNormFewRows = 1024;
+constexpr size_t kNormFewBytes = 6u << 20;
+constexpr int kNormFewLanes = 1024;
 
 // Arrays are [T, H], vectors [H]; what may be null is looked at once per launch.
 struct NormForwardParams {
@@ -32,7 +36,9 @@ struct NormBackwardParams {
   const void *dy, *x, *gamma, *dres;   // gamma, dres may be null
   const float *mean, *rstd;
   void *dx, *dv;                       // dv: fused form only
-  float* part;                         // [parts][2][H] sums of dy * xh and dy, null: not wanted
+  float* part;                         // [parts][2][H] sums of dy * xh and dy, null: not wanted (here)
+  void *dgamma, *dbeta;                // the launch of few rows alone: either may be null
+  int row_groups;                      // its workgroups for rows; those behind them have columns
   DropParams drop;
   float inv_h;
   int T, H, group, groups;             // lanes per row; rows that a workgroup has in hand at a time
@@ -149,10 +155,10 @@ __global__ __launch_bounds__(512) void norm_forward_kernel(NormForwardParams p) 
 // its rows' sums of dy * xh and dy in registers: one partial per workgroup at the end, a row per CU and 15 MB in all at H = 7168 (two
 // workgroups per CU with twice the partials: +1 .. +3 us).  T = 8192, H = 7168 bf16: 76 us, 6.4 TB/s (x still comes from the
 // memory-side cache in part); with dropout 101 us, 5.8 TB/s.
+// block: this workgroup among n_blocks.  s_part, for several groups' sums: [groups][4][G][4].
 template <typename T, bool TAIL, bool FUSED, bool NT>
-__global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackwardParams p) {
+__device__ __forceinline__ void norm_backward_rows(const NormBackwardParams& p, int block, int n_blocks, float* s_part) {
   __shared__ float s_sum[2][2][kRowMaxWaves];
-  extern __shared__ __align__(16) float s_part[];                // several groups: [groups][4][G][4]
   const int G = p.group, H = p.H;
   const int rg = threadIdx.x / G, g = threadIdx.x - rg * G, at = g * 8;
   const DropKey key = FUSED ? drop_key(p.drop) : DropKey{};
@@ -172,12 +178,12 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackwardParams 
       if (p.dres) r.dres = raw_request<T, TAIL, NT>(row_of<T>(p.dres, t, H), at, H);
     }
   };
-  const int stride = gridDim.x * p.groups;
+  const int stride = n_blocks * p.groups;
   Row cur;
-  load(cur, blockIdx.x * p.groups + rg);
+  load(cur, block * p.groups + rg);
   // as many turns for every group of the workgroup: the barrier of a turn is reached by all.  (64 bits: t0 + stride may pass 2^31.)
   int turn = 0;
-  for (long t0 = (long)blockIdx.x * p.groups; t0 < p.T; t0 += stride, turn ^= 1) {
+  for (long t0 = (long)block * p.groups; t0 < p.T; t0 += stride, turn ^= 1) {
     const int t = (int)min(t0 + rg, (long)p.T);
     Row next;
     load(next, (int)min(t0 + rg + stride, (long)p.T));
@@ -214,7 +220,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackwardParams 
     cur = next;
   }
   if (!p.part) return;
-  float* out = p.part + (size_t)blockIdx.x * 2 * H;
+  float* out = p.part + (size_t)block * 2 * H;
   if (p.groups == 1) {
     if (at >= H) return;
     raw_store<float, TAIL>(out, at, H, raw_pack<float>(acc_g));
@@ -241,6 +247,47 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackwardParams 
       for (int x = 0; x < 3; ++x)
         if (c + x < H) to[c + x] = t[x];
     }
+  }
+}
+
+template <typename T, bool TAIL, bool FUSED, bool NT>
+__global__ __launch_bounds__(1024) void norm_backward_kernel(NormBackwardParams p) {
+  extern __shared__ __align__(16) float s_part[];
+  norm_backward_rows<T, TAIL, FUSED, NT>(p, blockIdx.x, gridDim.x, s_part);
+}
+
+// Few rows in one launch: workgroups behind those of the rows take 64 columns each and go down all rows of dy and x for
+// them, mostly out of the L2s, so nothing has to meet across workgroups and the launch that adds up partial sums goes
+// away.  dx and dv may not lie over dy or x while both kinds run: then the columns have a launch of their own first, in the
+// same order.  Forward and backward of a step, two launches for the backward -> one, us: 64 x 2048 bf16 20.2 -> 14.9, 600 x
+// 4096 19.2 -> 17.0, 800 x 1408 fp32 19.0 -> 16.2; with dropout 600 x 1408 fp32 20.8 -> 16.7, 700 x 4096 bf16 23.2 -> 22.0.
+// Past the limits the columns' workgroups are too few for their bytes and too long for their rows: 512 x 7168 (7 MB) 20.8
+// -> 20.9, 1000 x 4096 (8 MB) 19.8 -> 24.4, 1500 x 512 18.4 -> 19.2, 3000 x 256 17.5 -> 30.8.  512 lanes in place of 1024:
+// 3 us more at 1000 x 512, level at few rows.
+template <typename T, bool TAIL, bool FUSED>
+__global__ __launch_bounds__(1024) void norm_backward_few_kernel(NormBackwardParams p) {
+  __shared__ float s_col[2][kRowMaxWaves][kWave];
+  if ((int)blockIdx.x < p.row_groups) {
+    norm_backward_rows<T, TAIL, FUSED, false>(p, blockIdx.x, p.row_groups, nullptr);
+    return;
+  }
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave, lane = lane_id();
+  const int col = ((int)blockIdx.x - p.row_groups) * kWave + lane, at = min(col, p.H - 1);
+  float g = 0.f, b = 0.f;
+#pragma unroll 8
+  for (int t = wave; t < p.T; t += waves) {
+    const float d = (float)row_of<T>(p.dy, t, p.H)[at], x = (float)row_of<T>(p.x, t, p.H)[at];
+    g += d * ((x - p.mean[t]) * p.rstd[t]);
+    b += d;
+  }
+  s_col[0][wave][lane] = g;
+  s_col[1][wave][lane] = b;
+  __syncthreads();
+  T* out = static_cast<T*>(wave ? p.dbeta : p.dgamma);           // one wave dgamma, one dbeta
+  if (wave < 2 && col < p.H && out) {
+    float t = 0.f;
+    for (int w = 0; w < waves; ++w) t += s_col[wave][w][lane];
+    out[col] = (T)t;
   }
 }
 

@@ -85,6 +85,32 @@ def test_many_rows(T, H, dtype):
     assert all(torch.equal(a, b) for a, b in zip((dx, dg, db), again))      # a fixed order of every sum
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H", [(1, 8), (1024, 64), (1025, 64), (1030, 7), (1100, 333), (1024, 1001), (1500, 1001), (384, 4096), (768, 4096),
+                                 (769, 4096), (200, 8191)])
+def test_backward_of_few_and_many_rows(T, H, dtype):
+    """Around the limits of the backward in one launch (1024 rows, 6 MB), alone and with dropout; with one of the two sums; dx over dy."""
+    print(f"few rows T={T} H={H} {dtype}", flush=True)
+    x, gamma, beta, dy, dres, _ = _inputs(T, H, dtype, 3 * H + T)
+    _, mean, rstd = _forward(x, gamma, beta)
+    want = backward_bounds(f64(dy), f64(x), f64(gamma), f64(mean), f64(rstd), f64(dres), dtype)
+    full = _backward(dy, x, gamma, mean, rstd, dres)
+    for i, name in enumerate(("dx", "dgamma", "dbeta")):
+        close(full[i], want[i], want[i + 3], name)
+    assert torch.equal(_backward(dy, x, gamma, mean, rstd, dres, dg=False)[2], full[2])
+    assert torch.equal(_backward(dy, x, gamma, mean, rstd, dres, db=False)[1], full[1])
+    over = dy.clone()
+    assert all(torch.equal(a, b) for a, b in zip(_backward(over, x, gamma, mean, rstd, dres, dx=over), full))
+    dz, dv = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    dg, db = torch.full_like(gamma, float("nan")), torch.full_like(gamma, float("nan"))
+    moe.moe_dropout_add_layer_norm_backward(dy, x, gamma, mean, rstd, dres, 0.3, _rng(5, 6), dz, dv, dg, db,
+                                            moe.alloc_layer_norm_workspace(T, H))
+    for got, i, name in ((dz, 0, "dz"), (dg, 1, "dgamma"), (db, 2, "dbeta")):
+        close(got, want[i], want[i + 3], name)
+    f = bo.dropout_factor(T, H, 0.3, 5, 6)
+    close(dv, want[0] * f, f * want[6] + (HALF[dtype] + 2 * U) * (np.abs(want[0]) + want[6]) * f, "dv")
+
+
 @pytest.mark.parametrize("T,H", [(30000, 72), (5300, 520), (5200, 1001), (3000, 2048), (1601, 7168)])
 def test_forward_walks_rows(T, H):
     """More rows than a launch has workgroups for: several turns in the forward too, alone and with dropout."""
