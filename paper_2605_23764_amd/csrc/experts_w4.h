@@ -231,9 +231,10 @@ __device__ __forceinline__ int w4_selected(const RouteParams& p, int e, W4Rows* 
   __syncthreads();
   return __popcll(members);
 }
-// topk_idx, topk_w and row_of of all tokens by one workgroup.
+// topk_idx, topk_w and row_of of all tokens by one workgroup, and the workspace's status, which a routing launch would clear.
 __device__ __forceinline__ void w4_route(const RouteParams& p, int32_t* s_idx, float* s_val) {
   const int lane = lane_id(), wave = threadIdx.x / kWave;
+  if (threadIdx.x == 0) p.tiles.meta[kMetaStatus] = 0;
   s_idx += wave * kRouteTokensPerWave * kMaxK;
   s_val += wave * kRouteTokensPerWave * kMaxK;
   for (int t0 = wave * kRouteTokensPerWave; t0 < p.T; t0 += kW4Waves * kRouteTokensPerWave) {

@@ -36,7 +36,7 @@ int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream) {
     else with_blocks(rt, std::integral_constant<int, 2>{}, routed);
   };
   if (l.logits) {
-    p.route.logits = l.logits; p.route.topk_idx = l.topk_idx; p.route.topk_w = l.topk_w; p.route.row_of = l.row_of;
+    p.route.logits = l.logits; p.route.topk_idx = l.topk_idx; p.route.topk_w = l.topk_w; p.route.row_of = l.row_of; p.route.tiles.meta = l.meta;
     p.route.T = l.T; p.route.E = l.E; p.route.E_local = l.E_local; p.route.expert_base = l.expert_base; p.route.k = l.k;
     with_rows(std::integral_constant<int, 1>{}, std::true_type{});
   } else if (rows32) {

@@ -19,6 +19,7 @@ struct W4Launch {
   int32_t* topk_idx;
   float* topk_w;
   int32_t* row_of;
+  int32_t* meta;                 // MetaWord, of which GEMM-1 clears the status
   int T, E, expert_base, k;
 };
 constexpr int kW4MaxRoutedT = 16, kW4FewRows = 8;

@@ -982,7 +982,7 @@ int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_lo
   // leaves.
   if (!saved && (long)c.s.T * ceil_div(c.s.E, kWave) <= kW4MaxRoutedT && rows <= kW4FewRows && c.s.k <= c.s.E_local) {
     for (W4Launch* g : {&g1, &g2}) {
-      g->logits = d_logits; g->topk_idx = c.sv.topk_idx; g->topk_w = c.sv.topk_w; g->row_of = c.sv.row_of;
+      g->logits = d_logits; g->topk_idx = c.sv.topk_idx; g->topk_w = c.sv.topk_w; g->row_of = c.sv.row_of; g->meta = tile_map(c).meta;
     }
   } else {
     if ((st = run_route(c, d_logits, false)) != MOE_OK) return st;
