@@ -130,7 +130,7 @@ template <bool FUSED> int run_norm_backward(NormBackwardParams p, int dtype, voi
       p.groups = 1024 / p.group;
       while (p.groups > 1 && p.groups * p.group > kWave && p.T < 256 * p.groups) p.groups /= 2;
       const int want = ceil_div(p.T, p.groups);
-      parts = want < 256 ? want : 256;
+      parts = want < kNormMaxParts ? want : kNormMaxParts;
       const size_t lds = p.groups > 1 ? (size_t)p.groups * p.group * 64 : 0;
       with_caching<T>(p.T, p.H, [&](auto nt) {
         hipLaunchKernelGGL((norm_backward_kernel<T, tail.value, FUSED, nt.value>), dim3(parts), dim3(p.group * p.groups), lds, s, p);

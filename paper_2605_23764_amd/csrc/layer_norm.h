@@ -15,7 +15,7 @@
 namespace moe {
 
 constexpr int kRowMaxH = kRowMaxWaves * kWave * 8;               // longest row that stays in registers
-constexpr int kNormMaxParts = 512;                               // partial sums of dgamma / dbeta, at most
+constexpr int kNormMaxParts = 256;                               // partial sums of dgamma / dbeta, at most: workgroups of the backward
 // norm_backward_few_kernel takes up to so many rows, in arrays of up to so many bytes, in workgroups of up to so many lanes
 constexpr int kNormFewRows = 1024;
 constexpr size_t kNormFewBytes = 6u << 20;
