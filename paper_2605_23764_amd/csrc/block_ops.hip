@@ -73,7 +73,7 @@ template <bool FUSED> int run_norm_forward(NormForwardParams p, int dtype, hipSt
     }
     p.group = vecs <= kWave ? row_group(p.H) : ceil_div(vecs, 2 * kWave) * kWave;
     const int rows = p.group > kWave ? 1 : 256 / p.group, threads = p.group * rows;
-    const int most = 256 * (threads > 768 ? 1 : 1536 / threads), want = ceil_div(p.T, rows);
+    const int most = 256 * (1536 / threads), want = ceil_div(p.T, rows);   // up to 512 threads
     const dim3 grid(want < most ? want : most);
     with_caching<T>(p.T, p.H, [&](auto nt) {
       if (vecs <= kWave) hipLaunchKernelGGL((norm_forward_kernel<T, 1, tail.value, FUSED, nt.value>), grid, dim3(threads), 0, s, p);
