@@ -4,7 +4,10 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 #include "balance.h"
+#include "device_cus.h"
 #include "layer_norm.h"
 
 using namespace moe;
@@ -73,7 +76,7 @@ template <bool FUSED> int run_norm_forward(NormForwardParams p, int dtype, hipSt
     }
     p.group = vecs <= kWave ? row_group(p.H) : ceil_div(vecs, 2 * kWave) * kWave;
     const int rows = p.group > kWave ? 1 : 256 / p.group, threads = p.group * rows;
-    const int most = 256 * (1536 / threads), want = ceil_div(p.T, rows);   // up to 512 threads
+    const int most = device_cus() * (1536 / threads), want = ceil_div(p.T, rows);   // up to 512 threads
     const dim3 grid(want < most ? want : most);
     with_caching<T>(p.T, p.H, [&](auto nt) {
       if (vecs <= kWave) hipLaunchKernelGGL((norm_forward_kernel<T, 1, tail.value, FUSED, nt.value>), grid, dim3(threads), 0, s, p);
@@ -126,11 +129,12 @@ template <bool FUSED> int run_norm_backward(NormBackwardParams p, int dtype, voi
       hipLaunchKernelGGL((norm_backward_long_kernel<T, tail.value, FUSED>), dim3(row_grid(p.T)), dim3(1024), 0, s, p);
     } else if (p.T > 0) {
       p.group = row_group(p.H);
+      const int cus = std::min(device_cus(), kNormMaxParts);
       // a workgroup per CU, of as many rows at a time as 1024 threads hold, fewer where that leaves CUs without rows
       p.groups = 1024 / p.group;
-      while (p.groups > 1 && p.groups * p.group > kWave && p.T < 256 * p.groups) p.groups /= 2;
+      while (p.groups > 1 && p.groups * p.group > kWave && p.T < cus * p.groups) p.groups /= 2;
       const int want = ceil_div(p.T, p.groups);
-      parts = want < kNormMaxParts ? want : kNormMaxParts;
+      parts = std::min(want, cus);
       const size_t lds = p.groups > 1 ? (size_t)p.groups * p.group * 64 : 0;
       with_caching<T>(p.T, p.H, [&](auto nt) {
         hipLaunchKernelGGL((norm_backward_kernel<T, tail.value, FUSED, nt.value>), dim3(parts), dim3(p.group * p.groups), lds, s, p);

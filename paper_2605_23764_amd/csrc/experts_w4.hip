@@ -2,6 +2,7 @@
 // routing and Combine around them, is in moe_ffn.hip).
 #include "../../include/moe_ffn.h"
 
+#include "device_cus.h"
 #include "experts_w4.h"
 #include "experts_w4_launch.h"
 
@@ -25,7 +26,7 @@ int launch_experts_w4(const W4Launch& l, bool swiglu, void* stream) {
   // leaves room for more waves, and the few experts above read their weights again.  Items of four column blocks, whose activations
   // are fetched half as often, as long as there are two of them per CU (32 tokens, H = 7168, I = 2048, 32 of 256 experts: 117 -> 97
   // us; 64 tokens, H = 2048, I = 1408, 16 experts: 47 -> 38; but one token there 20.8 -> 22.7).
-  const bool rows32 = l.rows > kW4FewRows, wide = (long)l.experts * (l.N / w4_columns(4, swiglu)) >= 512;
+  const bool rows32 = l.rows > kW4FewRows, wide = (long)l.experts * (l.N / w4_columns(4, swiglu)) >= 2 * device_cus();
   hipStream_t s = static_cast<hipStream_t>(stream);
   auto with_blocks = [&](auto rt, auto nb, auto routed) {
     if (swiglu) launch<rt.value, nb.value, true, routed.value>(p, l.E_local, s);

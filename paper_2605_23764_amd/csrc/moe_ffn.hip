@@ -11,6 +11,7 @@
 
 #include "backward.h"
 #include "common.h"
+#include "device_cus.h"
 #include "experts_w4_launch.h"
 #include "gemm_bf16.h"
 #include "gemm_f32.h"
@@ -134,18 +135,6 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 // that is only sound if no 128-byte line is shared by two tasks' rows, i.e. if the buffers that are both
 // written and read inside the launch start on a line boundary (rows are multiples of 128 bytes).
 bool aligned128(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 127u) == 0; }
-
-int device_cus() {
-  static int cached[64] = {0};
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-  if (!cached[dev]) {
-    int n = 0;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
-    cached[dev] = n;
-  }
-  return cached[dev];
-}
 
 int make_ctx(Ctx& c, const MoeShape* shape, const MoeSaved* saved, void* ws, size_t ws_bytes, void* stream) {
   int st = check_shape(shape);
