@@ -465,7 +465,7 @@ __global__ __launch_bounds__(256) void drop_add_kernel(DropAddParams p) {
   const int H = p.H, rows = 256 / p.group, wide = p.group * 8 * kItems, chunks = (H + wide - 1) / wide;
   const int r = threadIdx.x / p.group, g = threadIdx.x & (p.group - 1);
   const DropKey key = drop_key(p.drop);
-  const long tasks = ((long)p.T + rows - 1) / rows * chunks;   // 64 bits: T may be all that 31 bits hold
+  const long tasks = (long)(((uint32_t)p.T + (uint32_t)rows - 1) / (uint32_t)rows) * chunks;   // T may be all that 31 bits hold
   for (long task = blockIdx.x; task < tasks; task += gridDim.x) {
     const long rb = task / chunks;
     const int first = (int)(task - rb * chunks) * p.group * kItems + g;
