@@ -18,7 +18,7 @@
 namespace moe {
 
 constexpr int kBalThreads = 1024;
-constexpr int kBalMaxParts = 128;          // workgroups of the first launch, at most: what one workgroup joins afterwards (64: +2 us, 256: +3)
+constexpr int kBalMaxParts = 128;          // workgroups of the first launch, at most: what one workgroup joins afterwards (T = 8192: 64 +2 us, 256 +3)
 constexpr int kBalAhead = 4;               // tokens per group of lanes under way together (2: +0.5 us)
 // Tokens x lanes that one workgroup does alone, in one launch: two turns (E = 256: T = 128 11.3 -> 9.9 us, E = 64: T = 512 10.6 -> 9.2; with
 // four turns T = 256 11.2 -> 17.6).

@@ -15,15 +15,20 @@
 // Bound by that read: 32 tokens, H = 7168, I = 2048, 32 of 256 experts, k = 8 (about 20 with rows, 482 MB): GEMM-1 57 us, GEMM-2 30, 5.5 TB/s
 // where a loop that only loads pieces of 256 bytes reaches 6.2; with few weights (one token, H = 2048, I = 1408: 18 MB, 7.4 + 5.7 us) by
 // the latency of a workgroup's start, four steps and a join; with many rows by the activations' fetches.
-// Products are exact in fp32 (bf16 x 2 bits), sums fp32.  GEMM-1's results are rounded to bf16 (they are an MFMA's operand next), GEMM-2's
-// stay fp32 until Combine has added them up, which rounds the layer's output once: 8 bytes of traffic per value of few rows.
+// Products are exact in fp32 (bf16 x 2 bits), sums fp32.  GEMM-1's results are rounded to bf16, as the layer's are with bf16 weights: they are
+// an MFMA's operand next, and keeping more of them would take two operands, twice the MFMAs and the activations' fetches.  That rounding
+// costs 1.6e-3 of the output (2-norm) beside the 1.7e-3 of its own rounding, 2.3e-3 together.  GEMM-2's results stay fp32 until Combine has
+// added them up, which rounds the layer's output once: 8 bytes of traffic per value of few rows.
 #pragma once
 #include "experts_w4_launch.h"
 #include "route_select.h"
 
 namespace moe {
 
-constexpr int kW4Waves = 4;                // waves of a workgroup, each with a share of K
+// Waves of a workgroup, each with a share of K.  2, 4 or 8 of them, us: H = 2048, I = 1408, 16 experts, k = 4, T = 1 17.4, 15.4, 18.2, T = 64
+// 33.2, 34.5, 35.7, T = 128 56.9, 55.5, 58.9; H = 7168, I = 2048, 32 of 256, k = 8, T = 1 22.7, 21.5, 27.9, T = 8 55.5, 55.2, 51.9, T = 32 101.7,
+// 91.8, 93.9.
+constexpr int kW4Waves = 4;
 // Waves per SIMD that the registers have to leave room for.  A wave has one step of its share in registers and no more (a ring of two or
 // three steps: 2 to 30 % slower), so the bytes under way come from the number of waves.
 constexpr int w4_occupancy(int row_blocks, int blocks) { return row_blocks == 2 ? 3 : blocks == 4 ? 4 : 5; }
@@ -342,7 +347,8 @@ __global__ __launch_bounds__(256) void combine_w4_kernel(const float* y, const i
 
 // Weights to blocks: a lane per block.  The scale brings the largest magnitude of the 32 into [4, 8), values are rounded to the nearest
 // code (ties to the even one), those above 6 to 6.  A block of zeros has scale 1.  Non-finite values have no code: the block's
-// scale is 255.
+// scale is 255.  Bound by the weights' read, once: 32 x 7168 x 4096 bf16 (2.4 GB with the blocks) 531 us, 4.5 TB/s where a large copy takes
+// 436; fp32 759 us, 5.6 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_w4_kernel(const T* w, uint8_t* q, uint8_t* scale, long blocks, int groups, int N) {
   const long stride = (long)gridDim.x * 256;

@@ -2,7 +2,7 @@
 //
 // A row of H elements is ceil(H / 8) vectors.  Every vector is one 16-byte load (fp32: two), also in rows of odd H that start at no
 // multiple of 16 bytes: global memory takes vector accesses at any element's address.  Only a row's last vector may be short
-// (TAIL: H % 8 != 0) and is then moved element by element.
+// (TAIL: H % 8 != 0): it is loaded as the row's last eight elements and moved down, and stored element by element.
 #pragma once
 #include "common.h"
 #include "philox.h"
