@@ -144,8 +144,8 @@ def test_dropout_past_the_caches(T, H, dtype):
     assert torch.equal(a["z"], dz) and torch.equal(a["dy"], dv) and torch.equal(dg2, dg) and torch.equal(db2, db)
 
 
-# A launch of the forward has room for 6144 rows of 520 .. 1024 elements, 3072 of 2048, 2048 of 2051, 768 of 7168: one to three turns more, the
-# last one short; with short last vectors and in fp32.
+# A launch of the forward has room for 24 rows of 520 .. 1024 elements per CU (256 of them), 12 of 2048, 8 of 2051, 3 of 7168: one to three turns
+# more, the last one short; with short last vectors and in fp32.
 @pytest.mark.parametrize("T,H,dtype", [(6151, 520, "bf16"), (13001, 1001, "bf16"), (12300, 1001, "f32"), (3100, 2048, "bf16"), (4200, 2051, "bf16"),
                                        (2050, 2051, "f32"), (1700, 7167, "bf16"), (24600, 65, "bf16"), (50000, 7, "f32")])
 def test_forward_in_several_turns(T, H, dtype):
