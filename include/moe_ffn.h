@@ -401,6 +401,115 @@ int moe_router_backward(int32_t T, int32_t E, int32_t k, const float* d_logits, 
                         const float* d_topk_w, const float* d_dtopk_w, const uint8_t* d_mask, float coef,
                         const int32_t* d_counts, const float* d_dloss, float* d_dlogits, void* stream);
 
+/* ---- Routing by scores: sigmoid or softmax scores, a bias for balance, groups of experts, weights renormalised or as they are.
+ *      An alternative to moe_route in front of the layer; the layer, its backward and the balance loss are the same. ---- */
+
+typedef enum MoeScore { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } MoeScore;
+
+/*
+ * Limits: 1 <= n_group <= 16, n_group divides E, 1 <= topk_group <= n_group, k <= topk_group * E / n_group; renormalize 0 or 1;
+ * scale finite.
+ */
+typedef struct MoeScores {
+  int32_t score;       /* MoeScore: softmax over all E logits, or sigmoid of each */
+  int32_t n_group;     /* groups of E / n_group consecutive experts; 1: none */
+  int32_t topk_group;  /* groups that stay */
+  int32_t renormalize; /* 1: the selected scores are divided by their sum */
+  float scale;         /* of the weights */
+} MoeScores;
+
+/*
+ * moe_route with another selection.  s[t,e] = the score of expert e, key[t,e] = s[t,e] + bias[e];
+ *   the topk_group groups stay whose best key + second best key are largest (ties: the lowest group), of their experts the k
+ *   with the largest keys are selected, in that order (ties: the lowest expert), and
+ *   topk_w[t,j] = scale * s[t,e_j] / (renormalize ? sum over the selected of s : 1),  0 / 0 = 0
+ * Scores and keys are computed in 64 bits, so that the selection is that of the definition; the weights are rounded once.  The bias
+ * takes part in the selection alone.  A logit of NaN counts as -inf, as in moe_route.  An expert whose logit is -inf (or whose key is
+ * NaN) comes behind all others, with weight 0 where it is selected all the same (logit -inf); in a group's score it counts 0 beside a
+ * living one.  Several logits of +inf share a softmax's probability evenly.
+ *   d_logits [T,E] f32;  d_bias [E] f32 or NULL: 0
+ *   saved, d_workspace   filled as by moe_route: moe_dispatch_to_combine, moe_dispatch_to_combine_w4 or the stage entry points
+ *                        follow, then moe_ffn_backward, and moe_route_scores_backward on its d_dtopk_w
+ */
+int moe_route_scores(const MoeShape* shape, const MoeScores* scores, const float* d_logits, const float* d_bias,
+                     const MoeSaved* saved, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradient of its logits: d topk_w / d logits (the selection and the bias carry none) applied to dtopk_w, plus dadd.
+ *   d_topk_idx [T,k] as selected (ids outside 0 .. E-1 have no part);  d_dtopk_w [T,k] f32
+ *   d_dadd     [T,E] f32, NULL: 0.  moe_router_backward's without topk_w, for a balance loss; may be d_dlogits
+ *   d_dlogits  [T,E] f32, overwritten (may be d_logits)
+ */
+int moe_route_scores_backward(int32_t T, int32_t E, int32_t k, const MoeScores* scores, const float* d_logits,
+                              const int32_t* d_topk_idx, const float* d_dtopk_w, const float* d_dadd, float* d_dlogits,
+                              void* stream);
+
+/*
+ * A step of the bias towards balance: bias_out[e] = bias[e] + rate * sign(mean of the counts - counts[e]), compared as whole numbers.
+ *   d_counts [E] i32   selections per expert: moe_balance_forward's (or those summed over ranks); non-negative
+ *   d_bias, d_bias_out [E] f32, may be the same;  rate finite;  1 <= E <= 256
+ */
+int moe_bias_update(int32_t E, const int32_t* d_counts, float rate, const float* d_bias, float* d_bias_out, void* stream);
+
+/* ---- The router's projection ----
+ * logits = x W in fp32 from hidden rows in either storage type, and its backward, with fp32 sums in a fixed order.  The products under
+ * them are exact where x is bf16, off by less than 2^-21 where both sides are fp32 (2^-24 on average), and by less than 2^-13 in dx in
+ * bf16, ahead of its rounding.  An infinity in x, W or dlogits gives NaN in the sums that it takes part in.
+ * 1 <= H <= 262144, 1 <= E <= 256.
+ *   d_x [T,H] dtype;  d_w [H,E] f32;  d_logits, d_dlogits [T,E] f32
+ *   d_workspace  >= moe_router_project_workspace_bytes(T, H, E)
+ */
+int moe_router_project_workspace_bytes(int32_t T, int32_t H, int32_t E, size_t* bytes);
+int moe_router_project(int32_t T, int32_t H, int32_t E, int dtype, const void* d_x, const float* d_w, float* d_logits,
+                       void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * dx = dres + dlogits W^T, dW = x^T dlogits
+ *   d_dres  [T,H] dtype, NULL: 0.  What reaches x beside the router (the layer's d_dx); may be d_dx
+ *   d_dx    [T,H] dtype, NULL: not computed (d_w may then be NULL); may be d_x.  d_dw [H,E] f32, NULL: not computed (d_x and
+ *           d_workspace may then be NULL); with T == 0 it is zeroed
+ */
+int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, const float* d_dlogits, const void* d_x,
+                                const float* d_w, const void* d_dres, void* d_dx, float* d_dw, void* d_workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* ---- Orthogonal updates ----
+ * For B matrices [M,N], one behind the other (the experts' weights), each by itself: X0 = u / (|u| + eps), |u| the Frobenius norm, and
+ * `steps` times
+ *   X <- a X + b (X X^T) X + c (X X^T)^2 X
+ * which leaves the singular vectors of u and takes every singular value s of X0 through a s + b s^3 + c s^5: close to 1 after five
+ * steps with the usual coefficients, unless it is a very small part of the whole.
+ * Products on the matrix cores with fp32 sums, their operands in bf16 storage rounded to 11 bits, in fp32 storage to 22.  A rounding's share
+ * grows by up to a per later step: of the result's norm, five steps leave about 2e-3 (bf16; its own rounding included) and 5e-6
+ * (fp32), where the singular values reach down to a hundredth of the largest.  A matrix of zeros stays zeros; one with a NaN or
+ * an infinity becomes NaN and touches no other.  Sums have a fixed order.
+ *   steps    1 .. 16;  eps > 0, finite
+ *   coefs    host, [steps][3] a, b, c, read before the call returns; NULL: 3.4445, -4.7750, 2.0315 in each.  MOE_ERR_INVALID_ARG
+ *            where they let singular values grow beyond 32 (from at most 1), or |a + b s^2 + c s^4| beyond 1024 on the way
+ *   d_workspace  >= moe_muon_workspace_bytes(B, M, N, dtype)
+ * Limits: 1 <= M, N <= 262144; the shorter side at most 32768, an fp16 matrix of M x N (sides rounded up to 64) below 4 GB.  B == 0 is
+ * a no-op.
+ */
+int moe_muon_workspace_bytes(int32_t B, int32_t M, int32_t N, int dtype, size_t* bytes);
+
+/* out = the result for u; d_u, d_out [B,M,N] dtype, may be the same. */
+int moe_orthogonalize(int32_t B, int32_t M, int32_t N, int dtype, const void* d_u, int32_t steps, const float* coefs, float eps,
+                      void* d_out, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A step of an optimiser with it (Muon):
+ *   m' = mu m + g;  u = nesterov ? g + mu m' : m';  o = the result for u;  w' = (1 - lr * weight_decay) w - lr * scale * o
+ *   d_g       [B,M,N] dtype: the gradient (moe_ffn_backward's d_dw_gate_up, d_dw_down)
+ *   d_m, d_m_out [B,M,N] f32, may be the same: momentum
+ *   d_w, d_w_out [B,M,N] dtype, may be the same: weights
+ *   d_master  [B,M,N] f32, NULL: none.  Weights in fp32, updated in place, of which d_w_out is then the rounded copy; d_w is not
+ *             read and may be NULL
+ *   mu, lr, weight_decay, scale finite; nesterov 0 or 1.  No other two arrays may overlap
+ */
+int moe_muon_step(int32_t B, int32_t M, int32_t N, int dtype, const void* d_g, const float* d_m, const void* d_w, float* d_master,
+                  float mu, int32_t nesterov, float lr, float weight_decay, float scale, int32_t steps, const float* coefs,
+                  float eps, float* d_m_out, void* d_w_out, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* ---- 4-bit experts (serving) ----
  * Weights as 4-bit floats (sign, 2 exponent bits, 1 mantissa bit: 0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives) with a
  * power-of-two scale per block of 32 consecutive k of one column, w = code * 2^(scale - 127) (the MXFP4 block format of the
@@ -428,6 +537,12 @@ int moe_quantize_w4(int32_t E_local, int32_t K, int32_t N, int dtype, const void
 int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_logits, const void* d_q_gate_up,
                        const void* d_s_gate_up, const void* d_q_down, const void* d_s_down, void* d_out,
                        const MoeSaved* saved, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* The same on routing results that moe_route or moe_route_scores left in `saved` and the workspace: moe_dispatch_to_combine with 4-bit
+ * experts.  saved may not be NULL. */
+int moe_dispatch_to_combine_w4(const MoeShape* shape, const void* d_x, const void* d_q_gate_up, const void* d_s_gate_up,
+                               const void* d_q_down, const void* d_s_down, void* d_out, const MoeSaved* saved,
+                               void* d_workspace, size_t workspace_bytes, void* stream);
 
 /* ---- SwiGLU + Add microbenchmark (paper Section 6: tile interleaving and L2 reuse, Section 6.1;
  *      static against dynamic scheduling, Section 6.2) ----

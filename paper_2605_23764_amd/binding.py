@@ -13,6 +13,7 @@ from typing import Optional
 import torch
 
 MOE_F32, MOE_BF16 = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 MODE_SERIALIZED, MODE_PERSISTENT = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -27,6 +28,10 @@ class MoeError(RuntimeError):
 
 class _MoeShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "H", "I", "E", "E_local", "expert_base", "k", "dtype")]
+
+
+class _MoeScores(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("score", "n_group", "topk_group", "renormalize")] + [("scale", ctypes.c_float)]
 
 
 class _MoeSaved(ctypes.Structure):
@@ -44,6 +49,9 @@ EXPORTS = (
     "moe_layer_norm_workspace_bytes", "moe_layer_norm_forward", "moe_layer_norm_backward", "moe_dropout_add_forward",
     "moe_dropout_add_backward", "moe_dropout_add_layer_norm_forward", "moe_dropout_add_layer_norm_backward",
     "moe_balance_workspace_bytes", "moe_balance_forward", "moe_router_backward", "moe_quantize_w4", "moe_ffn_forward_w4",
+    "moe_dispatch_to_combine_w4", "moe_route_scores", "moe_route_scores_backward", "moe_bias_update",
+    "moe_router_project_workspace_bytes", "moe_router_project", "moe_router_project_backward", "moe_muon_workspace_bytes",
+    "moe_orthogonalize", "moe_muon_step",
 )
 LAYOUT_WORDS = 25   # MOE_LAYOUT_WORDS
 
@@ -54,7 +62,10 @@ _BLOCK_ARGS = {
     "moe_dropout_add_forward": "iiippfppp", "moe_dropout_add_backward": "iiipfppp",
     "moe_dropout_add_layer_norm_forward": "iiippfpppf" "ppppp", "moe_dropout_add_layer_norm_backward": "iiipppppp" "fpppppp" "zp",
     "moe_balance_workspace_bytes": "iip", "moe_balance_forward": "iiipppf" "ppppzp", "moe_router_backward": "iiippppp" "fpppp",
-    "moe_quantize_w4": "iiiipppp", "moe_ffn_forward_w4": "ppppppppppzp",
+    "moe_quantize_w4": "iiiipppp", "moe_ffn_forward_w4": "ppppppppppzp", "moe_dispatch_to_combine_w4": "pppppppppzp",
+    "moe_route_scores": "ppppppzp", "moe_route_scores_backward": "iiipppppp" "p", "moe_bias_update": "ipfppp",
+    "moe_router_project_workspace_bytes": "iiip", "moe_router_project": "iiiippppzp", "moe_router_project_backward": "iiiippppppp" "zp",
+    "moe_muon_workspace_bytes": "iiiip", "moe_orthogonalize": "iiiipipfp" "pzp", "moe_muon_step": "iiiippppfifffipfpp" "pzp",
 }
 
 
@@ -532,3 +543,148 @@ def moe_ffn_forward_w4(shape, x, logits, q_gate_up, s_gate_up, q_down, s_down, o
     _check(load_library().moe_ffn_forward_w4(ctypes.addressof(shape), x, logits, q_gate_up, s_gate_up, q_down, s_down, out,
                                              ctypes.addressof(sv) if sv is not None else None, ws, wb, _raw_stream(stream)),
            "moe_ffn_forward_w4")
+
+
+def moe_dispatch_to_combine_w4(shape, x, q_gate_up, s_gate_up, q_down, s_down, out, saved: Saved, workspace, stream=None) -> None:
+    """moe_dispatch_to_combine with 4-bit experts, on the routing results in `saved` and the workspace."""
+    T, H, I, El, u8 = shape.T, shape.H, shape.I, shape.E_local, torch.uint8
+    sv = saved.c_struct()
+    x, out = _args((T, H), torch.bfloat16, "x out", x, out)
+    q_gate_up, = _args((El, H // 32, 2 * I, 16), u8, "q_gate_up", q_gate_up)
+    s_gate_up, = _args((El, H // 32, 2 * I), u8, "s_gate_up", s_gate_up)
+    q_down, = _args((El, I // 32, H, 16), u8, "q_down", q_down)
+    s_down, = _args((El, I // 32, H), u8, "s_down", s_down)
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_dispatch_to_combine_w4(ctypes.addressof(shape), x, q_gate_up, s_gate_up, q_down, s_down, out,
+                                                     ctypes.addressof(sv), ws, wb, _raw_stream(stream)), "moe_dispatch_to_combine_w4")
+
+
+# ---- routing by scores ----
+
+def make_scores(score="sigmoid", n_group: int = 1, topk_group: int = 1, renormalize: bool = True, scale: float = 1.0) -> _MoeScores:
+    """score: "sigmoid" or "softmax" (or SCORE_*)."""
+    if isinstance(score, str):
+        if score not in ("sigmoid", "softmax"):
+            raise ValueError(f"score: expected 'sigmoid' or 'softmax', got {score!r}")
+        score = SCORE_SIGMOID if score == "sigmoid" else SCORE_SOFTMAX
+    return _MoeScores(score, n_group, topk_group, int(renormalize), scale)
+
+
+def moe_route_scores(shape, scores, logits, bias, saved: Saved, workspace, stream=None) -> None:
+    """moe_route by scores: fills the routing results of `saved` and the workspace; bias [E] or None."""
+    sv = saved.c_struct()
+    logits, = _args((shape.T, shape.E), torch.float32, "logits", logits)
+    bias, = _args((shape.E,), torch.float32, "bias", bias)
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_route_scores(ctypes.addressof(shape), ctypes.addressof(scores), logits, bias, ctypes.addressof(sv), ws, wb,
+                                           _raw_stream(stream)), "moe_route_scores")
+
+
+def moe_route_scores_backward(scores, logits, topk_idx, dtopk_w, dadd, dlogits, stream=None) -> None:
+    """dlogits [T, E] from the routing weights' gradient, plus dadd [T, E] (or None)."""
+    T, E, k, _ = _router(logits, topk_idx, None)
+    f32 = torch.float32
+    logits, dadd, dlogits = _args((T, E), f32, "logits dadd dlogits", logits, dadd, dlogits)
+    topk_idx, = _args((T, k), torch.int32, "topk_idx", topk_idx)
+    dtopk_w, = _args((T, k), f32, "dtopk_w", dtopk_w)
+    _check(load_library().moe_route_scores_backward(T, E, k, ctypes.addressof(scores), logits, topk_idx, dtopk_w, dadd, dlogits,
+                                                    _raw_stream(stream)), "moe_route_scores_backward")
+
+
+def moe_bias_update(counts, rate: float, bias, bias_out, stream=None) -> None:
+    """bias_out = bias + rate * sign(mean - counts); counts [E] or moe_balance_forward's [E + 1] i32."""
+    E, = bias.shape
+    bias, bias_out = _args((E,), torch.float32, "bias bias_out", bias, bias_out)
+    counts, = _args((E + 1,) if counts.shape == (E + 1,) else (E,), torch.int32, "counts", counts)
+    _check(load_library().moe_bias_update(E, counts, rate, bias, bias_out, _raw_stream(stream)), "moe_bias_update")
+
+
+# ---- the router's projection ----
+
+def moe_router_project_workspace_bytes(T: int, H: int, E: int) -> int:
+    return _size("moe_router_project_workspace_bytes", T, H, E)
+
+
+def alloc_router_project_workspace(T: int, H: int, E: int, device="cuda") -> torch.Tensor:
+    return torch.empty(moe_router_project_workspace_bytes(T, H, E), dtype=torch.uint8, device=device)
+
+
+def _projection(w):
+    """H, E of the router's weights."""
+    if w.dim() != 2:
+        raise ValueError(f"w: expected an [H, E] tensor in float32, got {tuple(w.shape)}, {w.dtype}")
+    return w.shape
+
+
+def moe_router_project(x, w, logits, workspace, stream=None) -> None:
+    """logits [T, E] f32 = x [T, H] w [H, E] (f32)."""
+    shape, dt, code = _rows(x, "x")
+    T, H = shape
+    E = _projection(w)[1]
+    x, = _args(shape, dt, "x", x)
+    w, = _args((H, E), torch.float32, "w", w)
+    logits, = _args((T, E), torch.float32, "logits", logits)
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_router_project(T, H, E, code, x, w, logits, ws, wb, _raw_stream(stream)), "moe_router_project")
+
+
+def moe_router_project_backward(dlogits, x, w, dres, dx, dw, workspace, stream=None) -> None:
+    """dx = dres (or 0) + dlogits w^T, dw = x^T dlogits; dx or dw None: not computed (then w or x is not read, but gives the sizes)."""
+    shape, dt, code = _rows(x, "x")
+    T, H = shape
+    E = _projection(w)[1]
+    x, dres, dx = _args(shape, dt, "x dres dx", x, dres, dx)
+    w, dw = _args((H, E), torch.float32, "w dw", w, dw)
+    dlogits, = _args((T, E), torch.float32, "dlogits", dlogits)
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_router_project_backward(T, H, E, code, dlogits, x, w, dres, dx, dw, ws, wb, _raw_stream(stream)),
+           "moe_router_project_backward")
+
+
+# ---- orthogonal updates ----
+
+def moe_muon_workspace_bytes(B: int, M: int, N: int, dtype: torch.dtype) -> int:
+    return _size("moe_muon_workspace_bytes", B, M, N, _STORAGE[dtype])
+
+
+def alloc_muon_workspace(B: int, M: int, N: int, dtype: torch.dtype, device="cuda") -> torch.Tensor:
+    return torch.empty(moe_muon_workspace_bytes(B, M, N, dtype), dtype=torch.uint8, device=device)
+
+
+def _matrices(t: torch.Tensor, name: str):
+    """(shape, storage type, its MoeDtype) of a [B, M, N] tensor."""
+    if t.dim() != 3 or t.dtype not in _STORAGE:
+        raise ValueError(f"{name}: expected a [B, M, N] tensor in bfloat16 or float32, got {tuple(t.shape)}, {t.dtype}")
+    return t.shape, t.dtype, _STORAGE[t.dtype]
+
+
+def _coefficients(coefs, steps: int):
+    """[steps][3] floats for the call, or None."""
+    if coefs is None:
+        return None
+    flat = [float(v) for row in coefs for v in row]
+    if len(flat) != 3 * steps:
+        raise ValueError(f"coefs: expected {steps} rows of 3, got {len(flat)} values")
+    return (ctypes.c_float * len(flat))(*flat)
+
+
+def moe_orthogonalize(u, out, workspace, steps: int = 5, coefs=None, eps: float = 1e-7, stream=None) -> None:
+    """out [B, M, N] = u with its singular values taken through the steps' polynomials."""
+    shape, dt, code = _matrices(u, "u")
+    B, M, N = shape
+    u, out = _args(shape, dt, "u out", u, out)
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_orthogonalize(B, M, N, code, u, steps, _coefficients(coefs, steps), eps, out, ws, wb, _raw_stream(stream)),
+           "moe_orthogonalize")
+
+
+def moe_muon_step(g, m, w, m_out, w_out, workspace, lr: float, mu: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                  scale: float = 1.0, steps: int = 5, coefs=None, eps: float = 1e-7, master=None, stream=None) -> None:
+    """m_out = mu m + g; w_out = (1 - lr weight_decay) w - lr scale o; with master (f32, in place) instead of w, which may be None."""
+    shape, dt, code = _matrices(g, "g")
+    B, M, N = shape
+    g, w, w_out = _args(shape, dt, "g w w_out", g, w, w_out)
+    m, m_out, master = _args(shape, torch.float32, "m m_out master", m, m_out, master)
+    ws, wb = _workspace(workspace)
+    _check(load_library().moe_muon_step(B, M, N, code, g, m, w, master, mu, int(nesterov), lr, weight_decay, scale, steps,
+                                        _coefficients(coefs, steps), eps, m_out, w_out, ws, wb, _raw_stream(stream)), "moe_muon_step")

@@ -9,7 +9,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmoe_ffn.so")
 SOURCES = [os.path.join(HERE, "csrc", "moe_ffn.hip")]                                        # the layer
-BLOCK_SOURCES = [os.path.join(HERE, "csrc", n) for n in ("block_ops.hip", "experts_w4.hip")]   # the operators around it
+BLOCK_SOURCES = [os.path.join(HERE, "csrc", n) for n in ("block_ops.hip", "experts_w4.hip", "router_project.hip",
+                                                                 "updates.hip")]   # the operators around it
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -1,5 +1,5 @@
-// Host side of the operators around the layer (include/moe_ffn.h): layer norm, dropout with residual, balance loss and the router's
-// backward.  Argument checks and launches on the caller's stream; nothing here allocates or synchronises.
+// Host side of the operators around the layer (include/moe_ffn.h): layer norm, dropout with residual, balance loss, the router's
+// backward and that of the routing by scores with its bias.  Argument checks and launches on the caller's stream; nothing here allocates or synchronises.
 #include "../../include/moe_ffn.h"
 
 #include <math.h>
@@ -9,6 +9,8 @@
 #include "balance.h"
 #include "device_cus.h"
 #include "layer_norm.h"
+#include "scores_backward.h"
+#include "scores_check.h"
 
 using namespace moe;
 
@@ -338,6 +340,33 @@ int moe_router_backward(int32_t T, int32_t E, int32_t k, const float* d_logits, 
     if (p.topk_w) hipLaunchKernelGGL((router_backward_kernel<lanes.value, tail.value, true>), grid, dim3(kRouterThreads), 0, s, p);
     else hipLaunchKernelGGL((router_backward_kernel<lanes.value, tail.value, false>), grid, dim3(kRouterThreads), 0, s, p);
   });
+  return launched();
+}
+
+int moe_route_scores_backward(int32_t T, int32_t E, int32_t k, const MoeScores* scores, const float* d_logits, const int32_t* d_topk_idx,
+                              const float* d_dtopk_w, const float* d_dadd, float* d_dlogits, void* stream) {
+  int st = check_router(T, E, k);
+  if (st != MOE_OK || (st = check_scores(scores, E, k)) != MOE_OK) return st;
+  if (T == 0) return MOE_OK;
+  if (!good(d_logits) || !good(d_topk_idx) || !good(d_dtopk_w) || !aligned(d_dadd) || !good(d_dlogits)) return MOE_ERR_INVALID_ARG;
+  ScoresBackwardParams p{};
+  p.logits = d_logits; p.topk_idx = d_topk_idx; p.dtopk_w = d_dtopk_w; p.dadd = d_dadd; p.dlogits = d_dlogits;
+  p.sigmoid = scores->score == MOE_SCORE_SIGMOID; p.renorm = scores->renormalize; p.scale = scores->scale;
+  p.T = T; p.E = E; p.k = k;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  with_token_form(E, [&](auto lanes, auto tail) {
+    const int want = ceil_div(T, kRouterThreads / lanes.value);
+    const dim3 grid(want < 2048 ? want : 2048);
+    if (p.sigmoid) hipLaunchKernelGGL((scores_backward_kernel<lanes.value, tail.value, false>), grid, dim3(kRouterThreads), 0, s, p);
+    else hipLaunchKernelGGL((scores_backward_kernel<lanes.value, tail.value, true>), grid, dim3(kRouterThreads), 0, s, p);
+  });
+  return launched();
+}
+
+int moe_bias_update(int32_t E, const int32_t* d_counts, float rate, const float* d_bias, float* d_bias_out, void* stream) {
+  if (E < 1 || E > kMaxE) return MOE_ERR_UNSUPPORTED_SHAPE;
+  if (!isfinite(rate) || !good(d_counts) || !good(d_bias) || !good(d_bias_out)) return MOE_ERR_INVALID_ARG;
+  hipLaunchKernelGGL(bias_update_kernel, dim3(1), dim3(kMaxE), 0, static_cast<hipStream_t>(stream), d_counts, E, rate, d_bias, d_bias_out);
   return launched();
 }
 

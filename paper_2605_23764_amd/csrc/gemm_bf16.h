@@ -363,7 +363,14 @@ __device__ __forceinline__ void static_for(F&& f) {
 // launch 1320 -> 1250; T = 4096, H = 2048, I = 1408, 16 experts: forward 401 -> 386, backward 731 -> 705.  With the copies
 // masked through exec instead of repeated past the end: 10 % slower than the general loop.  Waves with fewer row blocks
 // keep the general loop: those launches wait for the weights (this slice: 0 to 2 % slower at 64..125 rows per expert).
-template <int LAY, int NX, int LOAD0, bool STREAM>
+// F16: the operands' 16 bits are fp16 (newton_schulz.h), the same loop otherwise.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma_16bit(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+template <int LAY, int NX, int LOAD0, bool STREAM, bool F16 = false>
 __device__ __forceinline__ void gemm_slice_full(f32x16 (&acc)[kMaxMT][4], const GemmFrags<LAY, kMaxMT>& cur, GemmFrags<LAY, kMaxMT>& nxt,
                                                 lds_cptr as_n, lds_cptr bs_n, int ks_n, const GemmTileCtx& t,
                                                 const GemmLoadGroup& g, const uint32_t (&b_off)[8], f32x16 (&accx)[4],
@@ -379,7 +386,7 @@ __device__ __forceinline__ void gemm_slice_full(f32x16 (&acc)[kMaxMT][4], const 
   for (int mt = 0; mt < NMT; ++mt) xf[mt] = cur.xf[mt];
   static_for<0, n_mfma>([&](auto jc) __attribute__((always_inline)) {
     constexpr int j = decltype(jc)::value;
-    if constexpr (j < NMT * 4) acc[j >> 2][j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf[j & 3], xf[j >> 2], acc[j >> 2][j & 3], 0, 0, 0);
+    if constexpr (j < NMT * 4) acc[j >> 2][j & 3] = mfma_16bit<F16>(wf[j & 3], xf[j >> 2], acc[j >> 2][j & 3]);
     else mfma_vgpr_acc(accx[j & 3], wf[j & 3], xblk);
     // actions: reads 0 .. n_reads - 1 with copy c behind read ceil((c + 1) * n_reads / 4) - 1
     static_for<0, n_act>([&](auto ac) __attribute__((always_inline)) {
@@ -423,10 +430,11 @@ __device__ __forceinline__ void gemm_slice_full(f32x16 (&acc)[kMaxMT][4], const 
 // lies inside ONE loop trip (a value carried around the loop may be copied by the compiler at the back
 // edge, which must only happen to retired values) and ends, right behind the barrier's wait, in a statement
 // that names the registers, so that the compiler can neither use nor copy them earlier.
-template <int LAY, int NMT, bool TALL, int NX = 0, bool STREAM = false>
+template <int LAY, int NMT, bool TALL, int NX = 0, bool STREAM = false, bool F16 = false>
 __device__ __forceinline__ void gemm_k_loop(f32x16 (&acc)[kMaxMT][4], f32x16 (&accx)[4], const GemmTileCtx& t, char* smem,
                                             int n_steps) {
   typedef TileShape<TALL> S;
+  static_assert(!F16 || (NX == 0 && NMT == kMaxMT && !TALL), "full wide tiles");
   static_assert(NX == 0 || (NMT == kMaxMT && !TALL), "the register-fed block extends a full wide tile");
   const lds_cptr lds = (lds_cptr)smem;
   if (n_steps <= 0) return;
@@ -482,15 +490,15 @@ __device__ __forceinline__ void gemm_k_loop(f32x16 (&acc)[kMaxMT][4], f32x16 (&a
       const lds_cptr bs = lds + S::kBReg + bs_i * S::kBStage;
       const int bs_next = bs_i == kBStages - 1 ? 0 : bs_i + 1;
       if (NX) load_x(xn, min(s + 1, n_steps - 1));
-      gemm_slice_full<LAY, NX, 4, STREAM>(acc, cur, nxt, as, bs, 1, t, g, b_off, accx, xb[0]);
-      gemm_slice_full<LAY, NX, 8, STREAM>(acc, nxt, cur, as, bs, 2, t, g, b_off, accx, xb[1]);
-      gemm_slice_full<LAY, NX, 12, STREAM>(acc, cur, nxt, as, bs, 3, t, g, b_off, accx, xb[2]);
+      gemm_slice_full<LAY, NX, 4, STREAM, F16>(acc, cur, nxt, as, bs, 1, t, g, b_off, accx, xb[0]);
+      gemm_slice_full<LAY, NX, 8, STREAM, F16>(acc, nxt, cur, as, bs, 2, t, g, b_off, accx, xb[1]);
+      gemm_slice_full<LAY, NX, 12, STREAM, F16>(acc, cur, nxt, as, bs, 3, t, g, b_off, accx, xb[2]);
       wait_lgkmcnt0();
       wait_vmcnt<S::kBLoads>();
       __builtin_amdgcn_s_barrier();
       if (NX) wait_xblock<S::kBLoads>(xn);   // see the general loop below
       g = gemm_load_group<LAY, TALL>(t, min(s + 2, n_steps - 1), s & 1, min(s + 3, n_steps - 1), s == n_steps - 2 && bs_i == 2 ? 1 : bs_i);
-      gemm_slice_full<LAY, NX, 0, STREAM>(acc, nxt, cur, as_n, lds + S::kBReg + bs_next * S::kBStage, 0, t, g, b_off, accx,
+      gemm_slice_full<LAY, NX, 0, STREAM, F16>(acc, nxt, cur, as_n, lds + S::kBReg + bs_next * S::kBStage, 0, t, g, b_off, accx,
                                   xb[3]);
       if (NX) {
 #pragma unroll

@@ -21,6 +21,7 @@
 #include "persistent.h"
 #include "probe.h"
 #include "route.h"
+#include "scores_check.h"
 #include "stream_layer.h"
 #include "wgrad_bf16.h"
 #include "wgrad_panel.h"
@@ -368,8 +369,9 @@ SchedParams<BF16> sched_params(const Ctx& c, const void* x, const float* logits,
 // Routing, one launch for up to 64 tokens, otherwise two: the router (top-k, softmax, a histogram per sub-chunk), then prefix sums +
 // M-tile map + stable ranks.  The second launch also zeroes the tile scheduler's counters and writes its task tables (one
 // workgroup, beside the rank workgroups), so that either launch mode can follow.
+// scores: by scores instead of the logits themselves (router_scores.h).
 template <bool BF16>
-int run_route_t(const Ctx& c, const float* logits, bool tables, void* zero_out, const void* copy_x) {
+int run_route_t(const Ctx& c, const float* logits, bool tables, void* zero_out, const void* copy_x, const ScoreParams* scores) {
   SchedParams<BF16> sp = sched_params<BF16>(c, copy_x, logits, nullptr, nullptr, nullptr);
   sp.skip_tables = tables ? 0 : 1;
   const RouteParams& rp = sp.route;
@@ -383,10 +385,15 @@ int run_route_t(const Ctx& c, const float* logits, bool tables, void* zero_out, 
     fill_wgs = (int)(want < (size_t)c.n_cu * 4 ? want : (size_t)c.n_cu * 4);
   }
   if (one) {
-    hipLaunchKernelGGL(route_one_kernel<BF16>, dim3(1 + fill_wgs), dim3(kRouteOneThreads), 0, c.stream, sp);
+    const dim3 grid(1 + fill_wgs), threads(kRouteOneThreads);
+    if (!scores) hipLaunchKernelGGL(route_one_kernel<BF16>, grid, threads, 0, c.stream, sp);
+    else if (scores->n_group > 1) hipLaunchKernelGGL((route_scores_one_kernel<BF16, true>), grid, threads, 0, c.stream, sp, *scores);
+    else hipLaunchKernelGGL((route_scores_one_kernel<BF16, false>), grid, threads, 0, c.stream, sp, *scores);
     return launch_status();
   }
-  hipLaunchKernelGGL(route_kernel, dim3(rp.n_sub), dim3(512), 0, c.stream, rp);
+  if (!scores) hipLaunchKernelGGL(route_kernel, dim3(rp.n_sub), dim3(512), 0, c.stream, rp);
+  else if (scores->n_group > 1) hipLaunchKernelGGL(route_scores_kernel<true>, dim3(rp.n_sub), dim3(512), 0, c.stream, rp, *scores);
+  else hipLaunchKernelGGL(route_scores_kernel<false>, dim3(rp.n_sub), dim3(512), 0, c.stream, rp, *scores);
   if (copy_x) {
     // tokens per workgroup: a workgroup per CU, as long as each has a token (then rp.subs is 1)
     int tokens = kSub;
@@ -403,9 +410,10 @@ int run_route_t(const Ctx& c, const float* logits, bool tables, void* zero_out, 
 // second launch, which is the launch's critical path, about as long again as the prefix sums and the tile map).
 // zero_out: the layer output, zeroed by further workgroups of the second launch (scatter epilogue follows).
 // copy_x: Dispatch in the second launch as well (more than kRouteOneT tokens, no tables, nothing to zero).
-int run_route(const Ctx& c, const float* logits, bool tables = true, void* zero_out = nullptr, const void* copy_x = nullptr) {
-  return c.s.dtype == MOE_BF16 ? run_route_t<true>(c, logits, tables, zero_out, copy_x)
-                               : run_route_t<false>(c, logits, tables, zero_out, copy_x);
+int run_route(const Ctx& c, const float* logits, bool tables = true, void* zero_out = nullptr, const void* copy_x = nullptr,
+              const ScoreParams* scores = nullptr) {
+  return c.s.dtype == MOE_BF16 ? run_route_t<true>(c, logits, tables, zero_out, copy_x, scores)
+                               : run_route_t<false>(c, logits, tables, zero_out, copy_x, scores);
 }
 
 // Dispatch to Combine of up to 64 tokens as ONE launch of weight streams (stream_layer.h), after run_route on the same MoeSaved.
@@ -814,6 +822,21 @@ int moe_route(const MoeShape* shape, const float* d_logits, const MoeSaved* save
   return run_route(c, d_logits);
 }
 
+int moe_route_scores(const MoeShape* shape, const MoeScores* scores, const float* d_logits, const float* d_bias, const MoeSaved* saved,
+                     void* d_workspace, size_t workspace_bytes, void* stream) {
+  Ctx c;
+  int st = check_shape(shape);
+  if (st != MOE_OK || (st = check_scores(scores, shape->E, shape->k)) != MOE_OK) return st;
+  st = make_ctx(c, shape, saved, d_workspace, workspace_bytes, stream);
+  if (st != MOE_OK || c.s.T == 0) return st;
+  if (!d_logits || !aligned16(d_logits) || !aligned16(d_bias) || !saved) return MOE_ERR_INVALID_ARG;
+  ScoreParams sc;
+  sc.bias = d_bias;
+  sc.sigmoid = scores->score == MOE_SCORE_SIGMOID; sc.renorm = scores->renormalize; sc.scale = scores->scale;
+  sc.n_group = scores->n_group; sc.topk_group = scores->topk_group; sc.per_group = c.s.E / scores->n_group;
+  return run_route(c, d_logits, true, nullptr, nullptr, &sc);
+}
+
 int moe_permute(const MoeShape* shape, const void* d_x, const MoeSaved* saved, void* d_workspace,
                 size_t workspace_bytes, void* stream) {
   Ctx c;
@@ -940,17 +963,18 @@ int moe_ffn_forward(const MoeShape* shape, const void* d_x, const float* d_logit
   return run_dispatch_to_combine(c, d_x, d_w_gate_up, d_w_down, d_out, mode, copies);
 }
 
-int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_logits, const void* d_q_gate_up,
-                       const void* d_s_gate_up, const void* d_q_down, const void* d_s_down, void* d_out, const MoeSaved* saved,
-                       void* d_workspace, size_t workspace_bytes, void* stream) {
+// The layer with 4-bit experts; routed: on routing results that are in `saved` already, without logits.
+static int run_forward_w4(bool routed, const MoeShape* shape, const void* d_x, const float* d_logits, const void* d_q_gate_up, const void* d_s_gate_up,
+                          const void* d_q_down, const void* d_s_down, void* d_out, const MoeSaved* saved, void* d_workspace,
+                          size_t workspace_bytes, void* stream) {
   Ctx c;
   int st = make_ctx(c, shape, saved, d_workspace, workspace_bytes, stream);
   if (st != MOE_OK) return st;
   if (c.s.dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
   if (c.s.T == 0) return MOE_OK;
-  const void* ptrs[] = {d_x, d_logits, d_q_gate_up, d_s_gate_up, d_q_down, d_s_down, d_out};
+  const void* ptrs[] = {d_x, routed ? static_cast<const void*>(saved) : d_logits, d_q_gate_up, d_s_gate_up, d_q_down, d_s_down, d_out};
   for (const void* q : ptrs)
-    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+    if (!q || (q != saved && !aligned16(q))) return MOE_ERR_INVALID_ARG;
   if ((double)c.s.H * c.s.I >= 2147483648.0) return MOE_ERR_UNSUPPORTED_SHAPE;   // an expert's blocks: 31-bit offsets
   // GEMM-2's rows in fp32, [R_max,H], over what the bf16 layer uses for Xp and half of A and Yp behind it; A follows.  (The three are
   // 2 R_max (2 H + I) bytes; rows of H fp32 are multiples of 256 bytes.)
@@ -974,7 +998,7 @@ int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_lo
       g->logits = d_logits; g->topk_idx = c.sv.topk_idx; g->topk_w = c.sv.topk_w; g->row_of = c.sv.row_of; g->meta = tile_map(c).meta;
     }
   } else {
-    if ((st = run_route(c, d_logits, false)) != MOE_OK) return st;
+    if (!routed && (st = run_route(c, d_logits, false)) != MOE_OK) return st;
     g1.offsets = g2.offsets = c.sv.offsets;
     g1.gather = c.sv.token_of;
     // Token rows are read through the permutation, except where experts have many of them, whose fetches then bound GEMM-1 (H = 2048,
@@ -989,6 +1013,20 @@ int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_lo
   if ((st = launch_experts_w4(g1, true, stream)) != MOE_OK) return st;
   if ((st = launch_experts_w4(g2, false, stream)) != MOE_OK) return st;
   return launch_combine_w4(y, c.sv.row_of, c.sv.topk_w, d_out, c.s.T, c.s.H, c.s.k, stream);
+}
+
+int moe_ffn_forward_w4(const MoeShape* shape, const void* d_x, const float* d_logits, const void* d_q_gate_up,
+                       const void* d_s_gate_up, const void* d_q_down, const void* d_s_down, void* d_out, const MoeSaved* saved,
+                       void* d_workspace, size_t workspace_bytes, void* stream) {
+  return run_forward_w4(false, shape, d_x, d_logits, d_q_gate_up, d_s_gate_up, d_q_down, d_s_down, d_out, saved, d_workspace,
+                        workspace_bytes, stream);
+}
+
+int moe_dispatch_to_combine_w4(const MoeShape* shape, const void* d_x, const void* d_q_gate_up, const void* d_s_gate_up,
+                               const void* d_q_down, const void* d_s_down, void* d_out, const MoeSaved* saved, void* d_workspace,
+                               size_t workspace_bytes, void* stream) {
+  return run_forward_w4(true, shape, d_x, nullptr, d_q_gate_up, d_s_gate_up, d_q_down, d_s_down, d_out, saved, d_workspace,
+                        workspace_bytes, stream);
 }
 
 int moe_ffn_backward(const MoeShape* shape, const void* d_dy, const void* d_x, const void* d_w_gate_up,

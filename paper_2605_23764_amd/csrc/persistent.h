@@ -66,6 +66,7 @@
 #include "gemm_f32.h"
 #include "permute_combine.h"
 #include "route.h"
+#include "router_scores.h"
 #include "wave_sync.h"
 
 namespace moe {
@@ -437,19 +438,37 @@ __global__ __launch_bounds__(kRankThreads) void sched_prepare_copy_kernel(SchedP
 }
 
 // Both routing launches as one, for few tokens (route_one): workgroup 0 routes, further ones only fill.
-template <bool BF16>
-__global__ __launch_bounds__(kRouteOneThreads) void route_one_kernel(SchedParams<BF16> sp) {
+template <bool BF16, typename SELECT>
+__device__ __forceinline__ void route_one_launch(const SchedParams<BF16>& sp, const SELECT& select) {
   if (blockIdx.x > 0) {
     const size_t stride = (size_t)(gridDim.x - 1) * blockDim.x;
     for (size_t i = (size_t)(blockIdx.x - 1) * blockDim.x + threadIdx.x; i < sp.zero_n16; i += stride)
       sp.zero_dst[i] = make_uint4(0, 0, 0, 0);
     return;
   }
-  route_one(sp.route);
+  route_one(sp.route, select);
   if (sp.skip_tables) return;
   __threadfence_block();
   __syncthreads();   // tile map (written by wave 0) complete before every wave reads it
   build_task_tables<BF16>(sp);
+}
+template <bool BF16>
+__global__ __launch_bounds__(kRouteOneThreads) void route_one_kernel(SchedParams<BF16> sp) {
+  route_one_launch(sp, SelectLogits{});
+}
+
+// The same two with routing by scores (router_scores.h).
+template <bool GROUPS>
+__global__ __launch_bounds__(512) void route_scores_kernel(RouteParams p, ScoreParams sc) {
+  __shared__ int32_t s_idx[kSub * kMaxK];
+  __shared__ float s_val[kSub * kMaxK];
+  __shared__ uint64_t s_keys[GROUPS ? 512 / kWave * kRouteTokensPerWave * kMaxE : 1];
+  route_chunk(p, blockIdx.x, s_idx, s_val, SelectScores<GROUPS>{sc, s_keys});
+}
+template <bool BF16, bool GROUPS>
+__global__ __launch_bounds__(kRouteOneThreads) void route_scores_one_kernel(SchedParams<BF16> sp, ScoreParams sc) {
+  __shared__ uint64_t s_keys[GROUPS ? kRouteOneT * kMaxE : 1];
+  route_one_launch(sp, SelectScores<GROUPS>{sc, s_keys});
 }
 
 // SCATTER (bf16): GEMM-2 tiles add their weighted rows into the zeroed layer output from their epilogue

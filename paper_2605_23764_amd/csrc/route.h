@@ -31,11 +31,21 @@ __device__ __forceinline__ void local_mask(const int32_t* idx, int k, int base, 
   }
 }
 
+// The selection of moe_route: top-k of the logits themselves.  (A selection is called with a wave's four tokens' keys as route_load
+// leaves them, and with the wave's kMaxK words per token for ids and values.)
+struct SelectLogits {
+  template <int KP>
+  __device__ __forceinline__ void operator()(const RouteParams& p, int t_first, int lane, uint32_t (&key)[KP], int32_t* s_idx, float* s_val) const {
+    route_select(p, t_first, lane, key, s_idx, s_val);
+  }
+};
+
 // One sub-chunk of kSub tokens by a workgroup (a wave routes four tokens per pass;
 // the logits of the next pass are fetched while the current one is selected), then
 // wave 0 (lane = token) builds the sub-chunk's histogram row with ballots.
 // s_idx, s_val: kSub*kMaxK words of LDS each.
-__device__ __forceinline__ void route_chunk(const RouteParams& p, int sub, int32_t* s_idx, float* s_val) {
+template <typename SELECT>
+__device__ __forceinline__ void route_chunk(const RouteParams& p, int sub, int32_t* s_idx, float* s_val, const SELECT& select) {
   const int lane = lane_id();
   const int wave = threadIdx.x / kWave;
   const int n_waves = blockDim.x / kWave;
@@ -49,7 +59,7 @@ __device__ __forceinline__ void route_chunk(const RouteParams& p, int sub, int32
     for (; i < kSub && t0 + i < p.T; i += step) {
       const bool more = i + step < kSub && t0 + i + step < p.T;
       if (more) route_load<KP>(p, t0 + i + step, lane, key_next);
-      route_select<KP>(p, t0 + i, lane, key, s_idx + i * kMaxK, s_val + i * kMaxK);
+      select(p, t0 + i, lane, key, s_idx + i * kMaxK, s_val + i * kMaxK);
 #pragma unroll
       for (int q = 0; q < KP; ++q) key[q] = key_next[q];
     }
@@ -332,7 +342,7 @@ __device__ __forceinline__ void scan_all(const RouteParams& p, int32_t* s_cnt, i
 __global__ __launch_bounds__(512) void route_kernel(RouteParams p) {
   __shared__ int32_t s_idx[kSub * kMaxK];
   __shared__ float s_val[kSub * kMaxK];
-  route_chunk(p, blockIdx.x, s_idx, s_val);
+  route_chunk(p, blockIdx.x, s_idx, s_val, SelectLogits{});
 }
 
 // The whole routing of up to 64 tokens by ONE workgroup of 16 waves, nothing but results in memory: a wave routes four tokens,
@@ -342,7 +352,8 @@ __global__ __launch_bounds__(512) void route_kernel(RouteParams p) {
 // experts, T = 1 38.9 -> 36.1 us, T = 64 66.7 -> 65.4; H = 256, I = 128, 256 experts, T = 32 28.2 -> 23.4, T = 64 29.2 -> 26.8.  The
 // line is one pass of the 16 waves: with a second one T = 128 lost 3..5 us (72 -> 75, 29.8 -> 34.4), T = 256 10..18.
 constexpr int kRouteOneT = kWave, kRouteOneThreads = kRouteOneT / kRouteTokensPerWave * kWave;
-__device__ __forceinline__ void route_one(const RouteParams& p) {
+template <typename SELECT>
+__device__ __forceinline__ void route_one(const RouteParams& p, const SELECT& select) {
   __shared__ int32_t s_idx[kRouteOneT * kMaxK];
   __shared__ float s_val[kRouteOneT * kMaxK];
   __shared__ unsigned long long s_mask[kMaxE];
@@ -355,7 +366,7 @@ __device__ __forceinline__ void route_one(const RouteParams& p) {
     with_route_keys(p.E, [&](auto kp) __attribute__((always_inline)) {
       uint32_t key[decltype(kp)::value];
       route_load(p, t0, lane, key);
-      route_select(p, t0, lane, key, s_idx + t0 * kMaxK, s_val + t0 * kMaxK);
+      select(p, t0, lane, key, s_idx + t0 * kMaxK, s_val + t0 * kMaxK);
     });
   __syncthreads();
   // the local expert of slot j of token `lane`, or -1

@@ -1,0 +1,130 @@
+// Host side of the router's projection (include/moe_ffn.h): argument checks and launches on the caller's stream.
+#include "../../include/moe_ffn.h"
+
+#include <algorithm>
+
+#include "router_project.h"
+
+using namespace moe;
+
+namespace {
+
+constexpr int kProjMaxE = 256;
+constexpr int kProjWorkgroups = 512;       // two per CU
+constexpr int kProjMaxSplits = 256;
+
+bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool good(const void* p) { return p && aligned(p); }
+int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
+int launched() { return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_LAUNCH; }
+
+int check(int T, int H, int E, int dtype) {
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
+  if (T < 0 || H < 1 || H > (1 << 18) || E < 1 || E > kProjMaxE) return MOE_ERR_UNSUPPORTED_SHAPE;
+  // a launch holds 2^32 work-items at most
+  if ((size_t)ceil_div(T, kProjTile) * ceil_div(std::max(H, E), kProjTile) >= ((size_t)1 << 24)) return MOE_ERR_UNSUPPORTED_SHAPE;
+  return MOE_OK;
+}
+
+// k's per workgroup and workgroups along k of a product of rows x cols over K.
+struct Split { int k, n; };
+Split split_of(int rows, int cols, int K) {
+  const long tiles = (long)ceil_div(rows, kProjTile) * ceil_div(cols, kProjTile);
+  const int want = (int)std::max<long>(1, std::min<long>(kProjMaxSplits, kProjWorkgroups / std::max<long>(tiles, 1)));
+  Split s;
+  s.k = ceil_div(ceil_div(K, want), kProjK) * kProjK;
+  s.n = ceil_div(K, s.k);
+  return s;
+}
+size_t part_bytes(const Split& s, int rows, int cols) { return s.n > 1 ? (size_t)s.n * rows * cols * 4 : 0; }
+
+template <typename TP, bool KCP, int NP, typename TQ, bool KCQ, int NQ>
+int run_sums(ProjParams p, float* out, void* ws, hipStream_t s) {
+  const Split sp = split_of(p.rows, p.cols, p.K);
+  p.k_split = sp.k;
+  p.splits = sp.n;
+  p.ti = ceil_div(p.rows, kProjTile);
+  p.tj = ceil_div(p.cols, kProjTile);
+  p.part = sp.n > 1 ? static_cast<float*>(ws) : out;
+  hipLaunchKernelGGL((project_kernel<TP, KCP, NP, TQ, KCQ, NQ, void>), dim3((unsigned)p.ti * p.tj * p.splits), dim3(kProjThreads), 0, s, p);
+  if (sp.n > 1) {
+    const size_t n = (size_t)p.rows * p.cols;
+    hipLaunchKernelGGL(project_join_kernel, dim3((unsigned)((n + kWave - 1) / kWave)), dim3(256), 0, s, p.part, sp.n, n, out);
+  }
+  return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_router_project_workspace_bytes(int32_t T, int32_t H, int32_t E, size_t* bytes) {
+  const int st = check(T, H, E, MOE_F32);
+  if (st != MOE_OK) return st;
+  if (!bytes) return MOE_ERR_INVALID_ARG;
+  *bytes = T == 0 ? 16 : std::max<size_t>(16, std::max(part_bytes(split_of(T, E, H), T, E), part_bytes(split_of(H, E, T), H, E)));
+  return MOE_OK;
+}
+
+int moe_router_project(int32_t T, int32_t H, int32_t E, int dtype, const void* d_x, const float* d_w, float* d_logits, void* d_workspace,
+                       size_t workspace_bytes, void* stream) {
+  const int st = check(T, H, E, dtype);
+  if (st != MOE_OK || T == 0) return st;
+  if (!good(d_x) || !good(d_w) || !good(d_logits) || !good(d_workspace)) return MOE_ERR_INVALID_ARG;
+  size_t need = 0;
+  moe_router_project_workspace_bytes(T, H, E, &need);
+  if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  ProjParams p{};
+  p.P = d_x; p.Q = d_w;
+  p.ld_p = H; p.ld_q = E;
+  p.rows = T; p.cols = E; p.K = H;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return dtype == MOE_BF16 ? run_sums<__bf16, true, 1, float, false, 3>(p, d_logits, d_workspace, s)
+                           : run_sums<float, true, 3, float, false, 3>(p, d_logits, d_workspace, s);
+}
+
+int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, const float* d_dlogits, const void* d_x, const float* d_w,
+                                const void* d_dres, void* d_dx, float* d_dw, void* d_workspace, size_t workspace_bytes, void* stream) {
+  int st = check(T, H, E, dtype);
+  if (st != MOE_OK) return st;
+  if (!aligned(d_dx) || !aligned(d_dw) || !aligned(d_dres)) return MOE_ERR_INVALID_ARG;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (T == 0) {
+    if (!d_dw) return MOE_OK;
+    const size_t n = (size_t)H * E;        // sums over nothing
+    hipLaunchKernelGGL(project_join_kernel, dim3((unsigned)((n + kWave - 1) / kWave)), dim3(256), 0, s, (const float*)nullptr, 0, n, d_dw);
+    return launched();
+  }
+  if (!good(d_dlogits) || (d_dx && !good(d_w)) || (d_dw && !good(d_x))) return MOE_ERR_INVALID_ARG;
+  if (d_dw) {
+    size_t need = 0;
+    moe_router_project_workspace_bytes(T, H, E, &need);
+    if (!good(d_workspace)) return MOE_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
+    ProjParams p{};                        // ahead of dx, which may be x
+    p.P = d_x; p.Q = d_dlogits;
+    p.ld_p = H; p.ld_q = E;
+    p.rows = H; p.cols = E; p.K = T;
+    st = dtype == MOE_BF16 ? run_sums<__bf16, false, 1, float, false, 3>(p, d_dw, d_workspace, s)
+                           : run_sums<float, false, 3, float, false, 3>(p, d_dw, d_workspace, s);
+    if (st != MOE_OK) return st;
+  }
+  if (d_dx) {
+    ProjParams p{};
+    p.P = d_dlogits; p.Q = d_w;
+    p.ld_p = p.ld_q = E;
+    p.rows = T; p.cols = H; p.K = E;
+    p.k_split = ceil_div(E, kProjK) * kProjK;
+    p.splits = 1;
+    p.ti = ceil_div(T, kProjTile);
+    p.tj = ceil_div(H, kProjTile);
+    p.add = d_dres; p.out = d_dx;
+    const dim3 grid((unsigned)((size_t)p.ti * p.tj));
+    if (dtype == MOE_BF16) hipLaunchKernelGGL((project_kernel<float, true, 2, float, true, 2, __bf16>), grid, dim3(kProjThreads), 0, s, p);
+    else hipLaunchKernelGGL((project_kernel<float, true, 3, float, true, 3, float>), grid, dim3(kProjThreads), 0, s, p);
+    st = launched();
+  }
+  return st;
+}
+
+}  // extern "C"

@@ -1,0 +1,282 @@
+// Host side of the orthogonal updates (include/moe_ffn.h): argument checks, the scales of the matrices in between, launches on the
+// caller's stream.  Nothing here allocates or synchronises.
+#include "../../include/moe_ffn.h"
+
+#include <math.h>
+
+#include <algorithm>
+
+#include "device_cus.h"
+#include "newton_schulz.h"
+
+using namespace moe;
+
+namespace {
+
+constexpr int kMaxSteps = 16;
+// Matrices are worked on in groups whose workspace stays below this, one at least: enough tiles at a time for the whole chip.
+constexpr size_t kNsGroupBytes = (size_t)4 << 30;
+
+bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool good(const void* p) { return p && aligned(p); }
+int pad(int v) { return (v + kNsPad - 1) / kNsPad * kNsPad; }
+size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
+
+int check_matrices(int B, int M, int N, int dtype) {
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
+  if (B < 0 || M < 1 || N < 1 || M > (1 << 18) || N > (1 << 18)) return MOE_ERR_UNSUPPORTED_SHAPE;
+  const double s = pad(std::min(M, N)), l = pad(std::max(M, N));
+  if (s * l * 2 >= 4294967296.0 || s > (1 << 15)) return MOE_ERR_UNSUPPORTED_SHAPE;   // 32-bit offsets inside a matrix
+  if ((double)B * M * N * 4 > 9.0e18) return MOE_ERR_UNSUPPORTED_SHAPE;
+  return MOE_OK;
+}
+
+// Matrices of a group, and a group's workspace.
+struct Plan {
+  int B, M, N, Sp, Lp, group, halves;
+  size_t x_bytes, a_bytes;                 // of one matrix
+  size_t x, a, part, total;                // X and its transpose, twice; A and B; per half
+};
+Plan make_plan(int B, int M, int N, int dtype) {
+  Plan p{};
+  p.B = B; p.M = M; p.N = N;
+  p.Sp = pad(std::min(M, N));
+  p.Lp = pad(std::max(M, N));
+  p.halves = dtype == MOE_F32 ? 2 : 1;
+  p.x_bytes = (size_t)p.Sp * p.Lp * 2;
+  p.a_bytes = (size_t)p.Sp * p.Sp * 2;
+  const size_t per = p.halves * (4 * p.x_bytes + 2 * p.a_bytes) + kNsMaxParts * 8;
+  const int most = (int)std::min<size_t>(std::max<size_t>(kNsGroupBytes / per, 1), 1 << 14);
+  const int groups = std::max(1, (B + most - 1) / most);
+  p.group = std::max(1, (B + groups - 1) / groups);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+  p.x = take(p.halves * 4 * p.x_bytes * p.group);
+  p.a = take(p.halves * 2 * p.a_bytes * p.group);
+  p.part = take((size_t)kNsMaxParts * 8 * p.group);
+  p.total = off;
+  return p;
+}
+
+// Coefficients of each step and the scales that follow from how large singular values can become.
+struct Steps {
+  int n;
+  float c[kMaxSteps][3];
+  int ex, ea[kMaxSteps], eb[kMaxSteps];    // stored: X 2^ex, A 2^ea, B 2^eb
+};
+int floor_log2(double v) { return (int)floor(log2(v)); }
+// false: the coefficients let singular values grow out of bounds
+bool make_steps(Steps& s, int n, const float* coefs, int S, int L) {
+  static const float usual[3] = {3.4445f, -4.7750f, 2.0315f};
+  s.n = n;
+  s.ex = floor_log2((double)L) / 2;
+  double top = 1.0;                        // largest singular value possible
+  for (int i = 0; i < n; ++i) {
+    for (int j = 0; j < 3; ++j) {
+      s.c[i][j] = coefs ? coefs[3 * i + j] : usual[j];
+      if (!isfinite(s.c[i][j])) return false;
+    }
+    const double a = s.c[i][0], b = s.c[i][1], c = s.c[i][2];
+    const double t = top * top;            // of A: its eigenvalues lie in [0, t], those of B are q there
+    auto q = [&](double v) { return fabs(a + b * v + c * v * v); };
+    double qmax = std::max(q(0.0), q(t));
+    if (c != 0.0 && -b / (2 * c) > 0.0 && -b / (2 * c) < t) qmax = std::max(qmax, q(-b / (2 * c)));
+    auto p = [&](double v) { return v > 0.0 && v < t ? sqrt(v) * q(v) : 0.0; };   // p(s) = s q(s^2), at v = s^2
+    double pmax = top * q(t);
+    if (c != 0.0) {                        // p'(s) = a + 3 b v + 5 c v^2
+      const double d = 9 * b * b - 20 * a * c;
+      if (d >= 0.0) pmax = std::max(pmax, std::max(p((-3 * b + sqrt(d)) / (10 * c)), p((-3 * b - sqrt(d)) / (10 * c))));
+    } else if (b != 0.0) {
+      pmax = std::max(pmax, p(-a / (3 * b)));
+    }
+    // entries are at most the largest singular value; 2^15 leaves a factor of two for roundings
+    s.ea[i] = std::min(floor_log2(S), 15 - (int)ceil(log2(t)));
+    s.eb[i] = std::min(floor_log2(S), 15 - (int)ceil(log2(std::max(qmax, 1e-6))));
+    top = std::max(pmax, 1e-3) * 1.0001;
+    if (!(qmax <= 1024.0) || !(top <= 32.0)) return false;
+  }
+  return true;
+}
+
+struct Update {
+  const void* g;
+  const float* m;
+  float* m_out;
+  const void* w;
+  float* master;
+  void* out;
+  float mu, w_keep, w_step, eps;
+  int nesterov;
+};
+
+template <typename T> int run_update(const Plan& L, const Steps& st, const Update& u, char* ws, hipStream_t stream) {
+  constexpr bool SPLIT = sizeof(T) == 4;
+  const bool wide = L.M <= L.N;
+  const int cus = (device_cus() + 7) / 8 * 8;
+  for (int e0 = 0; e0 < L.B; e0 += L.group) {
+    const int n = std::min(L.group, L.B - e0);
+    const size_t first = (size_t)e0 * L.M * L.N;
+    // arrays of the group: X short x long and long x short, two of each; A; B; the halves' arrays behind each other
+    auto x_of = [&](int which) {
+      NsMat m;
+      m.hi = ws + L.x + (size_t)which * L.group * L.x_bytes * L.halves;
+      m.lo = SPLIT ? m.hi + (size_t)L.group * L.x_bytes : nullptr;
+      return m;
+    };
+    auto a_of = [&](int which) {
+      NsMat m;
+      m.hi = ws + L.a + (size_t)which * L.group * L.a_bytes * L.halves;
+      m.lo = SPLIT ? m.hi + (size_t)L.group * L.a_bytes : nullptr;
+      return m;
+    };
+    NsMat xs = x_of(0), xl = x_of(1), xs_next = x_of(2), xl_next = x_of(3);
+    const NsMat A = a_of(0), Bm = a_of(1);
+
+    NsPrepParams q{};
+    q.g = static_cast<const T*>(u.g) + first;
+    q.m = u.m ? u.m + first : nullptr;
+    q.m_out = u.m_out ? u.m_out + first : nullptr;
+    q.mu = u.mu; q.nesterov = u.nesterov;
+    q.part = reinterpret_cast<double*>(ws + L.part);
+    q.parts = (int)std::min<size_t>(kNsMaxParts, ((size_t)L.M * L.N + 2047) / 2048);
+    q.scale = ldexpf(1.f, st.ex);
+    q.eps = u.eps;
+    q.X = wide ? xs : xl;
+    q.XT = wide ? xl : xs;
+    q.stride = (long)L.x_bytes;
+    q.M = L.M; q.N = L.N; q.Mp = wide ? L.Sp : L.Lp; q.Np = wide ? L.Lp : L.Sp; q.n = n;
+    hipLaunchKernelGGL(ns_norm_kernel<T>, dim3((unsigned)(n * q.parts)), dim3(256), 0, stream, q);
+    hipLaunchKernelGGL((ns_first_kernel<T, SPLIT>), dim3((unsigned)n * (q.Mp / 64) * (q.Np / 64)), dim3(256), 0, stream, q);
+
+    for (int i = 0; i < st.n; ++i) {
+      NsGemmParams p{};
+      p.n = n;
+      p.rows = p.cols = L.Sp;
+      p.ld_c = p.ld_ct = L.Sp;
+      p.c_stride = p.a_stride = (long)L.a_bytes;
+      // A = X X^T
+      p.P = p.Q = xs; p.C = p.CT = A;
+      p.p_stride = p.q_stride = (long)L.x_bytes;
+      p.K = L.Lp;
+      p.s_acc = ldexpf(1.f, st.ea[i] - 2 * st.ex);
+      const int sym = ((L.Sp + kBM - 1) / kBM) * ((L.Sp + kBM - 1) / kBM + 1) / 2;
+      const int all = ((L.Sp + kBM - 1) / kBM) * ((L.Lp + kBM - 1) / kBM);
+      auto grid = [&](long tiles) { return dim3((unsigned)std::min<long>((tiles * n + 7) / 8 * 8, cus)); };
+      hipLaunchKernelGGL((ns_gemm_kernel<kNsGram, SPLIT, T>), grid(sym), dim3(kGemmThreads), 0, stream, p);
+      // B = a I + b A + c A^2
+      p.P = p.Q = p.A = A; p.C = p.CT = Bm;
+      p.p_stride = p.q_stride = (long)L.a_bytes;
+      p.K = L.Sp;
+      p.s_acc = ldexpf(st.c[i][2], st.eb[i] - 2 * st.ea[i]);
+      p.s_a = ldexpf(st.c[i][1], st.eb[i] - st.ea[i]);
+      p.diag = ldexpf(st.c[i][0], st.eb[i]);
+      hipLaunchKernelGGL((ns_gemm_kernel<kNsPoly, SPLIT, T>), grid(sym), dim3(kGemmThreads), 0, stream, p);
+      p.A = NsMat{};
+      if (i + 1 < st.n) {
+        // X <- B X, and its transpose
+        p.P = Bm; p.Q = xl; p.C = xs_next; p.CT = xl_next;
+        p.q_stride = p.c_stride = (long)L.x_bytes;
+        p.cols = L.Lp;
+        p.ld_c = L.Lp; p.ld_ct = L.Sp;
+        p.s_acc = ldexpf(1.f, -st.eb[i]);
+        hipLaunchKernelGGL((ns_gemm_kernel<kNsNext, SPLIT, T>), grid(all), dim3(kGemmThreads), 0, stream, p);
+        std::swap(xs, xs_next);
+        std::swap(xl, xl_next);
+      } else {
+        // the caller's side up: M x N
+        p.P = wide ? Bm : xl; p.Q = wide ? xl : Bm;
+        p.p_stride = wide ? (long)L.a_bytes : (long)L.x_bytes;
+        p.q_stride = wide ? (long)L.x_bytes : (long)L.a_bytes;
+        p.rows = wide ? L.Sp : L.Lp; p.cols = wide ? L.Lp : L.Sp;
+        p.s_acc = ldexpf(1.f, -st.eb[i] - st.ex);
+        p.w = u.w ? static_cast<const T*>(u.w) + first : nullptr;
+        p.master = u.master ? u.master + first : nullptr;
+        p.out = static_cast<T*>(u.out) + first;
+        p.w_keep = u.w_keep; p.w_step = u.w_step;
+        p.M = L.M; p.N = L.N;
+        hipLaunchKernelGGL((ns_gemm_kernel<kNsOut, SPLIT, T>), grid(all), dim3(kGemmThreads), 0, stream, p);
+      }
+    }
+    if (hipGetLastError() != hipSuccess) return MOE_ERR_LAUNCH;
+  }
+  return MOE_OK;
+}
+
+int check_call(const Plan& L, void* ws, size_t ws_bytes) {
+  if (!good(ws)) return MOE_ERR_INVALID_ARG;
+  return ws_bytes < L.total ? MOE_ERR_WORKSPACE_TOO_SMALL : MOE_OK;
+}
+
+int run(const Plan& L, int dtype, const Steps& st, const Update& u, void* ws, void* stream) {
+  char* w = static_cast<char*>(ws);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return dtype == MOE_BF16 ? run_update<__bf16>(L, st, u, w, s) : run_update<float>(L, st, u, w, s);
+}
+
+// Whether arrays of a and b bytes share any.
+bool overlap(const void* x, size_t a, const void* y, size_t b) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(x), q = reinterpret_cast<uintptr_t>(y);
+  return x && y && p < q + b && q < p + a;
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_muon_workspace_bytes(int32_t B, int32_t M, int32_t N, int dtype, size_t* bytes) {
+  const int st = check_matrices(B, M, N, dtype);
+  if (st != MOE_OK) return st;
+  if (!bytes) return MOE_ERR_INVALID_ARG;
+  *bytes = make_plan(B, M, N, dtype).total;
+  return MOE_OK;
+}
+
+int moe_orthogonalize(int32_t B, int32_t M, int32_t N, int dtype, const void* d_u, int32_t steps, const float* coefs, float eps,
+                      void* d_out, void* d_workspace, size_t workspace_bytes, void* stream) {
+  int st = check_matrices(B, M, N, dtype);
+  if (st != MOE_OK) return st;
+  Steps s;
+  if (steps < 1 || steps > kMaxSteps || !(eps > 0.f) || isinf(eps) || !make_steps(s, steps, coefs, std::min(M, N), std::max(M, N)))
+    return MOE_ERR_INVALID_ARG;
+  if (B == 0) return MOE_OK;
+  if (!good(d_u) || !good(d_out)) return MOE_ERR_INVALID_ARG;
+  const size_t bytes = (size_t)B * M * N * (dtype == MOE_BF16 ? 2 : 4);
+  if (d_out != d_u && overlap(d_out, bytes, d_u, bytes)) return MOE_ERR_INVALID_ARG;
+  const Plan L = make_plan(B, M, N, dtype);
+  if ((st = check_call(L, d_workspace, workspace_bytes)) != MOE_OK) return st;
+  Update u{};
+  u.g = d_u; u.out = d_out; u.eps = eps;
+  return run(L, dtype, s, u, d_workspace, stream);
+}
+
+int moe_muon_step(int32_t B, int32_t M, int32_t N, int dtype, const void* d_g, const float* d_m, const void* d_w, float* d_master,
+                  float mu, int32_t nesterov, float lr, float weight_decay, float scale, int32_t steps, const float* coefs, float eps,
+                  float* d_m_out, void* d_w_out, void* d_workspace, size_t workspace_bytes, void* stream) {
+  int st = check_matrices(B, M, N, dtype);
+  if (st != MOE_OK) return st;
+  Steps s;
+  if (steps < 1 || steps > kMaxSteps || !(eps > 0.f) || isinf(eps) || !make_steps(s, steps, coefs, std::min(M, N), std::max(M, N)))
+    return MOE_ERR_INVALID_ARG;
+  if (!isfinite(mu) || !isfinite(lr) || !isfinite(weight_decay) || !isfinite(scale) || (nesterov != 0 && nesterov != 1))
+    return MOE_ERR_INVALID_ARG;
+  if (B == 0) return MOE_OK;
+  if (!good(d_g) || !good(d_m) || !good(d_m_out) || !good(d_w_out) || !aligned(d_master) || !aligned(d_w) || (!d_w && !d_master))
+    return MOE_ERR_INVALID_ARG;
+  const Plan L = make_plan(B, M, N, dtype);
+  if ((st = check_call(L, d_workspace, workspace_bytes)) != MOE_OK) return st;
+  const size_t n = (size_t)B * M * N, nw = n * (dtype == MOE_BF16 ? 2 : 4);
+  // in place or apart: a group's outputs are written before the next group's inputs are read
+  if ((d_m_out != d_m && overlap(d_m_out, n * 4, d_m, n * 4)) || overlap(d_m_out, n * 4, d_g, nw) || overlap(d_m_out, n * 4, d_w_out, nw) ||
+      overlap(d_m_out, n * 4, d_w, nw) || overlap(d_m_out, n * 4, d_master, n * 4) || overlap(d_w_out, nw, d_master, n * 4) ||
+      (d_w_out != d_w && !d_master && overlap(d_w_out, nw, d_w, nw)) || overlap(d_w_out, nw, d_g, nw) || overlap(d_w_out, nw, d_m, n * 4) ||
+      overlap(d_master, n * 4, d_g, nw) || overlap(d_master, n * 4, d_m, n * 4))
+    return MOE_ERR_INVALID_ARG;
+  Update u{};
+  u.g = d_g; u.m = d_m; u.m_out = d_m_out; u.w = d_w; u.master = d_master; u.out = d_w_out;
+  u.mu = mu; u.nesterov = nesterov; u.eps = eps;
+  u.w_keep = (float)(1.0 - (double)lr * weight_decay);
+  u.w_step = (float)((double)lr * scale);
+  return run(L, dtype, s, u, d_workspace, stream);
+}
+
+}  // extern "C"
