@@ -17,6 +17,7 @@
 // fp32 storage: operands are pairs of fp16 (hi, and the rest times 2^11), products hi hi + hi lo + lo hi, so 22 bits.
 #pragma once
 #include "gemm_bf16.h"
+#include "rows.h"
 
 namespace moe {
 
@@ -24,20 +25,20 @@ constexpr float kNsLoScale = 2048.0f;      // what the second half of a pair is 
 constexpr int kNsMaxParts = 256;           // partial sums of squares per matrix
 constexpr int kNsPad = 64;
 
-struct NsMat {                             // fp16 [rows][ld] of each matrix
-  char* hi;
-  char* lo;                                // null: single
-};
-
 enum NsEpilogue { kNsGram = 0, kNsPoly = 1, kNsNext = 2, kNsOut = 3 };
 
+// Matrices in between: fp16 [rows][k]; as pairs [rows][k / 32][hi 32 | lo 32], so that a line of 128 bytes has both.
 struct NsGemmParams {
-  NsMat P, Q, C, CT;                       // C straight, CT transposed (gram, poly: the same array)
-  NsMat A;                                 // poly: the matrix that b is for
-  long p_stride, q_stride, c_stride, a_stride;   // bytes between matrices (of CT: c_stride as well)
+  const char *P, *Q;                       // C[i,j] = sum over k of P[i,k] Q[j,k]
+  char *C, *CT;                            // straight and transposed (gram, poly: the same array)
+  const char* A;                           // poly: the matrix that b is for
+  long p_stride, q_stride, c_stride, a_stride;   // bytes between matrices (of CT: c_stride)
   int rows, cols, K;                       // multiples of 64
-  int ld_c, ld_ct;
+  int ld_c, ld_ct;                         // elements
   int n;                                   // matrices
+  int first, tiles;                        // those of all tiles that this launch does
+  float* part;                             // sums along a share of k: [tile of the launch][splits][128 x 128 in the waves' order]
+  int splits;
   float s_acc, s_a, diag;                  // result = s_acc * sum + s_a * A + diag * I
   // out: o = s_acc * sum, M x N of them, weights w [M,N]
   const void* w;                           // null: out = o
@@ -47,92 +48,195 @@ struct NsGemmParams {
   int M, N;
 };
 
-// Values of four columns of this lane's row, fp16.
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char* lds_ptr;
+typedef __attribute__((address_space(3))) u32x2* lds_u32x2_ptr;
+typedef __attribute__((address_space(3))) u32x4* lds_u32x4_ptr;
+typedef __attribute__((address_space(3))) f32x4* lds_f32x4_ptr;
+
 __device__ __forceinline__ u32x2 pack_f16x4(const float (&v)[4]) {
-  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
   return __builtin_bit_cast(u32x2, (f16x4){(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]});
 }
 __device__ __forceinline__ void unpack_f16x4(u32x2 p, float (&v)[4]) {
-  typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
   const f16x4 h = __builtin_bit_cast(f16x4, p);
 #pragma unroll
   for (int x = 0; x < 4; ++x) v[x] = (float)h[x];
 }
-
-// A block of 32 rows x 128 columns through the wave's LDS region: rows to C, 256 bytes of each; columns to CT, 64 bytes of each, by
-// transposing reads.  Either may be null.
-__device__ __forceinline__ void ns_store_block(char* region, const u32x2 (&pk)[4][4], char* C, int ld_c, char* CT, int ld_ct, int cols_valid) {
-  typedef __attribute__((address_space(3))) char* lds_ptr;
-  typedef __attribute__((address_space(3))) u32x2* lds_u32x2_ptr;
-  typedef __attribute__((address_space(3))) const u32x4* lds_u32x4_cptr;
-  int lane = lane_id();
-  asm volatile("" : "+v"(lane));
-  const int l32 = lane & 31, lh = lane >> 5;
-  const lds_ptr base = (lds_ptr)region;
-#pragma unroll
-  for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) *(lds_u32x2_ptr)(base + l32 * kEpiRowBytes + (nt * 32 + q * 8 + lh * 4) * 2) = pk[nt][q];
+__device__ __forceinline__ void lds_settled() {            // a wave's own LDS accesses, which complete in order
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  if (C) {
-    const int r4 = lane >> 4, ch = lane & 15;
-    u32x4 v[8];
-#pragma unroll
-    for (int it = 0; it < 8; ++it) v[it] = *(lds_u32x4_cptr)(base + (it * 4 + r4) * kEpiRowBytes + ch * 16);
-    char* dst = C + ((size_t)r4 * ld_c + ch * 8) * 2;
-    if (ch * 8 < cols_valid)
-#pragma unroll
-      for (int it = 0; it < 8; ++it) *reinterpret_cast<u32x4*>(dst + (size_t)(it * 4) * ld_c * 2) = v[it];
-  }
-  if (CT) {
-    // 16 lanes read 4 rows x 16 columns and get a column's 4 rows each; lane (g, i): rows 8 g .. 8 g + 7 of column i
-    const int g = lane >> 4, i = lane & 15;
-    const lds_ptr at = base + (8 * g + (i >> 2)) * kEpiRowBytes + (i & 3) * 8;
-    u32x4 v[8];
-#pragma unroll
-    for (int cg = 0; cg < 8; ++cg) {
-      const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + cg * 32)));
-      const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + cg * 32 + 4 * kEpiRowBytes)));
-      v[cg] = u32x4{a.x, a.y, b.x, b.y};
-    }
-    char* dst = CT + ((size_t)i * ld_ct + 8 * g) * 2;
-#pragma unroll
-    for (int cg = 0; cg < 8; ++cg)
-      if (cg * 16 < cols_valid) *reinterpret_cast<u32x4*>(dst + (size_t)(cg * 16) * ld_ct * 2) = v[cg];
-  }
-  wait_lgkmcnt0();                         // see store_block_via_lds
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
 }
 
-// Weights of four columns n .. n + 3 of row m from the update o.  T: storage.
-template <typename T> __device__ __forceinline__ void ns_store_out(const NsGemmParams& p, int e, int m, int n, const float (&o)[4]) {
-  const size_t at = ((size_t)e * p.M + m) * p.N + n;
-#pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    if (n + x >= p.N) break;
-    float v = o[x];
+// Four columns n .. n + 3 of row m of the result: weights, or the update itself.  VEC: all four are there, and aligned.
+template <typename T, bool VEC> __device__ __forceinline__ void ns_put(const NsGemmParams& p, size_t at, int n, f32x4 o) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  if constexpr (VEC) {
     if (p.master) {
-      v = p.w_keep * p.master[at + x] - p.w_step * v;
-      p.master[at + x] = v;
+      const f32x4 w = *reinterpret_cast<const f32x4*>(p.master + at);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x] = p.w_keep * w[x] - p.w_step * o[x];
+      *reinterpret_cast<f32x4*>(p.master + at) = o;
     } else if (p.w) {
-      v = p.w_keep * (float)static_cast<const T*>(p.w)[at + x] - p.w_step * v;
+      const T4 w = *reinterpret_cast<const T4*>(static_cast<const T*>(p.w) + at);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x] = p.w_keep * (float)w[x] - p.w_step * o[x];
     }
-    static_cast<T*>(p.out)[at + x] = (T)v;
+    T4 v;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[x] = (T)o[x];
+    *reinterpret_cast<T4*>(static_cast<T*>(p.out) + at) = v;
+  } else {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (n + x >= p.N) break;
+      float v = o[x];
+      if (p.master) {
+        v = p.w_keep * p.master[at + x] - p.w_step * v;
+        p.master[at + x] = v;
+      } else if (p.w) {
+        v = p.w_keep * (float)static_cast<const T*>(p.w)[at + x] - p.w_step * v;
+      }
+      static_cast<T*>(p.out)[at + x] = (T)v;
+    }
   }
 }
 
-// One tile of 256 x 256: rows from i0, columns from j0 of matrix e.
-template <int EPI, bool SPLIT, typename T>
-__device__ __forceinline__ void ns_tile(const NsGemmParams& p, int e, int i0, int j0, char* smem) {
+// A wave's 32 rows x 32 NB columns of a result from (r0, c0) on, by way of its LDS region (kNsRegion bytes).
+// acc[nt]: lane (l32, lh) holds row l32 and, per q, columns 32 nt + 8 q + 4 lh .. + 3.
+// MIX: with the sums of the small products of pairs.
+constexpr int kNsRegion = 16384;
+template <int EPI, bool SPLIT, bool MIX, typename T, int NB>
+__device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&acc)[NB], const f32x16 (&mix)[NB], char* region, int e, int r0, int c0,
+                                         bool mirror) {
+  int lane = lane_id();
+  asm volatile("" : "+v"(lane));           // see store_block_via_lds
+  const int l32 = lane & 31, lh = lane >> 5;
+  const lds_ptr base = (lds_ptr)region;
+  auto value = [&](int nt, int q, int x) __attribute__((always_inline)) {
+    const float v = acc[nt][q * 4 + x];
+    return (MIX ? v + mix[nt][q * 4 + x] * (1.0f / kNsLoScale) : v) * p.s_acc;
+  };
+  if constexpr (EPI == kNsOut) {           // rows of fp32, 64 columns at a time
+    constexpr int kRow = 64 * 4 + 16;
+    static_assert(32 * kRow <= kNsRegion, "region");
+#pragma unroll
+    for (int h = 0; h < NB / 2; ++h) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *(lds_f32x4_ptr)(base + l32 * kRow + (nt * 32 + q * 8 + lh * 4) * 4) =
+              f32x4{value(2 * h + nt, q, 0), value(2 * h + nt, q, 1), value(2 * h + nt, q, 2), value(2 * h + nt, q, 3)};
+      lds_settled();
+      const int ch = lane & 15, r4 = lane >> 4, n = c0 + h * 64 + ch * 4;
+      f32x4 o[8];
+#pragma unroll
+      for (int it = 0; it < 8; ++it) o[it] = *(lds_f32x4_ptr)(base + (it * 4 + r4) * kRow + ch * 16);
+      if (p.N % 4 == 0) {
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+          const int m = r0 + it * 4 + r4;
+          if (m < p.M && n < p.N) ns_put<T, true>(p, ((size_t)e * p.M + m) * p.N + n, n, o[it]);
+        }
+      } else {
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+          const int m = r0 + it * 4 + r4;
+          if (m < p.M && n < p.N) ns_put<T, false>(p, ((size_t)e * p.M + m) * p.N + n, n, o[it]);
+        }
+      }
+      wait_lgkmcnt0();
+      lds_settled();
+    }
+  } else {
+    constexpr int kRow = 32 * NB * 2 + 16, kHalf = 32 * kRow, kLanes = NB * 4, kRows = kWave / kLanes, kIts = 32 / kRows;
+    static_assert((SPLIT ? 2 : 1) * kHalf <= kNsRegion, "region");
+    const int cols_valid = p.cols - c0;    // a multiple of 64
+    const int r = lane / kLanes, ch = lane % kLanes;
+    const bool col_ok = ch * 8 < cols_valid;
+    // bytes from a matrix's first to element (row, col) of 8-column chunk `col`, col a multiple of 8
+    auto offset = [&](int row, int col, int ld) __attribute__((always_inline)) {
+      return SPLIT ? (size_t)row * ld * 4 + (size_t)(col >> 5) * 128 + (col & 31) * 2 : ((size_t)row * ld + col) * 2;
+    };
+    if constexpr (EPI == kNsPoly) {        // A's block comes in whole lines as well
+      const char* A = p.A + (size_t)e * p.a_stride;
+#pragma unroll
+      for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+        u32x4 v[kIts];
+#pragma unroll
+        for (int it = 0; it < kIts; ++it)
+          v[it] = *reinterpret_cast<const u32x4*>(A + offset(r0 + it * kRows + r, col_ok ? c0 + ch * 8 : c0, p.ld_c) + h * 64);
+#pragma unroll
+        for (int it = 0; it < kIts; ++it) *(lds_u32x4_ptr)(base + h * kHalf + (it * kRows + r) * kRow + ch * 16) = v[it];
+      }
+      lds_settled();
+    }
+    const lds_ptr mine = base + l32 * kRow + lh * 8;
+#pragma unroll
+    for (int nt = 0; nt < NB; ++nt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const lds_ptr at = mine + (nt * 32 + q * 8) * 2;
+        float v[4] = {value(nt, q, 0), value(nt, q, 1), value(nt, q, 2), value(nt, q, 3)};
+        if constexpr (EPI == kNsPoly) {
+          float a[4], b[4] = {0.f, 0.f, 0.f, 0.f};
+          unpack_f16x4(*(lds_u32x2_ptr)at, a);
+          if constexpr (SPLIT) unpack_f16x4(*(lds_u32x2_ptr)(at + kHalf), b);
+          const int d = r0 + l32 - (c0 + nt * 32 + q * 8 + lh * 4);      // the column of the diagonal
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] += p.s_a * (SPLIT ? a[x] + b[x] * (1.0f / kNsLoScale) : a[x]) + (d == x ? p.diag : 0.f);
+        }
+        const u32x2 hi = pack_f16x4(v);
+        *(lds_u32x2_ptr)at = hi;
+        if constexpr (SPLIT) {
+          float h[4];
+          unpack_f16x4(hi, h);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) h[x] = (v[x] - h[x]) * kNsLoScale;
+          *(lds_u32x2_ptr)(at + kHalf) = pack_f16x4(h);
+        }
+      }
+    lds_settled();
+    char* C = p.C + (size_t)e * p.c_stride;
+    char* CT = p.CT + (size_t)e * p.c_stride;
+#pragma unroll
+    for (int h = 0; h < (SPLIT ? 2 : 1); ++h) {
+      u32x4 v[kIts];
+#pragma unroll
+      for (int it = 0; it < kIts; ++it) v[it] = *(lds_u32x4_ptr)(base + h * kHalf + (it * kRows + r) * kRow + ch * 16);
+#pragma unroll
+      for (int it = 0; it < kIts; ++it)
+        if (col_ok) *reinterpret_cast<u32x4*>(C + offset(r0 + it * kRows + r, c0 + ch * 8, p.ld_c) + h * 64) = v[it];
+      if (mirror) {
+        // 16 lanes read 4 rows x 16 columns and get a column's 4 rows each; lane (g, i): rows 8 g .. 8 g + 7 of column i
+        const int g = lane >> 4, i = lane & 15;
+        const lds_ptr at = base + h * kHalf + (8 * g + (i >> 2)) * kRow + (i & 3) * 8;
+        u32x4 t[NB * 2];
+#pragma unroll
+        for (int cg = 0; cg < NB * 2; ++cg) {
+          const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + cg * 32)));
+          const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + cg * 32 + 4 * kRow)));
+          t[cg] = u32x4{a.x, a.y, b.x, b.y};
+        }
+#pragma unroll
+        for (int cg = 0; cg < NB * 2; ++cg)
+          if (cg * 16 < cols_valid) *reinterpret_cast<u32x4*>(CT + offset(c0 + cg * 16 + i, r0 + 8 * g, p.ld_ct) + h * 64) = t[cg];
+      }
+    }
+    wait_lgkmcnt0();                       // the region is free again
+    lds_settled();
+  }
+}
+
+// One tile of 256 x 256 by four waves of 128 x 128 (the K loop of the grouped products): rows from i0, columns from j0 of matrix e.
+template <int EPI, typename T>
+__device__ __forceinline__ void ns_tile256(const NsGemmParams& p, int e, int i0, int j0, char* smem) {
   int lane = lane_id();
   asm volatile("" : "+v"(lane));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   const int l32 = lane & 31, lh = lane >> 5;
-  const int n_steps = p.K / kBK;
   GemmTileCtx t;
   t.wave = wave;
   t.nA = 8;
@@ -142,8 +246,8 @@ __device__ __forceinline__ void ns_tile(const NsGemmParams& p, int e, int i0, in
 #pragma unroll
   for (int i = 0; i < 8; ++i) {            // rows past the end read the last one again; they are not stored
     const int r = (wave + 4 * i) * 8 + kc_r;
-    t.a_off[i] = (uint32_t)min(i0 + r, p.rows - 1) * (uint32_t)(p.K * 2) + (uint32_t)(kc_c * 16);
-    t.b_off[i] = (uint32_t)min(j0 + r, p.cols - 1) * (uint32_t)(p.K * 2) + (uint32_t)(kc_c * 16);
+    t.a_off[i] = (uint32_t)min(i0 + r, p.rows - 1) * (uint32_t)t.lda_bytes + (uint32_t)(kc_c * 16);
+    t.b_off[i] = (uint32_t)min(j0 + r, p.cols - 1) * (uint32_t)t.ldb_bytes + (uint32_t)(kc_c * 16);
   }
   t.lds0 = lds_addr_of(smem);
   {
@@ -163,109 +267,258 @@ __device__ __forceinline__ void ns_tile(const NsGemmParams& p, int e, int i0, in
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  auto product = [&](const char* P, const char* Q) __attribute__((always_inline)) {
-    t.a_base = uniform_ptr(P + (size_t)e * p.p_stride);
-    t.b_base = uniform_ptr(Q + (size_t)e * p.q_stride);
-    gemm_k_loop<kLayNT, kMaxMT, false, 0, false, true>(acc, accx, t, smem, n_steps);
-  };
-  if constexpr (SPLIT) {                   // the small products first, in units of 2^-11
-    product(p.P.lo, p.Q.hi);
-    product(p.P.hi, p.Q.lo);
-#pragma unroll
-    for (int i = 0; i < kMaxMT; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] *= 1.0f / kNsLoScale;
-  }
-  product(p.P.hi, p.Q.hi);
-
-  // lane: row l32 of each block of 32 x 32, per q the columns q * 8 + lh * 4 .. + 3
-  char* region = epilogue_region(smem, wave);
+  t.a_base = uniform_ptr(p.P + (size_t)e * p.p_stride);
+  t.b_base = uniform_ptr(p.Q + (size_t)e * p.q_stride);
+  gemm_k_loop<kLayNT, kMaxMT, false, 0, false, true>(acc, accx, t, smem, p.K / kBK);
+  // The regions of epilogue_region lie clear of the next tile's first copies, so waves go on to it one by one; rows of fp32 need more.
+  char* region = EPI == kNsOut ? smem + wave * kNsRegion : epilogue_region(smem, wave);
+  if (EPI == kNsOut) __builtin_amdgcn_s_barrier();         // every wave has read its last operands, its copies have landed
   const int c0 = j0 + wn * 128;
-  if (c0 >= p.cols) return;
-  const int cols_valid = min(128, p.cols - c0);
 #pragma unroll
   for (int mt = 0; mt < kMaxMT; ++mt) {
     const int r0 = i0 + wm * 128 + mt * 32;
-    if (r0 >= p.rows) return;
-    if constexpr (EPI == kNsOut) {
-      const int m = r0 + l32;
+    if (r0 < p.rows && c0 < p.cols)
+      ns_block<EPI, false, false, T, 4>(p, acc[mt], acc[mt], region, e, r0, c0, EPI == kNsNext || i0 != j0);
+  }
+  if (EPI == kNsOut) __builtin_amdgcn_s_barrier();         // the next tile's copies go to the same places
+}
+
+// A wave's 64 x 64 of a tile of 128 x 128.
+template <int EPI, bool SPLIT, bool MIX, typename T>
+__device__ __forceinline__ void ns_blocks128(const NsGemmParams& p, const f32x16 (&acc)[2][2], const f32x16 (&mix)[2][2], char* region, int wave, int e,
+                                             int i0, int j0) {
+  const int c0 = j0 + (wave & 1) * 64;
 #pragma unroll
-      for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = c0 + nt * 32 + q * 8 + lh * 4;
-          const float o[4] = {acc[mt][nt][q * 4] * p.s_acc, acc[mt][nt][q * 4 + 1] * p.s_acc, acc[mt][nt][q * 4 + 2] * p.s_acc,
-                              acc[mt][nt][q * 4 + 3] * p.s_acc};
-          if (m < p.M && n < p.N) ns_store_out<T>(p, e, m, n, o);
-        }
-    } else {
-      u32x2 hi[4][4], lo[4][4];
-#pragma unroll
-      for (int nt = 0; nt < 4; ++nt)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int col = nt * 32 + q * 8 + lh * 4;
-          float v[4] = {acc[mt][nt][q * 4] * p.s_acc, acc[mt][nt][q * 4 + 1] * p.s_acc, acc[mt][nt][q * 4 + 2] * p.s_acc,
-                        acc[mt][nt][q * 4 + 3] * p.s_acc};
-          if constexpr (EPI == kNsPoly) {
-            if (col < cols_valid) {
-              const size_t at = (size_t)e * p.a_stride + ((size_t)(r0 + l32) * p.ld_c + c0 + col) * 2;
-              float a[4];
-              unpack_f16x4(*reinterpret_cast<const u32x2*>(p.A.hi + at), a);
-              if constexpr (SPLIT) {
-                float b[4];
-                unpack_f16x4(*reinterpret_cast<const u32x2*>(p.A.lo + at), b);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) a[x] += b[x] * (1.0f / kNsLoScale);
-              }
-#pragma unroll
-              for (int x = 0; x < 4; ++x) v[x] += p.s_a * a[x] + (r0 + l32 == c0 + col + x ? p.diag : 0.f);
-            }
-          }
-          hi[nt][q] = pack_f16x4(v);
-          if constexpr (SPLIT) {
-            float h[4];
-            unpack_f16x4(hi[nt][q], h);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) h[x] = (v[x] - h[x]) * kNsLoScale;
-            lo[nt][q] = pack_f16x4(h);
-          }
-        }
-      const size_t at = (size_t)e * p.c_stride + ((size_t)r0 * p.ld_c + c0) * 2, att = (size_t)e * p.c_stride + ((size_t)c0 * p.ld_ct + r0) * 2;
-      const bool mirror = EPI == kNsNext || i0 != j0;            // a tile on the diagonal is its own mirror
-      ns_store_block(region, hi, p.C.hi + at, p.ld_c, mirror ? p.CT.hi + att : nullptr, p.ld_ct, cols_valid);
-      if constexpr (SPLIT) ns_store_block(region, lo, p.C.lo + at, p.ld_c, mirror ? p.CT.lo + att : nullptr, p.ld_ct, cols_valid);
-    }
+  for (int mt = 0; mt < 2; ++mt) {
+    const int r0 = i0 + (wave >> 1) * 64 + mt * 32;
+    if (r0 < p.rows && c0 < p.cols)
+      ns_block<EPI, SPLIT, MIX, T, 2>(p, acc[mt], mix[mt], region, e, r0, c0, EPI == kNsNext || i0 != j0);
   }
 }
 
-// Tiles of all matrices, by workgroups that walk on in strides; gram and poly: those on and above the diagonal.
-template <int EPI, bool SPLIT, typename T>
-__global__ __launch_bounds__(kGemmThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void ns_gemm_kernel(NsGemmParams p) {
-  __shared__ __attribute__((aligned(1024))) char smem[kGemmLdsBytes];
-  constexpr bool SYM = EPI == kNsGram || EPI == kNsPoly;
-  const int ti = (p.rows + kBM - 1) / kBM, tj = (p.cols + kBN - 1) / kBN;
-  const int per = SYM ? ti * (ti + 1) / 2 : ti * tj, total = per * p.n;
-  const int G = gridDim.x;
-  for (int it = 0; it * G < total; ++it) {
-    const int tile = xcd_spread_tile(it, blockIdx.x, G, total);
-    if (tile < 0) continue;
-    const int e = __builtin_amdgcn_readfirstlane(tile / per);
-    int r = tile - e * per, i, j;
-    if (SYM) {
-      i = 0;
-      while (r >= ti - i) r -= ti - i++;
-      j = i + r;
-    } else {                               // strips of four tile rows, column by column
-      const int strip = __builtin_amdgcn_readfirstlane(r / (4 * tj)), h = min(4, ti - 4 * strip);
-      r -= strip * 4 * tj;
-      j = __builtin_amdgcn_readfirstlane(r / h);
-      i = strip * 4 + r - j * h;
-    }
-    ns_tile<EPI, SPLIT, T>(p, e, i * kBM, j * kBN, smem);
+// One tile of 128 x 128 by four waves of 64 x 64.  STAGES of 64 halves per row and side in LDS: two, and two workgroups to a CU, or four
+// and one, whose copies are then three steps under way.  Pairs: a stage is 32 k, and every fragment read serves three products.
+constexpr int kNsTile = 128, kNsStage = 2 * kNsTile * 128;
+// share, item: with splits > 1 the tile's k's are dealt to that many workgroups, of which this is number `share`; its sums go to place `item`.
+template <int EPI, bool SPLIT, typename T, int STAGES, bool SHARES>
+__device__ __forceinline__ void ns_tile128(const NsGemmParams& p, int e, int i0, int j0, int share, int item, char* smem) {
+  int lane = lane_id();
+  asm volatile("" : "+v"(lane));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const int l32 = lane & 31, lh = lane >> 5;
+  const int row_bytes = p.K * (SPLIT ? 4 : 2), all_steps = row_bytes / 128;
+  const int first_step = SHARES ? all_steps * share / p.splits : 0;
+  const int n_steps = SHARES ? all_steps * (share + 1) / p.splits - first_step : all_steps;
+  const int kc_r = lane >> 3;
+  const int kc_c = (lane & 7) ^ ((4 * (wave & 1) + (kc_r >> 1)) & 7);
+  uint32_t off[8];                         // of the lines that this wave copies: four of P, four of Q
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {            // rows past the end read the last one again; they are not stored
+    const int r = (wave + 4 * i) * 8 + kc_r;
+    off[i] = (uint32_t)min(i0 + r, p.rows - 1) * (uint32_t)row_bytes + (uint32_t)(kc_c * 16);
+    off[4 + i] = (uint32_t)min(j0 + r, p.cols - 1) * (uint32_t)row_bytes + (uint32_t)(kc_c * 16);
   }
+  const char* P = uniform_ptr(p.P + (size_t)e * p.p_stride + (size_t)first_step * 128);
+  const char* Q = uniform_ptr(p.Q + (size_t)e * p.q_stride + (size_t)first_step * 128);
+  const uint32_t lds0 = uniform_u32(lds_addr_of(smem) + (uint32_t)(wave * kLine));
+  // copy i of a step into its stage
+  auto copy = [&](auto ic, const char* ps, const char* qs, uint32_t stage) __attribute__((always_inline)) {
+    constexpr int i = decltype(ic)::value;
+    if constexpr (i < 4) lds_dma16_at<4 * i * kLine>(ps, off[i], stage);
+    else lds_dma16_at<kNsTile * 128 + 4 * (i - 4) * kLine>(qs, off[i], stage);
+  };
+  f32x16 acc[2][2], mix[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = mix[i][j][r] = 0.f;
+
+  // A part of a step: a slice of 16 k, or of pairs 16 k's both halves; per side kFrags fragments: block x % 2 of 32 rows, half x / 2.
+  constexpr int kParts = SPLIT ? 2 : 4, kFrags = SPLIT ? 4 : 2, kMfma = SPLIT ? 12 : 4;
+  uint32_t at_p[4], at_q[4];               // a lane's place in a stage, per slice
+  {
+    const uint32_t f = (uint32_t)((l32 >> 1) & 7), lane_at = lds_addr_of(smem) + (uint32_t)((l32 >> 3) * kLine + (l32 & 7) * 128);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      at_p[q] = lane_at + (uint32_t)(wm * 8 * kLine) + ((((uint32_t)(q * 2 + lh)) ^ f) & 7) * 16;
+      at_q[q] = lane_at + (uint32_t)(kNsTile * 128 + wn * 8 * kLine) + ((((uint32_t)(q * 2 + lh)) ^ f) & 7) * 16;
+    }
+  }
+  struct Frags { bf16x8 p[kFrags], q[kFrags]; };
+  auto read = [&](Frags& f, auto rc, int part, uint32_t stage) __attribute__((always_inline)) {     // read r of 2 kFrags
+    constexpr int r = decltype(rc)::value, x = r >> 1;
+    const uint32_t at = (r & 1 ? at_q : at_p)[part + (x >> 1) * 2] + stage;
+    (r & 1 ? f.q : f.p)[x] = *(lds_bf16x8_cptr)((lds_cptr)(uintptr_t)at + (x & 1) * 4 * kLine);
+  };
+  // The part's MFMAs with the next part's operand reads between them, and behind those CFROM .. CTO - 1 of the copies: a wave is alone on its
+  // SIMD, or with one other, and what it issues in a row leaves the matrix core idle.
+  auto multiply = [&](const Frags& f, Frags& next, bool reads, int part, uint32_t stage, auto from, auto to, const char* ps, const char* qs,
+                      uint32_t dst) __attribute__((always_inline)) {
+    constexpr int kFrom = decltype(from)::value, kReads = 2 * kFrags, kActs = kReads + decltype(to)::value - kFrom;
+    static_for<0, kMfma>([&](auto mc) __attribute__((always_inline)) {
+      constexpr int m = decltype(mc)::value, i = (m >> 1) & 1, j = m & 1, kind = m >> 2;     // kind: hi hi, lo hi, hi lo
+      if constexpr (kind == 0) acc[i][j] = mfma_16bit<true>(f.q[j], f.p[i], acc[i][j]);
+      else if constexpr (kind == 1) mix[i][j] = mfma_16bit<true>(f.q[j], f.p[kFrags - 2 + i], mix[i][j]);
+      else mix[i][j] = mfma_16bit<true>(f.q[kFrags - 2 + j], f.p[i], mix[i][j]);
+      static_for<0, kActs>([&](auto ac) __attribute__((always_inline)) {
+        constexpr int a = decltype(ac)::value;
+        if constexpr (a * kMfma / kActs == m) {
+          if constexpr (a < kReads) {
+            if (reads) read(next, ac, part, stage);
+          } else {
+            copy(std::integral_constant<int, a - kReads + kFrom>{}, ps, qs, dst);
+          }
+        }
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  typedef std::integral_constant<int, 0> C0;
+  typedef std::integral_constant<int, 8> C8;
+  // Behind it the copies of a step have landed in every wave, but for those of `ahead` later steps, and all have read what they had asked for.
+  auto settle = [&](int ahead) __attribute__((always_inline)) {
+    if (STAGES == 4 && ahead >= 2) asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)" ::: "memory");
+    else if (STAGES == 4 && ahead == 1) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  Frags fa, fb;
+  static_for<0, STAGES>([&](auto sc) __attribute__((always_inline)) {
+    constexpr int s = decltype(sc)::value;
+    if (s < n_steps)
+      static_for<0, 8>([&](auto ic) __attribute__((always_inline)) { copy(ic, P + s * 128, Q + s * 128, lds0 + s * kNsStage); });
+  });
+  if (STAGES == 4 && n_steps >= 4) asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
+  else if (STAGES == 4 && n_steps == 3) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+  else if (n_steps >= 2) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  static_for<0, 2 * kFrags>([&](auto rc) __attribute__((always_inline)) { read(fa, rc, 0, 0); });
+  const char *ps = P + STAGES * 128, *qs = Q + STAGES * 128;   // of the copies that come next
+  uint32_t stage = 0;                                          // bytes from the first stage
+  // A step; MORE: with the copies of the step STAGES later, into this one's stage.  The barrier is ahead of the last part, whose operands are
+  // in registers then.
+  auto step = [&](auto more, bool last, int ahead) __attribute__((always_inline)) {
+    constexpr bool MORE = decltype(more)::value;
+#pragma unroll
+    for (int part = 0; part + 2 < kParts; part += 2) {
+      multiply(fa, fb, true, part + 1, stage, C0{}, C0{}, nullptr, nullptr, 0);
+      multiply(fb, fa, true, part + 2, stage, C0{}, C0{}, nullptr, nullptr, 0);
+    }
+    multiply(fa, fb, true, kParts - 1, stage, C0{}, C0{}, nullptr, nullptr, 0);
+    const uint32_t old = stage;
+    stage = stage == (STAGES - 1) * kNsStage ? 0 : stage + kNsStage;
+    if (!last) settle(ahead);
+    if constexpr (MORE) {
+      multiply(fb, fa, true, 0, stage, C0{}, C8{}, ps, qs, lds0 + old);
+      ps += 128;
+      qs += 128;
+    } else {
+      multiply(fb, fa, !last, 0, stage, C0{}, C0{}, nullptr, nullptr, 0);
+    }
+  };
+  int s = 0;
+  for (; s + STAGES < n_steps; ++s) step(std::true_type{}, false, STAGES - 2);
+  for (; s < n_steps; ++s) step(std::false_type{}, s + 1 == n_steps, n_steps - 2 - s);
+  if constexpr (SHARES) {
+    float* dst = p.part + ((size_t)item * 4 + wave) * 4096 + lane;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dst[((i * 2 + j) * 16 + r) * 64] = SPLIT ? acc[i][j][r] + mix[i][j][r] * (1.0f / kNsLoScale) : acc[i][j][r];
+  } else {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();          // every wave has read its last operands
+    asm volatile("" ::: "memory");
+    ns_blocks128<EPI, SPLIT, SPLIT, T>(p, acc, mix, smem + wave * kNsRegion, wave, e, i0, j0);
+  }
+}
+
+// Tile r of a matrix of ti x tj tiles.  SYM: those on and above the diagonal, row by row; else strips of four tile rows, column by column,
+// so that tiles under way together share operands.
+template <bool SYM> __device__ __forceinline__ void ns_tile_at(int r, int ti, int tj, int& i, int& j) {
+  if (SYM) {
+    i = 0;
+    while (r >= ti - i) r -= ti - i++;
+    j = i + r;
+  } else {
+    const int strip = __builtin_amdgcn_readfirstlane(r / (4 * tj)), h = min(4, ti - 4 * strip);
+    r -= strip * 4 * tj;
+    j = __builtin_amdgcn_readfirstlane(r / h);
+    i = strip * 4 + r - j * h;
+  }
+}
+constexpr bool ns_symmetric(int epi) { return epi == kNsGram || epi == kNsPoly; }
+
+// Whole tiles of 256 x 256, by workgroups that walk on in strides.
+template <int EPI, typename T>
+__global__ __launch_bounds__(kGemmThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void ns_gemm256_kernel(NsGemmParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[kGemmLdsBytes];
+  constexpr bool SYM = ns_symmetric(EPI);
+  const int ti = (p.rows + kBM - 1) / kBM, tj = (p.cols + kBN - 1) / kBN;
+  const int per = SYM ? ti * (ti + 1) / 2 : ti * tj, G = gridDim.x;
+  for (int it = 0; it * G < p.tiles; ++it) {
+    const int tile = xcd_spread_tile(it, blockIdx.x, G, p.tiles);
+    if (tile < 0) continue;
+    const int at = p.first + tile, e = __builtin_amdgcn_readfirstlane(at / per);
+    int i, j;
+    ns_tile_at<SYM>(at - e * per, ti, tj, i, j);
+    ns_tile256<EPI, T>(p, e, i * kBM, j * kBN, smem);
+  }
+}
+
+// Tile `at` of 128 x 128.  QUARTERS: at / 4 counts tiles of 256 x 256.  Returns false where there is none.
+template <bool SYM, bool QUARTERS> __device__ __forceinline__ bool ns_tile128_at(const NsGemmParams& p, int at, int& e, int& i, int& j) {
+  constexpr int kSide = QUARTERS ? 256 : 128;
+  const int ti = (p.rows + kSide - 1) / kSide, tj = (p.cols + kSide - 1) / kSide;
+  const int per = SYM ? ti * (ti + 1) / 2 : ti * tj, big = QUARTERS ? at >> 2 : at;
+  e = __builtin_amdgcn_readfirstlane(big / per);
+  ns_tile_at<SYM>(big - e * per, ti, tj, i, j);
+  if (!QUARTERS) return true;
+  i = 2 * i + ((at >> 1) & 1);
+  j = 2 * j + (at & 1);
+  return i * 128 < p.rows && j * 128 < p.cols && !(SYM && i > j);
+}
+
+// Tiles of 128 x 128 (p.first .. p.first + p.tiles - 1), one to a workgroup, or p.splits workgroups to each.
+template <int EPI, bool SPLIT, typename T, bool QUARTERS, int STAGES, bool SHARES>
+__global__ __launch_bounds__(256, STAGES == 2 ? 2 : 1) void ns_gemm128_kernel(NsGemmParams p) {
+  static_assert(STAGES == 2 || STAGES == 4, "stages");
+  __shared__ __attribute__((aligned(1024))) char smem[STAGES * kNsStage];
+  // workgroups are dealt to the dies in turn: a die's take a contiguous eighth
+  const int item = xcd_spread_tile(0, blockIdx.x, gridDim.x, SHARES ? p.tiles * p.splits : p.tiles);
+  if (item < 0) return;
+  const int tile = SHARES ? __builtin_amdgcn_readfirstlane(item / p.splits) : item;
+  int e, i, j;
+  if (!ns_tile128_at<ns_symmetric(EPI), QUARTERS>(p, p.first + tile, e, i, j)) return;
+  ns_tile128<EPI, SPLIT, T, STAGES, SHARES>(p, e, i * 128, j * 128, SHARES ? item - tile * p.splits : 0, item, smem);
+}
+
+// The shares of a tile joined, in their order: a workgroup of one wave for each of the tile's four 64 x 64, as few tiles are left over and a CU
+// pulls in only some 50 bytes a nanosecond (four waves in one workgroup, 16 shares: 16 us).
+template <int EPI, bool SPLIT, typename T, bool QUARTERS>
+__global__ __launch_bounds__(64) void ns_join_kernel(NsGemmParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[kNsRegion];
+  const int tile = blockIdx.x >> 2, wave = blockIdx.x & 3;
+  int e, i, j;
+  if (!ns_tile128_at<ns_symmetric(EPI), QUARTERS>(p, p.first + tile, e, i, j)) return;
+  const float* src = p.part + ((size_t)tile * p.splits * 4 + wave) * 4096 + lane_id();
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int x = 0; x < 64; ++x) acc[x >> 5][(x >> 4) & 1][x & 15] = src[x * 64];
+  for (int s = 1; s < p.splits; ++s) {
+    src += 4 * 4096;
+#pragma unroll
+    for (int x = 0; x < 64; ++x) acc[x >> 5][(x >> 4) & 1][x & 15] += src[x * 64];
+  }
+  ns_blocks128<EPI, SPLIT, false, T>(p, acc, acc, smem, wave, e, i * 128, j * 128);
 }
 
 // ---- momentum, norm, and the first X ----
@@ -280,33 +533,50 @@ struct NsPrepParams {
   int parts;
   float scale;                             // 2^x
   float eps;
-  NsMat X, XT;                             // [M padded][N padded] and its transpose
+  char *X, *XT;                            // [M padded][N padded] and its transpose
   long stride;                             // bytes between matrices
   int M, N, Mp, Np, n;
 };
 
-template <typename T> __device__ __forceinline__ float ns_update(const NsPrepParams& p, size_t at) {
-  const float g = (float)static_cast<const T*>(p.g)[at];
-  if (!p.m) return g;
-  const float m = p.m_out[at];
-  return p.nesterov ? g + p.mu * m : m;
-}
-
-// Sums of squares in 64 bits, so that no update is too large or small; momentum on the way.  In 64 bits they also have no order to speak
-// of in the rounded result, and it is fixed all the same.
+// Sums of squares in 64 bits, so that no update is too large or too small for them; momentum on the way.  A workgroup takes every
+// parts-th piece of 2048 values, a thread eight of them.
 template <typename T> __global__ __launch_bounds__(256) void ns_norm_kernel(NsPrepParams p) {
   __shared__ double s_sum[4];
   const int e = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
   const size_t n = (size_t)p.M * p.N, base = (size_t)e * n;
+  const T* g = static_cast<const T*>(p.g) + base;
   double sum = 0.0;
-  for (size_t i = (size_t)part * 256 + threadIdx.x; i < n; i += (size_t)p.parts * 256) {
-    float u = (float)static_cast<const T*>(p.g)[base + i];
-    if (p.m) {
-      const float m = p.mu * p.m[base + i] + u;
-      p.m_out[base + i] = m;
-      u = p.nesterov ? u + p.mu * m : m;
+  for (size_t i = ((size_t)part * 256 + threadIdx.x) * 8; i < n; i += (size_t)p.parts * 2048) {
+    float u[8];
+    if (i + 8 <= n) {
+      const Raw8<T> a = raw_load<T, false>(g + i, 0, 8);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) u[x] = raw_get<T>(a, x);
+      if (p.m) {
+        const Raw8<float> b = raw_load<float, false>(p.m + base + i, 0, 8);
+        float m[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          m[x] = p.mu * raw_get<float>(b, x) + u[x];
+          u[x] = p.nesterov ? u[x] + p.mu * m[x] : m[x];
+        }
+        raw_store<float, false>(p.m_out + base + i, 0, 8, raw_pack<float>(m));
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        u[x] = 0.f;
+        if (i + x >= n) continue;
+        u[x] = (float)g[i + x];
+        if (p.m) {
+          const float m = p.mu * p.m[base + i + x] + u[x];
+          p.m_out[base + i + x] = m;
+          u[x] = p.nesterov ? u[x] + p.mu * m : m;
+        }
+      }
     }
-    sum += (double)u * (double)u;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) sum += (double)u[x] * (double)u[x];
   }
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o);
@@ -315,12 +585,39 @@ template <typename T> __global__ __launch_bounds__(256) void ns_norm_kernel(NsPr
   if (threadIdx.x == 0) p.part[(size_t)e * p.parts + part] = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
 }
 
-// Tiles of 64 x 64 of the padded matrix: fp16 straight and transposed.
+// Tiles of 64 x 64 of the padded matrix: fp16 straight, and transposed by way of LDS; a thread has eight columns of two rows, then
+// eight rows of two columns.
 template <typename T, bool SPLIT> __global__ __launch_bounds__(256) void ns_first_kernel(NsPrepParams p) {
   __shared__ float s[64][65];
   __shared__ double s_norm[4];
   const int tj = p.Np / 64, per = (p.Mp / 64) * tj;
   const int e = blockIdx.x / per, r = blockIdx.x % per, i0 = (r / tj) * 64, j0 = (r % tj) * 64;
+  const int ch = threadIdx.x & 7, row = threadIdx.x >> 3;
+  float u[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = i0 + row + 32 * h, j = j0 + ch * 8;
+    const size_t at = ((size_t)e * p.M + i) * p.N + j;
+    const T* g = static_cast<const T*>(p.g) + at;
+    if (i < p.M && j + 8 <= p.N) {
+      const Raw8<T> a = raw_load<T, false>(g, 0, 8);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) u[h][x] = raw_get<T>(a, x);
+      if (p.m) {
+        const Raw8<float> b = raw_load<float, false>(p.m_out + at, 0, 8);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) u[h][x] = p.nesterov ? u[h][x] + p.mu * raw_get<float>(b, x) : raw_get<float>(b, x);
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        u[h][x] = 0.f;
+        if (i >= p.M || j + x >= p.N) continue;
+        u[h][x] = (float)g[x];
+        if (p.m) u[h][x] = p.nesterov ? u[h][x] + p.mu * p.m_out[at + x] : p.m_out[at + x];
+      }
+    }
+  }
   double sum = threadIdx.x < (unsigned)p.parts ? p.part[(size_t)e * p.parts + threadIdx.x] : 0.0;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o);
@@ -328,20 +625,39 @@ template <typename T, bool SPLIT> __global__ __launch_bounds__(256) void ns_firs
   __syncthreads();
   sum = s_norm[0] + s_norm[1] + s_norm[2] + s_norm[3];
   const double f = (double)p.scale / (sqrt(sum) + (double)p.eps);   // beyond fp32 for a tiny norm
-  const int l = threadIdx.x & 63, w = threadIdx.x / 64;
-  for (int k = w; k < 64; k += 4) {
-    const int i = i0 + k, j = j0 + l;
-    s[k][l] = i < p.M && j < p.N ? (float)((double)ns_update<T>(p, ((size_t)e * p.M + i) * p.N + j) * f) : 0.f;
-  }
-  __syncthreads();
-  auto store = [&](const NsMat& m, size_t at, float v) __attribute__((always_inline)) {
-    const _Float16 h = (_Float16)v;
-    *reinterpret_cast<_Float16*>(m.hi + at) = h;
-    if constexpr (SPLIT) *reinterpret_cast<_Float16*>(m.lo + at) = (_Float16)((v - (float)h) * kNsLoScale);
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      u[h][x] = (float)((double)u[h][x] * f);
+      s[row + 32 * h][ch * 8 + x] = u[h][x];
+    }
+  auto store = [&](char* m, int i, int j, int ld, const float (&v)[8]) __attribute__((always_inline)) {
+    float a[4], b[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) { a[x] = v[x]; b[x] = v[4 + x]; }
+    const u32x2 h0 = pack_f16x4(a), h1 = pack_f16x4(b);
+    char* at = m + (size_t)e * p.stride + (SPLIT ? (size_t)i * ld * 4 + (size_t)(j >> 5) * 128 + (j & 31) * 2 : ((size_t)i * ld + j) * 2);
+    *reinterpret_cast<u32x4*>(at) = u32x4{h0.x, h0.y, h1.x, h1.y};
+    if constexpr (SPLIT) {
+      float c[4], d[4];
+      unpack_f16x4(h0, c);
+      unpack_f16x4(h1, d);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) { c[x] = (a[x] - c[x]) * kNsLoScale; d[x] = (b[x] - d[x]) * kNsLoScale; }
+      const u32x2 l0 = pack_f16x4(c), l1 = pack_f16x4(d);
+      *reinterpret_cast<u32x4*>(at + 64) = u32x4{l0.x, l0.y, l1.x, l1.y};
+    }
   };
-  for (int k = w; k < 64; k += 4) {
-    store(p.X, (size_t)e * p.stride + ((size_t)(i0 + k) * p.Np + j0 + l) * 2, s[k][l]);
-    store(p.XT, (size_t)e * p.stride + ((size_t)(j0 + k) * p.Mp + i0 + l) * 2, s[l][k]);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) store(p.X, i0 + row + 32 * h, j0 + ch * 8, p.Np, u[h]);
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float v[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x] = s[ch * 8 + x][row + 32 * h];
+    store(p.XT, j0 + row + 32 * h, i0 + ch * 8, p.Mp, v);
   }
 }
 

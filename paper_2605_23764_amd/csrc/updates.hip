@@ -16,6 +16,8 @@ namespace {
 constexpr int kMaxSteps = 16;
 // Matrices are worked on in groups whose workspace stays below this, one at least: enough tiles at a time for the whole chip.
 constexpr size_t kNsGroupBytes = (size_t)4 << 30;
+constexpr int kNsMaxShares = 256;          // partial tiles of a product's remainder
+constexpr int kNsShareSteps = 4;           // K steps of a share, at least
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool good(const void* p) { return p && aligned(p); }
@@ -26,34 +28,35 @@ int check_matrices(int B, int M, int N, int dtype) {
   if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
   if (B < 0 || M < 1 || N < 1 || M > (1 << 18) || N > (1 << 18)) return MOE_ERR_UNSUPPORTED_SHAPE;
   const double s = pad(std::min(M, N)), l = pad(std::max(M, N));
-  if (s * l * 2 >= 4294967296.0 || s > (1 << 15)) return MOE_ERR_UNSUPPORTED_SHAPE;   // 32-bit offsets inside a matrix
+  if (s * l * (dtype == MOE_F32 ? 4 : 2) >= 4294967296.0 || s > (1 << 15)) return MOE_ERR_UNSUPPORTED_SHAPE;   // 32-bit offsets inside a matrix
   if ((double)B * M * N * 4 > 9.0e18) return MOE_ERR_UNSUPPORTED_SHAPE;
   return MOE_OK;
 }
 
 // Matrices of a group, and a group's workspace.
 struct Plan {
-  int B, M, N, Sp, Lp, group, halves;
+  int B, M, N, Sp, Lp, group;
   size_t x_bytes, a_bytes;                 // of one matrix
-  size_t x, a, part, total;                // X and its transpose, twice; A and B; per half
+  size_t x, a, part, share, total;                // X and its transpose, two of each; A and B
 };
 Plan make_plan(int B, int M, int N, int dtype) {
   Plan p{};
   p.B = B; p.M = M; p.N = N;
   p.Sp = pad(std::min(M, N));
   p.Lp = pad(std::max(M, N));
-  p.halves = dtype == MOE_F32 ? 2 : 1;
-  p.x_bytes = (size_t)p.Sp * p.Lp * 2;
-  p.a_bytes = (size_t)p.Sp * p.Sp * 2;
-  const size_t per = p.halves * (4 * p.x_bytes + 2 * p.a_bytes) + kNsMaxParts * 8;
+  const size_t value = dtype == MOE_F32 ? 4 : 2;   // fp16, or pairs of it
+  p.x_bytes = (size_t)p.Sp * p.Lp * value;
+  p.a_bytes = (size_t)p.Sp * p.Sp * value;
+  const size_t per = 4 * p.x_bytes + 2 * p.a_bytes + kNsMaxParts * 8;
   const int most = (int)std::min<size_t>(std::max<size_t>(kNsGroupBytes / per, 1), 1 << 14);
   const int groups = std::max(1, (B + most - 1) / most);
   p.group = std::max(1, (B + groups - 1) / groups);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
-  p.x = take(p.halves * 4 * p.x_bytes * p.group);
-  p.a = take(p.halves * 2 * p.a_bytes * p.group);
+  p.x = take(4 * p.x_bytes * p.group);
+  p.a = take(2 * p.a_bytes * p.group);
   p.part = take((size_t)kNsMaxParts * 8 * p.group);
+  p.share = take((size_t)kNsMaxShares * 128 * 128 * 4);
   p.total = off;
   return p;
 }
@@ -109,28 +112,65 @@ struct Update {
   int nesterov;
 };
 
+// Tiles of 128 x 128 from p.first on, p.tiles of them, with fewer than one to a CU left over at the end of whole rounds.  A remainder that
+// would leave half of the CUs idle is dealt out along k as well and joined by a second launch.
+template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGemmParams p, int cus, hipStream_t s) {
+  auto grid = [](int n) { return dim3((unsigned)((n + 7) / 8 * 8)); };
+  const int n_steps = p.K * (SPLIT ? 4 : 2) / 128, first = p.first, tiles = p.tiles;
+  const int rest = tiles % cus;
+  p.splits = rest ? std::min(std::min(cus, kNsMaxShares) / rest, n_steps / kNsShareSteps) : 0;
+  if (p.splits < 2) p.splits = 0;
+  p.tiles = p.splits ? tiles - rest : tiles;
+  if (p.tiles > 0) {
+    if (p.tiles <= cus) hipLaunchKernelGGL((ns_gemm128_kernel<EPI, SPLIT, T, QUARTERS, 4, false>), grid(p.tiles), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((ns_gemm128_kernel<EPI, SPLIT, T, QUARTERS, 2, false>), grid(p.tiles), dim3(256), 0, s, p);
+  }
+  if (p.splits) {
+    p.first = first + p.tiles;
+    p.tiles = rest;
+    hipLaunchKernelGGL((ns_gemm128_kernel<EPI, SPLIT, T, QUARTERS, 4, true>), grid(rest * p.splits), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((ns_join_kernel<EPI, SPLIT, T, QUARTERS>), dim3(4 * rest), dim3(64), 0, s, p);
+  }
+}
+
+// One product of every matrix of the group.  Whole rounds of tiles of 256 x 256, one to a CU, as long as they fill the chip; what is left
+// over, and everything of a product with too few of them (or in pairs), as tiles of 128 x 128.
+template <int EPI, typename T> void run_product(NsGemmParams p, int cus, hipStream_t s) {
+  constexpr bool SPLIT = sizeof(T) == 4, SYM = ns_symmetric(EPI);
+  auto tiles = [&](int side) {
+    const int ti = (p.rows + side - 1) / side, tj = (p.cols + side - 1) / side;
+    return p.n * (SYM ? ti * (ti + 1) / 2 : ti * tj);
+  };
+  p.first = 0;
+  if constexpr (!SPLIT) {
+    const int whole = tiles(256), rest = whole % cus;
+    if (whole >= cus) {
+      const bool quarters = rest > 0 && 2 * rest <= cus;
+      p.tiles = quarters ? whole - rest : whole;
+      hipLaunchKernelGGL((ns_gemm256_kernel<EPI, T>), dim3(cus), dim3(kGemmThreads), 0, s, p);
+      if (quarters) {
+        p.first = 4 * p.tiles;
+        p.tiles = 4 * rest;
+        run_tiles128<EPI, false, T, true>(p, cus, s);
+      }
+      return;
+    }
+  }
+  p.tiles = tiles(128);
+  run_tiles128<EPI, SPLIT, T, false>(p, cus, s);
+}
+
 template <typename T> int run_update(const Plan& L, const Steps& st, const Update& u, char* ws, hipStream_t stream) {
   constexpr bool SPLIT = sizeof(T) == 4;
   const bool wide = L.M <= L.N;
-  const int cus = (device_cus() + 7) / 8 * 8;
+  const int cus = device_cus() / 8 * 8;
   for (int e0 = 0; e0 < L.B; e0 += L.group) {
     const int n = std::min(L.group, L.B - e0);
     const size_t first = (size_t)e0 * L.M * L.N;
-    // arrays of the group: X short x long and long x short, two of each; A; B; the halves' arrays behind each other
-    auto x_of = [&](int which) {
-      NsMat m;
-      m.hi = ws + L.x + (size_t)which * L.group * L.x_bytes * L.halves;
-      m.lo = SPLIT ? m.hi + (size_t)L.group * L.x_bytes : nullptr;
-      return m;
-    };
-    auto a_of = [&](int which) {
-      NsMat m;
-      m.hi = ws + L.a + (size_t)which * L.group * L.a_bytes * L.halves;
-      m.lo = SPLIT ? m.hi + (size_t)L.group * L.a_bytes : nullptr;
-      return m;
-    };
-    NsMat xs = x_of(0), xl = x_of(1), xs_next = x_of(2), xl_next = x_of(3);
-    const NsMat A = a_of(0), Bm = a_of(1);
+    // the group's arrays: X short x long and long x short, two of each; A; B
+    auto x_of = [&](int i) { return ws + L.x + (size_t)i * L.group * L.x_bytes; };
+    char *xs = x_of(0), *xl = x_of(1), *xs_next = x_of(2), *xl_next = x_of(3);
+    char *A = ws + L.a, *Bm = A + (size_t)L.group * L.a_bytes;
 
     NsPrepParams q{};
     q.g = static_cast<const T*>(u.g) + first;
@@ -151,6 +191,7 @@ template <typename T> int run_update(const Plan& L, const Steps& st, const Updat
     for (int i = 0; i < st.n; ++i) {
       NsGemmParams p{};
       p.n = n;
+      p.part = reinterpret_cast<float*>(ws + L.share);
       p.rows = p.cols = L.Sp;
       p.ld_c = p.ld_ct = L.Sp;
       p.c_stride = p.a_stride = (long)L.a_bytes;
@@ -159,10 +200,7 @@ template <typename T> int run_update(const Plan& L, const Steps& st, const Updat
       p.p_stride = p.q_stride = (long)L.x_bytes;
       p.K = L.Lp;
       p.s_acc = ldexpf(1.f, st.ea[i] - 2 * st.ex);
-      const int sym = ((L.Sp + kBM - 1) / kBM) * ((L.Sp + kBM - 1) / kBM + 1) / 2;
-      const int all = ((L.Sp + kBM - 1) / kBM) * ((L.Lp + kBM - 1) / kBM);
-      auto grid = [&](long tiles) { return dim3((unsigned)std::min<long>((tiles * n + 7) / 8 * 8, cus)); };
-      hipLaunchKernelGGL((ns_gemm_kernel<kNsGram, SPLIT, T>), grid(sym), dim3(kGemmThreads), 0, stream, p);
+      run_product<kNsGram, T>(p, cus, stream);
       // B = a I + b A + c A^2
       p.P = p.Q = p.A = A; p.C = p.CT = Bm;
       p.p_stride = p.q_stride = (long)L.a_bytes;
@@ -170,8 +208,7 @@ template <typename T> int run_update(const Plan& L, const Steps& st, const Updat
       p.s_acc = ldexpf(st.c[i][2], st.eb[i] - 2 * st.ea[i]);
       p.s_a = ldexpf(st.c[i][1], st.eb[i] - st.ea[i]);
       p.diag = ldexpf(st.c[i][0], st.eb[i]);
-      hipLaunchKernelGGL((ns_gemm_kernel<kNsPoly, SPLIT, T>), grid(sym), dim3(kGemmThreads), 0, stream, p);
-      p.A = NsMat{};
+      run_product<kNsPoly, T>(p, cus, stream);
       if (i + 1 < st.n) {
         // X <- B X, and its transpose
         p.P = Bm; p.Q = xl; p.C = xs_next; p.CT = xl_next;
@@ -179,14 +216,14 @@ template <typename T> int run_update(const Plan& L, const Steps& st, const Updat
         p.cols = L.Lp;
         p.ld_c = L.Lp; p.ld_ct = L.Sp;
         p.s_acc = ldexpf(1.f, -st.eb[i]);
-        hipLaunchKernelGGL((ns_gemm_kernel<kNsNext, SPLIT, T>), grid(all), dim3(kGemmThreads), 0, stream, p);
+        run_product<kNsNext, T>(p, cus, stream);
         std::swap(xs, xs_next);
         std::swap(xl, xl_next);
       } else {
         // the caller's side up: M x N
         p.P = wide ? Bm : xl; p.Q = wide ? xl : Bm;
-        p.p_stride = wide ? (long)L.a_bytes : (long)L.x_bytes;
-        p.q_stride = wide ? (long)L.x_bytes : (long)L.a_bytes;
+        p.p_stride = (long)(wide ? L.a_bytes : L.x_bytes);
+        p.q_stride = (long)(wide ? L.x_bytes : L.a_bytes);
         p.rows = wide ? L.Sp : L.Lp; p.cols = wide ? L.Lp : L.Sp;
         p.s_acc = ldexpf(1.f, -st.eb[i] - st.ex);
         p.w = u.w ? static_cast<const T*>(u.w) + first : nullptr;
@@ -194,7 +231,7 @@ template <typename T> int run_update(const Plan& L, const Steps& st, const Updat
         p.out = static_cast<T*>(u.out) + first;
         p.w_keep = u.w_keep; p.w_step = u.w_step;
         p.M = L.M; p.N = L.N;
-        hipLaunchKernelGGL((ns_gemm_kernel<kNsOut, SPLIT, T>), grid(all), dim3(kGemmThreads), 0, stream, p);
+        run_product<kNsOut, T>(p, cus, stream);
       }
     }
     if (hipGetLastError() != hipSuccess) return MOE_ERR_LAUNCH;

@@ -78,6 +78,31 @@ def test_orthogonalize(n, M, N, dtype):
     assert torch.equal(again, out)
 
 
+@pytest.mark.parametrize("M,N", [(1000, 1570), (1570, 1000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_whole_rounds_and_what_is_left_over(M, N, dtype):
+    """Products of several rounds of the chip: whole tiles, quarters of the last, shares along the reduction; the first, a middle and the last
+    matrix against the oracle, all against each other's spectra."""
+    n = 26 if dtype == "bf16" else 7
+    print(f"orthogonalize {n} x {M} x {N} {dtype}", flush=True)
+    g = torch.Generator("cuda").manual_seed(M)
+    u = (torch.randn(n, M, 40, generator=g, device="cuda") @ torch.randn(n, 40, N, generator=g, device="cuda") * 40 ** -0.5
+         + torch.randn(n, M, N, generator=g, device="cuda")).to(TORCH[dtype])
+    out = torch.full_like(u, float("nan"))
+    moe.moe_orthogonalize(u, out, _ws(n, M, N, dtype))
+    assert torch.isfinite(out).all()
+    for e in (0, n // 2, n - 1):
+        want, err = _bound(u[e], dtype)
+        want = want if M <= N else want.T
+        off = np.linalg.norm(f64(out)[e] - want)
+        assert off <= 0.5 * err + HALF[dtype] * (np.linalg.norm(want) + err), f"matrix {e}: {off:.3g}, {err:.3g}"
+    one = torch.empty_like(u[:1])
+    ws = _ws(1, M, N, dtype)
+    for e in range(n):                                                # alone a matrix takes other tiles: the same up to roundings
+        moe.moe_orthogonalize(u[e:e + 1], one, ws)
+        assert torch.linalg.vector_norm((one[0] - out[e]).float()) <= (err + HALF[dtype] * np.linalg.norm(want)), e
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_coefficients_and_steps(dtype):
     u = _dev(_u(2, 70, 150, 3), dtype)
