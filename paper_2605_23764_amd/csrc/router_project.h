@@ -7,10 +7,10 @@
 // that is 5 and 2.7 times as fast.  (An infinity has NaN pieces.)
 //
 // One form, C[i,j] = sum over k of P(i,k) Q(j,k), with either operand k-contiguous or row-contiguous in memory.  Tiles of 128 x 128 by
-// four waves of 64 x 64, k steps of 32: a step's values are fetched into registers while the step before is multiplied, split there,
-// and stand in LDS k-contiguous by rows of 64 bytes, whose four 16-byte chunks are swizzled so that operand reads spread over the
-// banks.  logits (long H) and dW (long T) split k over workgroups, as they have few tiles; a second launch joins the partial sums in a
-// fixed order.
+// four waves of 64 x 64 (up to 32 experts: 128 x 32, by four of 32 x 32), k steps of 64: a step's values are fetched into registers while
+// the step before is multiplied, split there, and stand in LDS k-contiguous by rows of 128 bytes, whose eight 16-byte chunks are
+// swizzled so that operand reads and the writes of row-contiguous operands spread over the banks.  logits (long H) and dW (long T)
+// split k over workgroups, as they have few tiles; a second launch joins the partial sums in a fixed order.
 #pragma once
 #include <type_traits>
 
@@ -18,15 +18,14 @@
 
 namespace moe {
 
-constexpr int kProjTile = 128, kProjK = 32, kProjThreads = 256;
-constexpr int kProjPiece = kProjTile * kProjK * 2;   // bytes of a piece of a side's step
+constexpr int kProjTile = 128, kProjK = 64, kProjThreads = 256;
 
 struct ProjParams {
   const void *P, *Q;             // P(i,k): k-contiguous P[i ld_p + k], else P[k ld_p + i]
   int ld_p, ld_q;
   int rows, cols, K;             // C is rows x cols
   int k_split, splits;           // k's of a workgroup (a multiple of kProjK), workgroups along k
-  int ti, tj;                    // tiles
+  int tj;                        // tiles along the columns
   float* part;                   // [splits][rows][cols]; the result itself with one
   const void* add;               // out: added, [rows][cols] of the storage type, or null
   void* out;
@@ -64,18 +63,24 @@ typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 typedef uint32_t u32x4_half __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32_half __attribute__((aligned(2)));
 
-// One side's step: two chunks per thread.  k-contiguous: rows tid / 4 and 64 more, k's 8 (tid % 4) on.  Row-contiguous: rows 2 (tid % 64)
-// and the next, k's 8 (tid / 64) on: eight loads of two neighbouring rows' values.
-template <typename T, bool KC> struct ProjSide {
-  ProjChunk<T> c[2];
-  __device__ __forceinline__ static int row(int n) { return KC ? (threadIdx.x >> 2) + 64 * n : 2 * (threadIdx.x & 63) + n; }
-  __device__ __forceinline__ static int chunk() { return KC ? threadIdx.x & 3 : threadIdx.x >> 6; }
+// 16-byte chunk c of row r in its row of a stage.
+__device__ __forceinline__ int proj_chunk(int r, int c) { return r * 128 + ((c ^ (r >> 1) ^ (r >> 4)) & 7) * 16; }
+
+// One side's step of R rows: R / 32 chunks per thread.  k-contiguous: rows tid / 8 and every 32nd behind it, k's 8 (tid % 8) on.
+// Row-contiguous: R / 32 neighbouring rows from R / 32 (tid % 32) on, k's 8 (tid / 32) on: eight loads of those rows' values.
+template <typename T, bool KC, int R> struct ProjSide {
+  static constexpr int kN = R / 32;
+  typedef float fvec __attribute__((ext_vector_type(kN), aligned(4)));
+  typedef uint16_t hvec __attribute__((ext_vector_type(kN), aligned(2)));
+  ProjChunk<T> c[kN];
+  __device__ __forceinline__ static int row(int n) { return KC ? (threadIdx.x >> 3) + 32 * n : kN * (threadIdx.x & 31) + n; }
+  __device__ __forceinline__ static int chunk() { return KC ? threadIdx.x & 7 : threadIdx.x >> 5; }
 
   __device__ __forceinline__ void fetch(const T* base, int ld, int rows, int i0, int k0, int k_end) {
     const int k = k0 + chunk() * 8;
     if constexpr (KC) {
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
+      for (int n = 0; n < kN; ++n) {
         const int i = i0 + row(n);
         const T* src = base + (size_t)i * ld + k;
         c[n] = ProjChunk<T>{};
@@ -96,29 +101,31 @@ template <typename T, bool KC> struct ProjSide {
         }
       }
     } else {
-      c[0] = ProjChunk<T>{};
-      c[1] = ProjChunk<T>{};
+#pragma unroll
+      for (int n = 0; n < kN; ++n) c[n] = ProjChunk<T>{};
       const int i = i0 + row(0);
-      if (i + 1 < rows && k + 8 <= k_end) {
+      if (i + kN <= rows && k + 8 <= k_end) {
+        const T* src = base + (size_t)k * ld + i;
         if constexpr (sizeof(T) == 4) {
-          f32x2_any v[8];
+          fvec v[8];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) v[x] = *reinterpret_cast<const f32x2_any*>(base + (size_t)(k + x) * ld + i);
+          for (int x = 0; x < 8; ++x) v[x] = *reinterpret_cast<const fvec*>(src + (size_t)x * ld);
 #pragma unroll
-          for (int x = 0; x < 8; ++x) { c[0].v[x] = v[x][0]; c[1].v[x] = v[x][1]; }
+          for (int n = 0; n < kN; ++n)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) c[n].v[x] = v[x][n];
         } else {
-          uint32_t v[8];
+          hvec v[8];
 #pragma unroll
-          for (int x = 0; x < 8; ++x) v[x] = *reinterpret_cast<const u32_half*>(base + (size_t)(k + x) * ld + i);
+          for (int x = 0; x < 8; ++x) v[x] = *reinterpret_cast<const hvec*>(src + (size_t)x * ld);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            c[0].w[x] = __builtin_amdgcn_perm(v[2 * x + 1], v[2 * x], 0x05040100);
-            c[1].w[x] = high_halves(v[2 * x], v[2 * x + 1]);
-          }
+          for (int n = 0; n < kN; ++n)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) c[n].w[x] = (uint32_t)v[2 * x][n] | (uint32_t)v[2 * x + 1][n] << 16;
         }
       } else {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < kN; ++n)
 #pragma unroll
           for (int x = 0; x < 8; ++x)
             if (i + n < rows && k + x < k_end) put(n, x, base[(size_t)(k + x) * ld + i + n]);
@@ -131,63 +138,86 @@ template <typename T, bool KC> struct ProjSide {
   }
   template <int N> __device__ __forceinline__ void store(char* lds) const {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int n = 0; n < kN; ++n) {
       u32x4 piece[N];
       proj_pieces<N>(c[n], piece);
-      const int r = row(n);
 #pragma unroll
-      for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + i * kProjPiece + r * 64 + ((chunk() ^ (r >> 1)) & 3) * 16) = piece[i];
+      for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + i * R * 128 + proj_chunk(row(n), chunk())) = piece[i];
     }
   }
 };
 
-// NP, NQ: pieces of a value of each side.  OUT: storage of the result of dx, void: partial sums in fp32.
-template <typename TP, bool KCP, int NP, typename TQ, bool KCQ, int NQ, typename OUT>
+// Four columns of a result from `at` on, n of them there.  One load and one store where all four are, at any element's address.
+template <typename OUT> __device__ __forceinline__ void proj_put(const ProjParams& p, size_t at, int n, f32x4 v) {
+  typedef OUT vec __attribute__((ext_vector_type(4), aligned(sizeof(OUT))));
+  const OUT* add = static_cast<const OUT*>(p.add);
+  OUT* out = static_cast<OUT*>(p.out);
+  if (n >= 4) {
+    if (add) {
+      const vec a = *reinterpret_cast<const vec*>(add + at);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[x] += (float)a[x];
+    }
+    vec o;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o[x] = (OUT)v[x];
+    *reinterpret_cast<vec*>(out + at) = o;
+  } else {
+#pragma unroll
+    for (int x = 0; x < 3; ++x)
+      if (x < n) out[at + x] = (OUT)(add ? (float)add[at + x] + v[x] : v[x]);
+  }
+}
+
+// NP, NQ: pieces of a value of each side.  TN: columns of a tile, 128 or 32.  OUT: storage of the result of dx, void: partial sums in fp32.
+template <typename TP, bool KCP, int NP, typename TQ, bool KCQ, int NQ, int TN, typename OUT>
 __global__ __launch_bounds__(kProjThreads) void project_kernel(ProjParams p) {
-  constexpr int kStage = (NP + NQ) * kProjPiece, kOrder = NP > NQ ? NP : NQ;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * kStage];
+  constexpr int kOrder = NP > NQ ? NP : NQ, kPieceP = kProjTile * 128, kPieceQ = TN * 128;
+  constexpr int BI = TN == 128 ? 2 : 1, BJ = BI;                 // blocks of 32 x 32 of a wave
+  constexpr int kRow = 64 * 4 + 16, kRegion = 32 * kRow;
+  constexpr int kStage = NP * kPieceP + NQ * kPieceQ;
+  constexpr int kLds = !std::is_void<OUT>::value && kStage < 4 * kRegion ? 4 * kRegion : kStage;
+  __shared__ __attribute__((aligned(1024))) char smem[kLds];
   // the splits of a tile go to different dies, a split's tiles to the same ones: there its part of W stays in the L2
   int b = blockIdx.x;
   const int split = b % p.splits;
   b /= p.splits;
-  const int j0 = (b % p.tj) * kProjTile, i0 = (b / p.tj) * kProjTile;
+  const int j0 = (b % p.tj) * TN, i0 = (b / p.tj) * kProjTile;
   const int k0 = split * p.k_split, k_end = min(p.K, k0 + p.k_split);
-  const int lane = lane_id(), wave = threadIdx.x / kWave, wm = wave >> 1, wn = wave & 1, l32 = lane & 31, lh = lane >> 5;
+  const int lane = lane_id(), wave = threadIdx.x / kWave, l32 = lane & 31, lh = lane >> 5;
+  const int pr = TN == 128 ? (wave >> 1) * 64 : wave * 32, qr = TN == 128 ? (wave & 1) * 64 : 0;   // the wave's first row of each side
   const TP* P = static_cast<const TP*>(p.P);
   const TQ* Q = static_cast<const TQ*>(p.Q);
-  f32x16 acc[2][2];
+  f32x16 acc[BI][BJ];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < BI; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < BJ; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  ProjSide<TP, KCP> sp;
-  ProjSide<TQ, KCQ> sq;
+  ProjSide<TP, KCP, kProjTile> sp;
+  ProjSide<TQ, KCQ, TN> sq;
   sp.fetch(P, p.ld_p, p.rows, i0, k0, k_end);
   sq.fetch(Q, p.ld_q, p.cols, j0, k0, k_end);
-  int stage = 0;
   for (int k = k0; k < k_end; k += kProjK) {
-    char* lds = smem + stage * kStage;
-    sp.template store<NP>(lds);
-    sq.template store<NQ>(lds + NP * kProjPiece);
-    __syncthreads();                       // a wave is here only once it has read the stage of the step before
+    sp.template store<NP>(smem);
+    sq.template store<NQ>(smem + NP * kPieceP);
+    __syncthreads();
     if (k + kProjK < k_end) {
       sp.fetch(P, p.ld_p, p.rows, i0, k + kProjK, k_end);
       sq.fetch(Q, p.ld_q, p.cols, j0, k + kProjK, k_end);
     }
-    auto at = [&](int piece, int r, int ks) __attribute__((always_inline)) {
-      return *reinterpret_cast<const bf16x8*>(lds + piece * kProjPiece + r * 64 + (((ks * 2 + lh) ^ (r >> 1)) & 3) * 16);
-    };
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8 fp[2][NP], fq[2][NQ];
+    for (int ks = 0; ks < kProjK / 16; ++ks) {
+      bf16x8 fp[BI][NP], fq[BJ][NQ];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < BI; ++x) {
 #pragma unroll
-        for (int n = 0; n < NP; ++n) fp[x][n] = at(n, wm * 64 + x * 32 + l32, ks);
+        for (int n = 0; n < NP; ++n)
+          fp[x][n] = *reinterpret_cast<const bf16x8*>(smem + n * kPieceP + proj_chunk(pr + x * 32 + l32, ks * 2 + lh));
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) fq[x][n] = at(NP + n, wn * 64 + x * 32 + l32, ks);
+        for (int n = 0; n < NQ; ++n)
+          fq[x][n] = *reinterpret_cast<const bf16x8*>(smem + NP * kPieceP + n * kPieceQ + proj_chunk(qr + x * 32 + l32, ks * 2 + lh));
       }
       // smallest products first
 #pragma unroll
@@ -196,55 +226,90 @@ __global__ __launch_bounds__(kProjThreads) void project_kernel(ProjParams p) {
         for (int n = 0; n < NP; ++n)
           if (o - n >= 0 && o - n < NQ)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < BI; ++i)
 #pragma unroll
-              for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[j][o - n], fp[i][n], acc[i][j], 0, 0, 0);
+              for (int j = 0; j < BJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[j][o - n], fp[i][n], acc[i][j], 0, 0, 0);
     }
-    stage ^= 1;
+    __syncthreads();                       // every wave has read the stage
   }
   // lane: row l32 of each block, per q the columns 8 q + 4 lh .. + 3
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = i0 + wm * 64 + i * 32 + l32;
-    if (r >= p.rows) continue;
+  for (int i = 0; i < BI; ++i) {
+    const int r0 = i0 + pr + i * 32;
+    if constexpr (std::is_void<OUT>::value) {
+      const int r = r0 + l32;
+      if (r >= p.rows) continue;
+      float* dst = p.part + ((size_t)split * p.rows + r) * p.cols;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < BJ; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = j0 + wn * 64 + j * 32 + q * 8 + lh * 4;
-        const size_t at = (size_t)r * p.cols + c;
-        float v[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) v[x] = acc[i][j][q * 4 + x];
-        if constexpr (std::is_void<OUT>::value) {
-          float* dst = p.part + (size_t)split * p.rows * p.cols + at;
-          if (c + 4 <= p.cols) *reinterpret_cast<f32x4_any*>(dst) = f32x4_any{v[0], v[1], v[2], v[3]};
+        for (int q = 0; q < 4; ++q) {
+          const int c = j0 + qr + j * 32 + q * 8 + lh * 4;
+          if (c + 4 <= p.cols) *reinterpret_cast<f32x4_any*>(dst + c) = f32x4_any{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
           else
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              if (c + x < p.cols) dst[x] = v[x];
-        } else {
-          const OUT* add = static_cast<const OUT*>(p.add);
-          OUT* dst = static_cast<OUT*>(p.out);
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            if (c + x < p.cols) dst[at + x] = (OUT)(add ? (float)add[at + x] + v[x] : v[x]);
+            for (int x = 0; x < 3; ++x)
+              if (c + x < p.cols) dst[c + x] = acc[i][j][q * 4 + x];
         }
+    } else {                               // whole lines, by way of the wave's place in LDS
+      static_assert(std::is_void<OUT>::value || TN == 128, "64 columns of a wave");
+      char* region = smem + wave * kRegion;
+#pragma unroll
+      for (int j = 0; j < BJ; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          *reinterpret_cast<f32x4*>(region + l32 * kRow + (j * 32 + q * 8 + lh * 4) * 4) =
+              f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      const int c = j0 + qr + (lane & 15) * 4;
+#pragma unroll
+      for (int it = 0; it < 8; ++it) {
+        const int r = it * 4 + (lane >> 4);
+        const f32x4 v = *reinterpret_cast<const f32x4*>(region + r * kRow + (lane & 15) * 16);
+        if (r0 + r < p.rows && c < p.cols) proj_put<OUT>(p, (size_t)(r0 + r) * p.cols + c, p.cols - c, v);
       }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
   }
 }
 
-// out[i] = sum over the splits of part[split][i]: 64 values per workgroup, whose waves take every fourth split.
-__global__ __launch_bounds__(256) void project_join_kernel(const float* part, int splits, size_t n, float* out) {
-  __shared__ float s[4][kWave];
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
-  const size_t i = (size_t)blockIdx.x * kWave + lane;
+// out[i] = sum over the splits of part[split][i], n of them: 256 / PARTS values per workgroup, whose PARTS shares take every PARTS-th split
+// (eight loads at a time) and are added up in their order.
+template <int PARTS> __global__ __launch_bounds__(256) void project_join_kernel(const float* part, int splits, size_t n, float* out) {
+  constexpr int kValues = 256 / PARTS;
+  __shared__ float s[PARTS][kValues];
+  const int value = threadIdx.x % kValues, share = threadIdx.x / kValues;
+  const size_t i = (size_t)blockIdx.x * kValues + value;
   float v = 0.f;
   if (i < n)
-    for (int w = wave; w < splits; w += 4) v += part[(size_t)w * n + i];
-  s[wave][lane] = v;
+    for (int w = share; w < splits; w += 8 * PARTS) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = part[(size_t)min(w + u * PARTS, splits - 1) * n + i];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v += w + u * PARTS < splits ? x[u] : 0.f;
+    }
+  s[share][value] = v;
   __syncthreads();
-  if (wave == 0 && i < n) out[i] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
+  if (share == 0 && i < n) {
+    float t = s[0][value];
+#pragma unroll
+    for (int w = 1; w < PARTS; ++w) t += s[w][value];
+    out[i] = t;
+  }
+}
+
+// Few splits of many values: four at a time.
+__global__ __launch_bounds__(256) void project_join4_kernel(const float* part, int splits, size_t n4, float* out) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n4) return;
+  f32x4 v = reinterpret_cast<const f32x4*>(part)[i];
+  for (int w = 1; w < splits; ++w) v += reinterpret_cast<const f32x4*>(part)[(size_t)w * n4 + i];
+  reinterpret_cast<f32x4*>(out)[i] = v;
 }
 
 }  // namespace moe

@@ -26,10 +26,13 @@ int check(int T, int H, int E, int dtype) {
   return MOE_OK;
 }
 
+// Columns of a tile: 32 for up to as many experts.
+int tile_cols(int cols) { return cols <= 32 ? 32 : kProjTile; }
+
 // k's per workgroup and workgroups along k of a product of rows x cols over K.
 struct Split { int k, n; };
 Split split_of(int rows, int cols, int K) {
-  const long tiles = (long)ceil_div(rows, kProjTile) * ceil_div(cols, kProjTile);
+  const long tiles = (long)ceil_div(rows, kProjTile) * ceil_div(cols, tile_cols(cols));
   const int want = (int)std::max<long>(1, std::min<long>(kProjMaxSplits, kProjWorkgroups / std::max<long>(tiles, 1)));
   Split s;
   s.k = ceil_div(ceil_div(K, want), kProjK) * kProjK;
@@ -38,20 +41,31 @@ Split split_of(int rows, int cols, int K) {
 }
 size_t part_bytes(const Split& s, int rows, int cols) { return s.n > 1 ? (size_t)s.n * rows * cols * 4 : 0; }
 
-template <typename TP, bool KCP, int NP, typename TQ, bool KCQ, int NQ>
-int run_sums(ProjParams p, float* out, void* ws, hipStream_t s) {
+int join(const float* part, int splits, size_t n, float* out, hipStream_t s) {
+  if (splits > 0 && splits <= 8 && n % 4 == 0)
+    hipLaunchKernelGGL(project_join4_kernel, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, s, part, splits, n / 4, out);
+  else if (splits <= 16)
+    hipLaunchKernelGGL(project_join_kernel<4>, dim3((unsigned)((n + 63) / 64)), dim3(256), 0, s, part, splits, n, out);
+  else
+    hipLaunchKernelGGL(project_join_kernel<16>, dim3((unsigned)((n + 15) / 16)), dim3(256), 0, s, part, splits, n, out);
+  return launched();
+}
+
+template <typename TP, bool KCP, int NP, int NQ, int TN> int run_sums(ProjParams p, float* out, void* ws, hipStream_t s) {
   const Split sp = split_of(p.rows, p.cols, p.K);
   p.k_split = sp.k;
   p.splits = sp.n;
-  p.ti = ceil_div(p.rows, kProjTile);
-  p.tj = ceil_div(p.cols, kProjTile);
+  p.tj = ceil_div(p.cols, TN);
   p.part = sp.n > 1 ? static_cast<float*>(ws) : out;
-  hipLaunchKernelGGL((project_kernel<TP, KCP, NP, TQ, KCQ, NQ, void>), dim3((unsigned)p.ti * p.tj * p.splits), dim3(kProjThreads), 0, s, p);
-  if (sp.n > 1) {
-    const size_t n = (size_t)p.rows * p.cols;
-    hipLaunchKernelGGL(project_join_kernel, dim3((unsigned)((n + kWave - 1) / kWave)), dim3(256), 0, s, p.part, sp.n, n, out);
-  }
-  return launched();
+  hipLaunchKernelGGL((project_kernel<TP, KCP, NP, float, false, NQ, TN, void>), dim3((unsigned)ceil_div(p.rows, kProjTile) * p.tj * p.splits),
+                     dim3(kProjThreads), 0, s, p);
+  if (sp.n == 1) return launched();
+  return join(p.part, sp.n, (size_t)p.rows * p.cols, out, s);
+}
+// P in the storage type, k-contiguous or not, against fp32 row-contiguous.
+template <bool KCP> int run_sums(const ProjParams& p, int dtype, float* out, void* ws, hipStream_t s) {
+  if (p.cols <= 32) return dtype == MOE_BF16 ? run_sums<__bf16, KCP, 1, 3, 32>(p, out, ws, s) : run_sums<float, KCP, 3, 3, 32>(p, out, ws, s);
+  return dtype == MOE_BF16 ? run_sums<__bf16, KCP, 1, 3, 128>(p, out, ws, s) : run_sums<float, KCP, 3, 3, 128>(p, out, ws, s);
 }
 
 }  // namespace
@@ -79,8 +93,7 @@ int moe_router_project(int32_t T, int32_t H, int32_t E, int dtype, const void* d
   p.ld_p = H; p.ld_q = E;
   p.rows = T; p.cols = E; p.K = H;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  return dtype == MOE_BF16 ? run_sums<__bf16, true, 1, float, false, 3>(p, d_logits, d_workspace, s)
-                           : run_sums<float, true, 3, float, false, 3>(p, d_logits, d_workspace, s);
+  return run_sums<true>(p, dtype, d_logits, d_workspace, s);
 }
 
 int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, const float* d_dlogits, const void* d_x, const float* d_w,
@@ -91,9 +104,7 @@ int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, cons
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (T == 0) {
     if (!d_dw) return MOE_OK;
-    const size_t n = (size_t)H * E;        // sums over nothing
-    hipLaunchKernelGGL(project_join_kernel, dim3((unsigned)((n + kWave - 1) / kWave)), dim3(256), 0, s, (const float*)nullptr, 0, n, d_dw);
-    return launched();
+    return join(nullptr, 0, (size_t)H * E, d_dw, s);   // sums over nothing
   }
   if (!good(d_dlogits) || (d_dx && !good(d_w)) || (d_dw && !good(d_x))) return MOE_ERR_INVALID_ARG;
   if (d_dw) {
@@ -105,8 +116,7 @@ int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, cons
     p.P = d_x; p.Q = d_dlogits;
     p.ld_p = H; p.ld_q = E;
     p.rows = H; p.cols = E; p.K = T;
-    st = dtype == MOE_BF16 ? run_sums<__bf16, false, 1, float, false, 3>(p, d_dw, d_workspace, s)
-                           : run_sums<float, false, 3, float, false, 3>(p, d_dw, d_workspace, s);
+    st = run_sums<false>(p, dtype, d_dw, d_workspace, s);
     if (st != MOE_OK) return st;
   }
   if (d_dx) {
@@ -116,12 +126,11 @@ int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, cons
     p.rows = T; p.cols = H; p.K = E;
     p.k_split = ceil_div(E, kProjK) * kProjK;
     p.splits = 1;
-    p.ti = ceil_div(T, kProjTile);
     p.tj = ceil_div(H, kProjTile);
     p.add = d_dres; p.out = d_dx;
-    const dim3 grid((unsigned)((size_t)p.ti * p.tj));
-    if (dtype == MOE_BF16) hipLaunchKernelGGL((project_kernel<float, true, 2, float, true, 2, __bf16>), grid, dim3(kProjThreads), 0, s, p);
-    else hipLaunchKernelGGL((project_kernel<float, true, 3, float, true, 3, float>), grid, dim3(kProjThreads), 0, s, p);
+    const dim3 grid((unsigned)((size_t)ceil_div(T, kProjTile) * p.tj));
+    if (dtype == MOE_BF16) hipLaunchKernelGGL((project_kernel<float, true, 2, float, true, 2, 128, __bf16>), grid, dim3(kProjThreads), 0, s, p);
+    else hipLaunchKernelGGL((project_kernel<float, true, 3, float, true, 3, 128, float>), grid, dim3(kProjThreads), 0, s, p);
     st = launched();
   }
   return st;

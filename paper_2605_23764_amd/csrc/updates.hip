@@ -17,7 +17,7 @@ constexpr int kMaxSteps = 16;
 // Matrices are worked on in groups whose workspace stays below this, one at least: enough tiles at a time for the whole chip.
 constexpr size_t kNsGroupBytes = (size_t)4 << 30;
 constexpr int kNsMaxShares = 256;          // partial tiles of a product's remainder
-constexpr int kNsShareSteps = 4;           // K steps of a share, at least
+constexpr int kNsShareSteps = 4, kNsMaxSplits = 8;   // K steps of a share, at least; shares of a tile, at most
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool good(const void* p) { return p && aligned(p); }
@@ -118,7 +118,7 @@ template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGe
   auto grid = [](int n) { return dim3((unsigned)((n + 7) / 8 * 8)); };
   const int n_steps = p.K * (SPLIT ? 4 : 2) / 128, first = p.first, tiles = p.tiles;
   const int rest = tiles % cus;
-  p.splits = rest ? std::min(std::min(cus, kNsMaxShares) / rest, n_steps / kNsShareSteps) : 0;
+  p.splits = rest ? std::min({std::min(cus, kNsMaxShares) / rest, n_steps / kNsShareSteps, kNsMaxSplits}) : 0;
   if (p.splits < 2) p.splits = 0;
   p.tiles = p.splits ? tiles - rest : tiles;
   if (p.tiles > 0) {
