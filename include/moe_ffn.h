@@ -423,16 +423,18 @@ typedef struct MoeScores {
  *   the topk_group groups stay whose best key + second best key are largest (ties: the lowest group), of their experts the k
  *   with the largest keys are selected, in that order (ties: the lowest expert), and
  *   topk_w[t,j] = scale * s[t,e_j] / (renormalize ? sum over the selected of s : 1),  0 / 0 = 0
- * Scores and keys are computed in 64 bits, so that the selection is that of the definition; the weights are rounded once.  The bias
- * takes part in the selection alone.  A logit of NaN counts as -inf, as in moe_route.  An expert whose logit is -inf (or whose key is
- * NaN) comes behind all others, with weight 0 where it is selected all the same (logit -inf); in a group's score it counts 0 beside a
- * living one.  Several logits of +inf share a softmax's probability evenly.
+ * Scores are computed in 64 bits; keys and groups' sums of them are rounded to 44 and compared (roundings to fp32 would decide between
+ * near ones); the weights are rounded once.  The bias takes part in the selection alone.  A logit of NaN counts as -inf, as in moe_route.  An expert whose logit or key is
+ * -inf (or whose key is NaN) comes behind all others, with weight 0 where it is selected all the same (logit -inf); in a group's score
+ * it counts 0 beside a living one.  Several logits of +inf share a softmax's probability evenly.  Keys beyond +-1e300 are equal.
  *   d_logits [T,E] f32;  d_bias [E] f32 or NULL: 0
  *   saved, d_workspace   filled as by moe_route: moe_dispatch_to_combine, moe_dispatch_to_combine_w4 or the stage entry points
  *                        follow, then moe_ffn_backward, and moe_route_scores_backward on its d_dtopk_w
+ *   mode     MoeMode of the moe_dispatch_to_combine that follows.  MOE_MODE_SERIALIZED leaves the tile scheduler's counters and task
+ *            tables out (nobody reads them then), as moe_ffn_forward's routing does: a MOE_MODE_PERSISTENT call may not follow
  */
 int moe_route_scores(const MoeShape* shape, const MoeScores* scores, const float* d_logits, const float* d_bias,
-                     const MoeSaved* saved, void* d_workspace, size_t workspace_bytes, void* stream);
+                     const MoeSaved* saved, void* d_workspace, size_t workspace_bytes, int mode, void* stream);
 
 /*
  * The gradient of its logits: d topk_w / d logits (the selection and the bias carry none) applied to dtopk_w, plus dadd.

@@ -63,7 +63,7 @@ _BLOCK_ARGS = {
     "moe_dropout_add_layer_norm_forward": "iiippfpppf" "ppppp", "moe_dropout_add_layer_norm_backward": "iiipppppp" "fpppppp" "zp",
     "moe_balance_workspace_bytes": "iip", "moe_balance_forward": "iiipppf" "ppppzp", "moe_router_backward": "iiippppp" "fpppp",
     "moe_quantize_w4": "iiiipppp", "moe_ffn_forward_w4": "ppppppppppzp", "moe_dispatch_to_combine_w4": "pppppppppzp",
-    "moe_route_scores": "ppppppzp", "moe_route_scores_backward": "iiipppppp" "p", "moe_bias_update": "ipfppp",
+    "moe_route_scores": "ppppppzip", "moe_route_scores_backward": "iiipppppp" "p", "moe_bias_update": "ipfppp",
     "moe_router_project_workspace_bytes": "iiip", "moe_router_project": "iiiippppzp", "moe_router_project_backward": "iiiippppppp" "zp",
     "moe_muon_workspace_bytes": "iiiip", "moe_orthogonalize": "iiiipipfp" "pzp", "moe_muon_step": "iiiippppfifffipfpp" "pzp",
 }
@@ -570,13 +570,14 @@ def make_scores(score="sigmoid", n_group: int = 1, topk_group: int = 1, renormal
     return _MoeScores(score, n_group, topk_group, int(renormalize), scale)
 
 
-def moe_route_scores(shape, scores, logits, bias, saved: Saved, workspace, stream=None) -> None:
-    """moe_route by scores: fills the routing results of `saved` and the workspace; bias [E] or None."""
+def moe_route_scores(shape, scores, logits, bias, saved: Saved, workspace, mode: int = MODE_SERIALIZED, stream=None) -> None:
+    """moe_route by scores: fills the routing results of `saved` and the workspace; bias [E] or None.  mode: that of the
+    moe_dispatch_to_combine that follows."""
     sv = saved.c_struct()
     logits, = _args((shape.T, shape.E), torch.float32, "logits", logits)
     bias, = _args((shape.E,), torch.float32, "bias", bias)
     ws, wb = _workspace(workspace)
-    _check(load_library().moe_route_scores(ctypes.addressof(shape), ctypes.addressof(scores), logits, bias, ctypes.addressof(sv), ws, wb,
+    _check(load_library().moe_route_scores(ctypes.addressof(shape), ctypes.addressof(scores), logits, bias, ctypes.addressof(sv), ws, wb, mode,
                                            _raw_stream(stream)), "moe_route_scores")
 
 

@@ -823,18 +823,19 @@ int moe_route(const MoeShape* shape, const float* d_logits, const MoeSaved* save
 }
 
 int moe_route_scores(const MoeShape* shape, const MoeScores* scores, const float* d_logits, const float* d_bias, const MoeSaved* saved,
-                     void* d_workspace, size_t workspace_bytes, void* stream) {
+                     void* d_workspace, size_t workspace_bytes, int mode, void* stream) {
   Ctx c;
   int st = check_shape(shape);
   if (st != MOE_OK || (st = check_scores(scores, shape->E, shape->k)) != MOE_OK) return st;
+  if (mode != MOE_MODE_SERIALIZED && mode != MOE_MODE_PERSISTENT) return MOE_ERR_INVALID_ARG;
   st = make_ctx(c, shape, saved, d_workspace, workspace_bytes, stream);
   if (st != MOE_OK || c.s.T == 0) return st;
   if (!d_logits || !aligned16(d_logits) || !aligned16(d_bias) || !saved) return MOE_ERR_INVALID_ARG;
   ScoreParams sc;
   sc.bias = d_bias;
   sc.sigmoid = scores->score == MOE_SCORE_SIGMOID; sc.renorm = scores->renormalize; sc.scale = scores->scale;
-  sc.n_group = scores->n_group; sc.topk_group = scores->topk_group; sc.per_group = c.s.E / scores->n_group;
-  return run_route(c, d_logits, true, nullptr, nullptr, &sc);
+  sc.n_group = scores->n_group; sc.topk_group = scores->topk_group; sc.per_group = c.s.E / scores->n_group; sc.group_mul = 65536 / sc.per_group + 1;
+  return run_route(c, d_logits, mode == MOE_MODE_PERSISTENT, nullptr, nullptr, &sc);
 }
 
 int moe_permute(const MoeShape* shape, const void* d_x, const MoeSaved* saved, void* d_workspace,

@@ -462,13 +462,13 @@ template <bool GROUPS>
 __global__ __launch_bounds__(512) void route_scores_kernel(RouteParams p, ScoreParams sc) {
   __shared__ int32_t s_idx[kSub * kMaxK];
   __shared__ float s_val[kSub * kMaxK];
-  __shared__ uint64_t s_keys[GROUPS ? 512 / kWave * kRouteTokensPerWave * kMaxE : 1];
-  route_chunk(p, blockIdx.x, s_idx, s_val, SelectScores<GROUPS>{sc, s_keys});
+  __shared__ double s_slots[512 / kWave * kSlotWords];
+  route_chunk(p, blockIdx.x, s_idx, s_val, SelectScores<GROUPS>{sc, s_slots});
 }
 template <bool BF16, bool GROUPS>
 __global__ __launch_bounds__(kRouteOneThreads) void route_scores_one_kernel(SchedParams<BF16> sp, ScoreParams sc) {
-  __shared__ uint64_t s_keys[GROUPS ? kRouteOneT * kMaxE : 1];
-  route_one_launch(sp, SelectScores<GROUPS>{sc, s_keys});
+  __shared__ double s_slots[kRouteOneThreads / kWave * kSlotWords];
+  route_one_launch(sp, SelectScores<GROUPS>{sc, s_slots});
 }
 
 // SCATTER (bf16): GEMM-2 tiles add their weighted rows into the zeroed layer output from their epilogue

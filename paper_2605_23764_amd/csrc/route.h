@@ -38,6 +38,9 @@ struct SelectLogits {
   __device__ __forceinline__ void operator()(const RouteParams& p, int t_first, int lane, uint32_t (&key)[KP], int32_t* s_idx, float* s_val) const {
     route_select(p, t_first, lane, key, s_idx, s_val);
   }
+  __device__ __forceinline__ void few(const RouteParams& p, int wave, int lane, int32_t* s_idx, float* s_val) const {
+    select_four(p, wave, lane, s_idx, s_val, *this);
+  }
 };
 
 // One sub-chunk of kSub tokens by a workgroup (a wave routes four tokens per pass;
@@ -361,13 +364,7 @@ __device__ __forceinline__ void route_one(const RouteParams& p, const SELECT& se
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   for (int e = threadIdx.x; e < p.E_local; e += blockDim.x) s_mask[e] = 0ull;
-  const int t0 = wave * kRouteTokensPerWave;
-  if (t0 < p.T)
-    with_route_keys(p.E, [&](auto kp) __attribute__((always_inline)) {
-      uint32_t key[decltype(kp)::value];
-      route_load(p, t0, lane, key);
-      select(p, t0, lane, key, s_idx + t0 * kMaxK, s_val + t0 * kMaxK);
-    });
+  select.few(p, wave, lane, s_idx, s_val);
   __syncthreads();
   // the local expert of slot j of token `lane`, or -1
   auto local_of = [&](int j) __attribute__((always_inline)) {

@@ -7,7 +7,14 @@
 //
 // Scores, keys and weights are in 64 bits: between two experts whose keys differ by less than a rounding to 32 bits, the rounding would
 // decide, and with a bias the order of the logits does not (8192 tokens of 256 experts have a few such pairs; every implementation would
-// select others).  Weights are rounded once.
+// select others).  Weights are rounded once.  Keys, and groups' sums of them, are rounded to 44 bits, and the lowest 8 are the expert's number, so
+// that one maximum finds the key, the expert and the lowest of equals.
+//
+// Bound by instructions, and where a wave has few tokens by fetching them: a line of eight that no wave has run yet costs some 300 clocks, so
+// what is done per expert is a loop on the token's keys in LDS where a lane has more than four (all unrolled: T = 8192, 256 experts
+// 41 us, T = 64 61; this: MEASURED).  A token takes 16 lanes; each lane sorts its experts' keys (a network of maxima and minima), and a
+// round of the selection is a maximum over the lanes' first keys, behind which the winner's move up.  Up to 16 tokens, a wave to each, take
+// all 64 lanes.
 #pragma once
 #include "route_select.h"
 #include "scores_math.h"
@@ -19,149 +26,221 @@ constexpr int kMaxGroups = 16;             // a lane of the token's row to a gro
 struct ScoreParams {
   const float* bias;     // [E] or null
   int sigmoid;           // 0: softmax
-  int n_group, topk_group, per_group;
+  int n_group, topk_group, per_group, group_mul;   // (e * group_mul) >> 16 = e / per_group for e < 256
   int renorm;
   float scale;
 };
 
-// Monotone map double -> uint64, NaN as -inf; every value's key is above 0.
-__device__ __forceinline__ uint64_t double_order_key(double v) {
-  if (v != v) v = -__builtin_huge_val();
-  const uint64_t u = __builtin_bit_cast(uint64_t, v == 0.0 ? 0.0 : v);
-  return (u >> 63) ? ~u : (u | (1ull << 63));
+// A key, rounded to 44 bits, with its number n below 256 in the lowest 8: larger keys are larger, and of equal ones those with the lower number.
+// (Rounded, not cut off: two scores that add up to 1 do so still.)
+constexpr double kKeyDead = -1e301;        // an expert that comes behind all others, a group without a living one
+constexpr double kKeyNone = -1e308;        // nothing there
+__device__ __forceinline__ double key_with(double v, int n) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v) + 128;
+  const uint32_t hi = (uint32_t)(u >> 32);
+  const uint32_t low = (int32_t)hi < 0 ? (uint32_t)n : 255u - (uint32_t)n;
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | (((uint32_t)u & ~255u) | low));
 }
-__device__ __forceinline__ double double_from_order_key(uint64_t k) {
-  return __builtin_bit_cast(double, (k >> 63) ? k & ~(1ull << 63) : ~k);
+__device__ __forceinline__ int key_number(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const int low = (int)(u & 255u);
+  return (int32_t)(u >> 32) < 0 ? low : 255 - low;
 }
+__device__ __forceinline__ double key_without(double v) { return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, v) & ~255ull); }
 
-// Over the 16 lanes of a DPP row, in all of them.
-template <typename OP> __device__ __forceinline__ uint64_t row_reduce_u64(uint64_t v, OP op) {
+// Over the LPT lanes of a token, in all of them.
+template <int LPT, typename OP> __device__ __forceinline__ double lanes_reduce(double v, OP op) {
 #define MOE_STEP(ctrl)                                                                                                          \
   {                                                                                                                             \
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, ctrl, 0xf, 0xf, false);                      \
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), ctrl, 0xf, 0xf, false);              \
-    v = op(v, (uint64_t)hi << 32 | lo);                                                                                         \
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);                                                                         \
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, ctrl, 0xf, 0xf, false);                      \
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), ctrl, 0xf, 0xf, false);              \
+    v = op(v, __builtin_bit_cast(double, (uint64_t)hi << 32 | lo));                                                             \
   }
   MOE_STEP(0xB1) MOE_STEP(0x4E) MOE_STEP(0x141) MOE_STEP(0x140)
 #undef MOE_STEP
+  if constexpr (LPT == 64) {
+    auto join = [&](auto a, auto b) __attribute__((always_inline)) {
+      v = op(__builtin_bit_cast(double, (uint64_t)(uint32_t)b[0] << 32 | (uint32_t)a[0]), __builtin_bit_cast(double, (uint64_t)(uint32_t)b[1] << 32 | (uint32_t)a[1]));
+    };
+    uint64_t u = __builtin_bit_cast(uint64_t, v);
+    join(__builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false), __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
+    u = __builtin_bit_cast(uint64_t, v);
+    join(__builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
+  }
   return v;
 }
-__device__ __forceinline__ uint64_t row_max_u64(uint64_t v) {
-  return row_reduce_u64(v, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+template <int LPT> __device__ __forceinline__ double lanes_max(double v) {
+  return lanes_reduce<LPT>(v, [](double a, double b) { return __builtin_fmax(a, b); });
 }
-__device__ __forceinline__ double row_sum_f64(double v) {
-  return __builtin_bit_cast(double, row_reduce_u64(__builtin_bit_cast(uint64_t, v), [](uint64_t a, uint64_t b) {
-    return __builtin_bit_cast(uint64_t, __builtin_bit_cast(double, a) + __builtin_bit_cast(double, b));
-  }));
+template <int LPT> __device__ __forceinline__ double lanes_sum(double v) {
+  return lanes_reduce<LPT>(v, [](double a, double b) { return a + b; });
 }
 
-// Four tokens by one wave, one per 16-lane row, as route_select; the keys of the wave's tokens also stand in LDS, where a lane per group
-// finds the group's two best (s_keys: 4 E words, used with more than one group).
-template <int KP, bool GROUPS>
-__device__ __forceinline__ void route_scores_select(const RouteParams& p, const ScoreParams& sc, int t_first, int lane, const uint32_t (&order)[KP],
-                                                    int32_t* s_idx, float* s_val, uint64_t* s_keys) {
-  const int row = lane >> 4, s = lane & 15, e0 = s * KP;
-  float l[KP];
+// Descending, by Batcher's odd-even merges (Batcher, 1968).
+template <int N> __device__ __forceinline__ void sort_keys(double (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < KP; ++i) l[i] = order[i] ? float_from_order_key(order[i]) : -__builtin_huge_valf();   // 0: no expert there
-  float m = 0.f;
-  double inv = 1.0;
-  if (!sc.sigmoid) {
-    uint32_t top = order[0];
+  for (int p = 1; p < N; p *= 2)
 #pragma unroll
-    for (int i = 1; i < KP; ++i) top = order[i] > top ? order[i] : top;
-    m = float_from_order_key(row_max_u32(top));
-    double sum = 0.0;
+    for (int k = p; k >= 1; k /= 2)
 #pragma unroll
-    for (int i = 0; i < KP; ++i) sum += exp_below(l[i], m);
-    sum = row_sum_f64(sum);
-    inv = sum > 0.0 ? 1.0 / sum : 0.0;
-  }
-  auto score = [&](float v) __attribute__((always_inline)) { return sc.sigmoid ? sigmoid64(v) : exp_below(v, m) * inv; };
-  uint64_t key[KP];
+      for (int j = k % p; j + k < N; j += 2 * k)
 #pragma unroll
-  for (int i = 0; i < KP; ++i) {
-    const double b = sc.bias && e0 + i < p.E ? (double)sc.bias[e0 + i] : 0.0;
-    const double v = l[i] == -__builtin_huge_valf() ? -__builtin_huge_val() : score(l[i]) + b;
-    key[i] = e0 + i < p.E ? double_order_key(v) : 0ull;
-  }
-  if constexpr (GROUPS) {
-    uint64_t* mine = s_keys + row * p.E;
-#pragma unroll
-    for (int i = 0; i < KP; ++i)
-      if (e0 + i < p.E) mine[e0 + i] = key[i];
+        for (int i = 0; i < k; ++i)
+          if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            const double a = v[i + j], b = v[i + j + k];
+            v[i + j] = __builtin_fmax(a, b);
+            v[i + j + k] = __builtin_fmin(a, b);
+          }
+}
+
+// 64 / LPT tokens by one wave, LPT lanes to each, KP experts to a lane; l: the logits of the lane's, -inf where there is none.
+// slots: the wave's kSlotWords (a token by itself has those of all).
+constexpr int kSlotWords = kRouteTokensPerWave * (kMaxE + 16);
+template <int LPT, int KP, bool GROUPS>
+__device__ __forceinline__ void route_scores_select(const RouteParams& p, const ScoreParams& sc, int t_first, int lane, const float (&l)[KP],
+                                                    int32_t* s_idx, double* slots) {
+  constexpr int kUnroll = KP <= 4 ? KP : 1;
+  const int row = lane / LPT, s = lane % LPT, e0 = s * KP, n = p.E - e0, tok = t_first + row;
+  const float none = -__builtin_huge_valf();
+  double* mine = slots + row * (kSlotWords / kRouteTokensPerWave);
+  auto at = [](int e) __attribute__((always_inline)) { return e + e / KP; };   // a word beside each lane's, so that the lanes' lie in all banks
+  auto settled = []() __attribute__((always_inline)) {           // a wave's LDS accesses, seen by its other lanes
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    uint64_t group = 0;                                          // of group s; 0: no such group
-    if (s < sc.n_group) {
-      uint64_t best = 0, second = 0;
-      int at = s;                                                // lanes start at different banks
-      while (at >= sc.per_group) at -= sc.per_group;
-      for (int i = 0; i < sc.per_group; ++i) {
-        const uint64_t v = mine[s * sc.per_group + at];
-        second = v > best ? best : (v > second ? v : second);
-        best = v > best ? v : best;
-        at = at + 1 == sc.per_group ? 0 : at + 1;
-      }
-      const double b1 = double_from_order_key(best), b2 = second ? double_from_order_key(second) : 0.0;
-      group = double_order_key(b1 + (b2 == -__builtin_huge_val() ? 0.0 : b2));
-    }
-    uint32_t keep = 0;
-    for (int j = 0; j < sc.topk_group; ++j) {
-      const uint64_t best = row_max_u64(group);
-      const int first = __builtin_ctz((uint32_t)(__ballot(group == best) >> (row * 16)) & 0xFFFFu);
-      keep |= 1u << first;
-      if (s == first) group = 0;
-    }
-    int g = e0 / sc.per_group, left = (g + 1) * sc.per_group - e0;
+  };
+  float m = none;
 #pragma unroll
+  for (int i = 0; i < KP; ++i) {
+    m = __builtin_fmaxf(m, l[i]);
+    mine[at(e0) + i] = (double)l[i];                             // also where the lane has no expert: -inf, in the token's words
+  }
+  // scores, -1 for the dead; softmax: not yet over their sum
+  double inv = 1.0;
+  if (sc.sigmoid) {
+#pragma unroll kUnroll
     for (int i = 0; i < KP; ++i) {
-      if (!((keep >> g) & 1)) key[i] = 0;
-      if (--left == 0) { ++g; left = sc.per_group; }
+      const float v = (float)mine[at(e0) + i];
+      mine[at(e0) + i] = v == none ? -1.0 : sigmoid64(v);
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");       // the next four tokens' keys go to the same place
-    __builtin_amdgcn_wave_barrier();
+  } else {
+    m = (float)lanes_max<LPT>((double)m);
+    double sum = 0.0;
+#pragma unroll kUnroll
+    for (int i = 0; i < KP; ++i) {
+      const float v = (float)mine[at(e0) + i];
+      const double t = exp_below(v, m);
+      sum += t;
+      mine[at(e0) + i] = v == none ? -1.0 : t;
+    }
+    sum = lanes_sum<LPT>(sum);
+    inv = sum > 0.0 ? reciprocal64(sum) : 0.0;                   // a living row's sum is 1 .. E
   }
+  // keys
+  float next = sc.bias ? sc.bias[min(e0, p.E - 1)] : 0.f;
+#pragma unroll kUnroll
+  for (int i = 0; i < KP; ++i) {
+    const float b = next;
+    if (sc.bias) next = sc.bias[min(e0 + i + 1, p.E - 1)];
+    const double t = mine[at(e0) + i];
+    double v = __builtin_fmax(__builtin_fmin(t * inv + (double)b, 1e300), -1e300);
+    v = t < 0.0 || b != b || b == none ? kKeyDead : v;
+    mine[at(e0) + i] = key_with(v, e0 + i);
+  }
+  settled();
+  uint32_t keep = ~0u;
+  if constexpr (GROUPS) {
+    double group = kKeyNone;                                     // of group s
+    if (s < sc.n_group) {
+      double best = kKeyNone, second = kKeyNone;
+      int e = s * sc.per_group;
+#pragma unroll 2
+      for (int i = 0; i < sc.per_group; ++i, ++e) {
+        const double v = mine[at(e)];
+        second = __builtin_fmax(second, __builtin_fmin(best, v));
+        best = __builtin_fmax(best, v);
+      }
+      // a key's own number is gone from the sum; kKeyDead stays below every living group
+      group = best < -1e300 ? kKeyDead : key_without(best) + (second < -1e300 ? 0.0 : key_without(second));
+      group = key_with(group, s);
+    }
+    keep = 0;
+    for (int j = 0; j < sc.topk_group; ++j) {
+      const double best = lanes_max<LPT>(group);
+      keep |= 1u << key_number(best);
+      if (group == best) group = kKeyNone;
+    }
+  }
+  double key[KP];
+#pragma unroll
+  for (int i = 0; i < KP; ++i) {
+    const double v = mine[at(e0) + i];
+    const bool stays = !GROUPS || ((keep >> (((uint32_t)(e0 + i) * (uint32_t)sc.group_mul) >> 16)) & 1);
+    key[i] = i < n && stays ? v : kKeyNone;
+  }
+  sort_keys(key);
+  double chosen = kKeyNone;                                      // of slot s
   for (int j = 0; j < p.k; ++j) {
-    uint64_t local = key[0];
-    float val = l[0];
-    int li = 0;
+    const double best = lanes_max<LPT>(key[0]);
+    chosen = s == j ? best : chosen;
+    const bool winner = key[0] == best;
+    double up = kKeyNone;
 #pragma unroll
-    for (int i = 1; i < KP; ++i)
-      if (key[i] > local) { local = key[i]; val = l[i]; li = i; }
-    const uint64_t best = row_max_u64(local);
-    const uint32_t in_row = (uint32_t)(__ballot(local == best) >> (row * 16)) & 0xFFFFu;
-    const bool winner = s == __builtin_ctz(in_row);
-#pragma unroll
-    for (int i = 0; i < KP; ++i)
-      if (winner && i == li) key[i] = 0;
-    if (winner) {
-      s_idx[row * kMaxK + j] = e0 + li;
-      s_val[row * kMaxK + j] = val;
+    for (int i = KP - 1; i >= 0; --i) {
+      double v = key[i];
+      asm("" : "+v"(v));                                         // as a value: a choice between two places of the array becomes one by number
+      key[i] = winner ? up : v;
+      up = v;
     }
   }
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  const int t = t_first + row;
   const bool slot = s < p.k;
-  const int idx = slot ? s_idx[row * kMaxK + s] : 0;
-  const double ps = slot ? score(s_val[row * kMaxK + s]) : 0.0;
-  const double sum = row_sum_f64(ps);
-  if (t < p.T && slot) {
-    p.topk_idx[(size_t)t * p.k + s] = idx;
-    p.topk_w[(size_t)t * p.k + s] = (float)((double)sc.scale * (sc.renorm ? (sum > 0.0 ? ps / sum : 0.0) : ps));
+  const int idx = slot ? key_number(chosen) : 0;
+  if (slot) s_idx[row * kMaxK + s] = idx;
+  float val = p.logits[(size_t)min(tok, p.T - 1) * p.E + idx];
+  if (!slot || val != val) val = none;
+  const double ps = sc.sigmoid ? sigmoid64(val) : exp_below(val, m) * inv;
+  const double sum = lanes_sum<LPT>(slot ? ps : 0.0);
+  if (tok < p.T && slot) {
+    p.topk_idx[(size_t)tok * p.k + s] = idx;
+    p.topk_w[(size_t)tok * p.k + s] = (float)((double)sc.scale * (sc.renorm ? (sum > 0.0 ? ps / sum : 0.0) : ps));
   }
+  settled();                                                     // the next tokens' go to the same places
 }
 
-// The selection as route_chunk and route_one call it.  s_keys: the workgroup's, 4 kMaxE words per wave.
+// The selection as route_chunk and route_one call it.  s_slots: the workgroup's, kSlotWords per wave.
 template <bool GROUPS> struct SelectScores {
   const ScoreParams& sc;
-  uint64_t* s_keys;
+  double* s_slots;
+  __device__ __forceinline__ double* slots() const { return s_slots + (threadIdx.x / kWave) * kSlotWords; }
   template <int KP>
-  __device__ __forceinline__ void operator()(const RouteParams& p, int t_first, int lane, uint32_t (&key)[KP], int32_t* s_idx, float* s_val) const {
-    route_scores_select<KP, GROUPS>(p, sc, t_first, lane, key, s_idx, s_val, s_keys + (threadIdx.x / kWave) * (kRouteTokensPerWave * kMaxE));
+  __device__ __forceinline__ void operator()(const RouteParams& p, int t_first, int lane, uint32_t (&order)[KP], int32_t* s_idx, float*) const {
+    float l[KP];
+#pragma unroll
+    for (int i = 0; i < KP; ++i) l[i] = order[i] ? float_from_order_key(order[i]) : -__builtin_huge_valf();   // 0: no expert there
+    route_scores_select<16, KP, GROUPS>(p, sc, t_first, lane, l, s_idx, slots());
+  }
+  // All tokens of a launch of up to 64, by its 16 waves: a wave to a token as long as there are as many.
+  __device__ __forceinline__ void few(const RouteParams& p, int wave, int lane, int32_t* s_idx, float* s_val) const {
+    if (p.T > kRouteFewWaves) {
+      select_four(p, wave, lane, s_idx, s_val, *this);
+      return;
+    }
+    if (wave >= p.T) return;
+    auto one = [&](auto kp) __attribute__((always_inline)) {
+      constexpr int KP = decltype(kp)::value;
+      float l[KP];
+#pragma unroll
+      for (int i = 0; i < KP; ++i) {
+        const int e = lane * KP + i;
+        l[i] = p.logits[(size_t)wave * p.E + min(e, p.E - 1)];
+        if (e >= p.E || l[i] != l[i]) l[i] = -__builtin_huge_valf();
+      }
+      route_scores_select<64, KP, GROUPS>(p, sc, wave, lane, l, s_idx + wave * kMaxK, slots());
+    };
+    if (p.E <= 64) one(std::integral_constant<int, 1>{});
+    else if (p.E <= 128) one(std::integral_constant<int, 2>{});
+    else one(std::integral_constant<int, 4>{});
   }
 };
 

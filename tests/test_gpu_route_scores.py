@@ -23,7 +23,7 @@ def _logits(T, E, seed):
     return (1.5 * r.normal(size=(T, E)) + 0.5 * r.normal(size=E)).astype(np.float32), r
 
 
-def _route(logits, scores, bias, k, E_local, base, dtype=torch.bfloat16):
+def _route(logits, scores, bias, k, E_local, base, dtype=torch.bfloat16, mode=moe.MODE_SERIALIZED):
     T, E = logits.shape
     shape = moe.make_shape(T, 64, 64, E, E_local, base, k, dtype)
     saved, ws = moe.alloc_saved(shape, keep_xp=False), moe.alloc_workspace(shape)
@@ -31,7 +31,7 @@ def _route(logits, scores, bias, k, E_local, base, dtype=torch.bfloat16):
         t.fill_(-7)
     saved.topk_w.fill_(float("nan"))
     ws.fill_(255)
-    moe.moe_route_scores(shape, scores, logits, bias, saved, ws)
+    moe.moe_route_scores(shape, scores, logits, bias, saved, ws, mode)
     return shape, saved, ws
 
 
@@ -56,8 +56,8 @@ def test_selection_tables_weights_and_gradient(T, E, k, G, top, El, base, kind, 
     logits = torch.from_numpy(L).cuda()
     dev_bias = None if bias is None else torch.from_numpy(bias).cuda()
     idx, s = ro.select(L, kind, k, bias, G, top)
-    for dtype in (torch.bfloat16, torch.float32):
-        shape, saved, ws = _route(logits, scores, dev_bias, k, El, base, dtype)
+    for dtype, mode in ((torch.bfloat16, moe.MODE_SERIALIZED), (torch.float32, moe.MODE_SERIALIZED), (torch.bfloat16, moe.MODE_PERSISTENT)):
+        shape, saved, ws = _route(logits, scores, dev_bias, k, El, base, dtype, mode)
         np.testing.assert_array_equal(saved.topk_idx.cpu().numpy(), idx)
         _check_tables(saved, idx, El, base)
         w = ro.weights(s, idx, renorm, 2.5)
@@ -202,7 +202,7 @@ def test_layer_behind_it(T, mode):
     shape = moe.make_shape(T, H, I, E, El, base, k, torch.bfloat16)
     saved, ws, out = moe.alloc_saved(shape), moe.alloc_workspace(shape), torch.empty_like(x)
     scores = moe.make_scores("sigmoid", 4, 2, True, 2.0)
-    moe.moe_route_scores(shape, scores, torch.from_numpy(L).cuda(), torch.from_numpy(bias).cuda(), saved, ws)
+    moe.moe_route_scores(shape, scores, torch.from_numpy(L).cuda(), torch.from_numpy(bias).cuda(), saved, ws, mode)
     moe.moe_dispatch_to_combine(shape, x, w1, w2, out, saved, ws, mode)
     torch.cuda.synchronize()
     assert moe.moe_ffn_last_status(shape, ws) == 0

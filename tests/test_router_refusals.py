@@ -32,16 +32,16 @@ BAD_SCORES = [(INVALID, dict(score=2)), (INVALID, dict(score=-1)), (INVALID, dic
               (SHAPE, dict(n_group=32)), (SHAPE, dict(topk_group=0)), (SHAPE, dict(topk_group=5)), (SHAPE, dict(n_group=8, topk_group=1))]
 
 
-def route(lib, scores=None, shape=(100, 64, 64, 32, 16, 8, 5, moe.MOE_BF16), logits=at(1), bias=at(2), saved=True, ws=at(3), size=1 << 30, **change):
+def route(lib, scores=None, shape=(100, 64, 64, 32, 16, 8, 5, moe.MOE_BF16), logits=at(1), bias=at(2), saved=True, ws=at(3), size=1 << 30, mode=0, **change):
     s = moe.make_shape(*shape)
     sc = moe.make_scores(**{**SCORES, **(scores or {})})
     sv = _MoeSaved(*(change.get(n, at(10 + i)) for i, (n, _) in enumerate(_MoeSaved._fields_)))
     return lib.moe_route_scores(ctypes.addressof(s), ctypes.addressof(sc) if scores is not False else None, logits, bias,
-                                ctypes.addressof(sv) if saved else None, ws, size, None)
+                                ctypes.addressof(sv) if saved else None, ws, size, mode, None)
 
 
 @pytest.mark.parametrize("want,change", [
-    *[(w, dict(scores=c)) for w, c in BAD_SCORES], (INVALID, dict(scores=False)), (INVALID, dict(logits=None)), (INVALID, dict(logits=at(1, 8))),
+    *[(w, dict(scores=c)) for w, c in BAD_SCORES], (INVALID, dict(scores=False)), (INVALID, dict(mode=2)), (INVALID, dict(mode=-1)), (INVALID, dict(logits=None)), (INVALID, dict(logits=at(1, 8))),
     (INVALID, dict(bias=at(2, 4))), (INVALID, dict(saved=False)), (INVALID, dict(topk_w=None)), (INVALID, dict(row_of=at(9, 4))),
     (INVALID, dict(ws=None)), (INVALID, dict(ws=at(3, 8))), (SMALL, dict(size=16)), (SHAPE, dict(shape=(100, 64, 64, 320, 16, 8, 5, 1))),
     (SHAPE, dict(shape=(-1, 64, 64, 32, 16, 8, 5, 1))), (SHAPE, dict(shape=(100, 64, 64, 32, 16, 20, 5, 1)))])
