@@ -468,8 +468,8 @@ int moe_router_project(int32_t T, int32_t H, int32_t E, int dtype, const void* d
 /*
  * dx = dres + dlogits W^T, dW = x^T dlogits
  *   d_dres  [T,H] dtype, NULL: 0.  What reaches x beside the router (the layer's d_dx); may be d_dx
- *   d_dx    [T,H] dtype, NULL: not computed (d_w may then be NULL); may be d_x.  d_dw [H,E] f32, NULL: not computed (d_x and
- *           d_workspace may then be NULL); with T == 0 it is zeroed
+ *   d_dx    [T,H] dtype, NULL: not computed (d_w may then be NULL); may be d_x
+ *   d_dw    [H,E] f32, NULL: not computed (d_x may then be NULL); with T == 0 it is zeroed
  */
 int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, const float* d_dlogits, const void* d_x,
                                 const float* d_w, const void* d_dres, void* d_dx, float* d_dw, void* d_workspace,

@@ -375,7 +375,7 @@ int run_route_t(const Ctx& c, const float* logits, bool tables, void* zero_out, 
   SchedParams<BF16> sp = sched_params<BF16>(c, copy_x, logits, nullptr, nullptr, nullptr);
   sp.skip_tables = tables ? 0 : 1;
   const RouteParams& rp = sp.route;
-  const bool one = c.s.T <= kRouteOneT;   // one workgroup does it all in one launch (see route_one)
+  const bool one = c.s.T <= (scores ? kScoresOneT : kRouteOneT);   // one workgroup does it all in one launch (see route_one)
   const int fill_threads = one ? kRouteOneThreads : kScanWaves * kWave;
   int fill_wgs = 0;
   if (zero_out) {
@@ -392,8 +392,12 @@ int run_route_t(const Ctx& c, const float* logits, bool tables, void* zero_out, 
     return launch_status();
   }
   if (!scores) hipLaunchKernelGGL(route_kernel, dim3(rp.n_sub), dim3(512), 0, c.stream, rp);
-  else if (scores->n_group > 1) hipLaunchKernelGGL(route_scores_kernel<true>, dim3(rp.n_sub), dim3(512), 0, c.stream, rp, *scores);
-  else hipLaunchKernelGGL(route_scores_kernel<false>, dim3(rp.n_sub), dim3(512), 0, c.stream, rp, *scores);
+  else
+    with_score_lanes(rp.E, [&](auto lpt, auto kp, auto threads) {
+      constexpr int LPT = decltype(lpt)::value, KP = decltype(kp)::value, N = decltype(threads)::value;
+      if (scores->n_group > 1) hipLaunchKernelGGL((route_scores_kernel<true, LPT, KP, N>), dim3(rp.n_sub), dim3(N), 0, c.stream, rp, *scores);
+      else hipLaunchKernelGGL((route_scores_kernel<false, LPT, KP, N>), dim3(rp.n_sub), dim3(N), 0, c.stream, rp, *scores);
+    });
   if (copy_x) {
     // tokens per workgroup: a workgroup per CU, as long as each has a token (then rp.subs is 1)
     int tokens = kSub;

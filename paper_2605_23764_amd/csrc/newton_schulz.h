@@ -16,8 +16,8 @@
 // entries near 1 where they are typical, clear of both ends of the range: X by about sqrt(L), A and B by about S.
 // fp32 storage: operands are pairs of fp16 (hi, and the rest times 2^11), products hi hi + hi lo + lo hi, so 22 bits.
 #pragma once
-#include "gemm_bf16.h"
 #include "rows.h"
+#include "tile128.h"
 
 namespace moe {
 
@@ -68,38 +68,54 @@ __device__ __forceinline__ void lds_settled() {            // a wave's own LDS a
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Four columns n .. n + 3 of row m of the result: weights, or the update itself.  VEC: all four are there, and aligned.
-template <typename T, bool VEC> __device__ __forceinline__ void ns_put(const NsGemmParams& p, size_t at, int n, f32x4 o) {
+// Four columns n .. n + 3 of a row.  VEC: all four are there, and aligned; else those below N.
+template <typename T, bool VEC> __device__ __forceinline__ f32x4 ns_get(const T* src, size_t at, int n, int N) {
   typedef T T4 __attribute__((ext_vector_type(4)));
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if constexpr (VEC) {
-    if (p.master) {
-      const f32x4 w = *reinterpret_cast<const f32x4*>(p.master + at);
+    const T4 a = *reinterpret_cast<const T4*>(src + at);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) o[x] = p.w_keep * w[x] - p.w_step * o[x];
-      *reinterpret_cast<f32x4*>(p.master + at) = o;
-    } else if (p.w) {
-      const T4 w = *reinterpret_cast<const T4*>(static_cast<const T*>(p.w) + at);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) o[x] = p.w_keep * (float)w[x] - p.w_step * o[x];
-    }
-    T4 v;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) v[x] = (T)o[x];
-    *reinterpret_cast<T4*>(static_cast<T*>(p.out) + at) = v;
+    for (int x = 0; x < 4; ++x) v[x] = (float)a[x];
   } else {
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      if (n + x >= p.N) break;
-      float v = o[x];
-      if (p.master) {
-        v = p.w_keep * p.master[at + x] - p.w_step * v;
-        p.master[at + x] = v;
-      } else if (p.w) {
-        v = p.w_keep * (float)static_cast<const T*>(p.w)[at + x] - p.w_step * v;
-      }
-      static_cast<T*>(p.out)[at + x] = (T)v;
+    for (int x = 0; x < 4; ++x)
+      if (n + x < N) v[x] = (float)src[at + x];
+  }
+  return v;
+}
+template <typename T, bool VEC> __device__ __forceinline__ void ns_put(T* dst, size_t at, int n, int N, f32x4 v) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  if constexpr (VEC) {
+    T4 o;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o[x] = (T)v[x];
+    *reinterpret_cast<T4*>(dst + at) = o;
+  } else {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (n + x < N) dst[at + x] = (T)v[x];
+  }
+}
+// Eight rows, every fourth from m on, of the result: weights, or the update itself.  All weights are read ahead of the first store: they may be
+// the output, so no load passes a store by itself.
+template <typename T, bool VEC> __device__ __forceinline__ void ns_put_rows(const NsGemmParams& p, int e, int m, int n, f32x4 (&o)[8]) {
+  const size_t at = ((size_t)e * p.M + m) * p.N + n, step = (size_t)4 * p.N;
+  const int rows = n < p.N ? (p.M - m + 3) / 4 : 0;
+  if (p.master || p.w) {
+    f32x4 w[8];
+#pragma unroll
+    for (int it = 0; it < 8; ++it)
+      if (it < rows) w[it] = p.master ? ns_get<float, VEC>(p.master, at + it * step, n, p.N) : ns_get<T, VEC>(static_cast<const T*>(p.w), at + it * step, n, p.N);
+#pragma unroll
+    for (int it = 0; it < 8; ++it) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[it][x] = p.w_keep * w[it][x] - p.w_step * o[it][x];
+      if (p.master && it < rows) ns_put<float, VEC>(p.master, at + it * step, n, p.N, o[it]);
     }
   }
+#pragma unroll
+  for (int it = 0; it < 8; ++it)
+    if (it < rows) ns_put<T, VEC>(static_cast<T*>(p.out), at + it * step, n, p.N, o[it]);
 }
 
 // A wave's 32 rows x 32 NB columns of a result from (r0, c0) on, by way of its LDS region (kNsRegion bytes).
@@ -133,19 +149,8 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
       f32x4 o[8];
 #pragma unroll
       for (int it = 0; it < 8; ++it) o[it] = *(lds_f32x4_ptr)(base + (it * 4 + r4) * kRow + ch * 16);
-      if (p.N % 4 == 0) {
-#pragma unroll
-        for (int it = 0; it < 8; ++it) {
-          const int m = r0 + it * 4 + r4;
-          if (m < p.M && n < p.N) ns_put<T, true>(p, ((size_t)e * p.M + m) * p.N + n, n, o[it]);
-        }
-      } else {
-#pragma unroll
-        for (int it = 0; it < 8; ++it) {
-          const int m = r0 + it * 4 + r4;
-          if (m < p.M && n < p.N) ns_put<T, false>(p, ((size_t)e * p.M + m) * p.N + n, n, o[it]);
-        }
-      }
+      if (p.N % 4 == 0) ns_put_rows<T, true>(p, e, r0 + r4, n, o);
+      else ns_put_rows<T, false>(p, e, r0 + r4, n, o);
       wait_lgkmcnt0();
       lds_settled();
     }
@@ -296,135 +301,17 @@ __device__ __forceinline__ void ns_blocks128(const NsGemmParams& p, const f32x16
   }
 }
 
-// One tile of 128 x 128 by four waves of 64 x 64.  STAGES of 64 halves per row and side in LDS: two, and two workgroups to a CU, or four
-// and one, whose copies are then three steps under way.  Pairs: a stage is 32 k, and every fragment read serves three products.
-constexpr int kNsTile = 128, kNsStage = 2 * kNsTile * 128;
-// share, item: with splits > 1 the tile's k's are dealt to that many workgroups, of which this is number `share`; its sums go to place `item`.
+// One tile of 128 x 128 (tile128.h).  share, item: with splits > 1 the tile's k's are dealt to that many workgroups, of which this is number
+// `share`; its sums go to place `item`.
 template <int EPI, bool SPLIT, typename T, int STAGES, bool SHARES>
 __device__ __forceinline__ void ns_tile128(const NsGemmParams& p, int e, int i0, int j0, int share, int item, char* smem) {
-  int lane = lane_id();
-  asm volatile("" : "+v"(lane));
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wave >> 1, wn = wave & 1;
-  const int l32 = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
   const int row_bytes = p.K * (SPLIT ? 4 : 2), all_steps = row_bytes / 128;
   const int first_step = SHARES ? all_steps * share / p.splits : 0;
   const int n_steps = SHARES ? all_steps * (share + 1) / p.splits - first_step : all_steps;
-  const int kc_r = lane >> 3;
-  const int kc_c = (lane & 7) ^ ((4 * (wave & 1) + (kc_r >> 1)) & 7);
-  uint32_t off[8];                         // of the lines that this wave copies: four of P, four of Q
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {            // rows past the end read the last one again; they are not stored
-    const int r = (wave + 4 * i) * 8 + kc_r;
-    off[i] = (uint32_t)min(i0 + r, p.rows - 1) * (uint32_t)row_bytes + (uint32_t)(kc_c * 16);
-    off[4 + i] = (uint32_t)min(j0 + r, p.cols - 1) * (uint32_t)row_bytes + (uint32_t)(kc_c * 16);
-  }
-  const char* P = uniform_ptr(p.P + (size_t)e * p.p_stride + (size_t)first_step * 128);
-  const char* Q = uniform_ptr(p.Q + (size_t)e * p.q_stride + (size_t)first_step * 128);
-  const uint32_t lds0 = uniform_u32(lds_addr_of(smem) + (uint32_t)(wave * kLine));
-  // copy i of a step into its stage
-  auto copy = [&](auto ic, const char* ps, const char* qs, uint32_t stage) __attribute__((always_inline)) {
-    constexpr int i = decltype(ic)::value;
-    if constexpr (i < 4) lds_dma16_at<4 * i * kLine>(ps, off[i], stage);
-    else lds_dma16_at<kNsTile * 128 + 4 * (i - 4) * kLine>(qs, off[i], stage);
-  };
   f32x16 acc[2][2], mix[2][2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = mix[i][j][r] = 0.f;
-
-  // A part of a step: a slice of 16 k, or of pairs 16 k's both halves; per side kFrags fragments: block x % 2 of 32 rows, half x / 2.
-  constexpr int kParts = SPLIT ? 2 : 4, kFrags = SPLIT ? 4 : 2, kMfma = SPLIT ? 12 : 4;
-  uint32_t at_p[4], at_q[4];               // a lane's place in a stage, per slice
-  {
-    const uint32_t f = (uint32_t)((l32 >> 1) & 7), lane_at = lds_addr_of(smem) + (uint32_t)((l32 >> 3) * kLine + (l32 & 7) * 128);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      at_p[q] = lane_at + (uint32_t)(wm * 8 * kLine) + ((((uint32_t)(q * 2 + lh)) ^ f) & 7) * 16;
-      at_q[q] = lane_at + (uint32_t)(kNsTile * 128 + wn * 8 * kLine) + ((((uint32_t)(q * 2 + lh)) ^ f) & 7) * 16;
-    }
-  }
-  struct Frags { bf16x8 p[kFrags], q[kFrags]; };
-  auto read = [&](Frags& f, auto rc, int part, uint32_t stage) __attribute__((always_inline)) {     // read r of 2 kFrags
-    constexpr int r = decltype(rc)::value, x = r >> 1;
-    const uint32_t at = (r & 1 ? at_q : at_p)[part + (x >> 1) * 2] + stage;
-    (r & 1 ? f.q : f.p)[x] = *(lds_bf16x8_cptr)((lds_cptr)(uintptr_t)at + (x & 1) * 4 * kLine);
-  };
-  // The part's MFMAs with the next part's operand reads between them, and behind those CFROM .. CTO - 1 of the copies: a wave is alone on its
-  // SIMD, or with one other, and what it issues in a row leaves the matrix core idle.
-  auto multiply = [&](const Frags& f, Frags& next, bool reads, int part, uint32_t stage, auto from, auto to, const char* ps, const char* qs,
-                      uint32_t dst) __attribute__((always_inline)) {
-    constexpr int kFrom = decltype(from)::value, kReads = 2 * kFrags, kActs = kReads + decltype(to)::value - kFrom;
-    static_for<0, kMfma>([&](auto mc) __attribute__((always_inline)) {
-      constexpr int m = decltype(mc)::value, i = (m >> 1) & 1, j = m & 1, kind = m >> 2;     // kind: hi hi, lo hi, hi lo
-      if constexpr (kind == 0) acc[i][j] = mfma_16bit<true>(f.q[j], f.p[i], acc[i][j]);
-      else if constexpr (kind == 1) mix[i][j] = mfma_16bit<true>(f.q[j], f.p[kFrags - 2 + i], mix[i][j]);
-      else mix[i][j] = mfma_16bit<true>(f.q[kFrags - 2 + j], f.p[i], mix[i][j]);
-      static_for<0, kActs>([&](auto ac) __attribute__((always_inline)) {
-        constexpr int a = decltype(ac)::value;
-        if constexpr (a * kMfma / kActs == m) {
-          if constexpr (a < kReads) {
-            if (reads) read(next, ac, part, stage);
-          } else {
-            copy(std::integral_constant<int, a - kReads + kFrom>{}, ps, qs, dst);
-          }
-        }
-      });
-      __builtin_amdgcn_sched_barrier(0);
-    });
-  };
-  typedef std::integral_constant<int, 0> C0;
-  typedef std::integral_constant<int, 8> C8;
-  // Behind it the copies of a step have landed in every wave, but for those of `ahead` later steps, and all have read what they had asked for.
-  auto settle = [&](int ahead) __attribute__((always_inline)) {
-    if (STAGES == 4 && ahead >= 2) asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)" ::: "memory");
-    else if (STAGES == 4 && ahead == 1) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
-    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-  Frags fa, fb;
-  static_for<0, STAGES>([&](auto sc) __attribute__((always_inline)) {
-    constexpr int s = decltype(sc)::value;
-    if (s < n_steps)
-      static_for<0, 8>([&](auto ic) __attribute__((always_inline)) { copy(ic, P + s * 128, Q + s * 128, lds0 + s * kNsStage); });
-  });
-  if (STAGES == 4 && n_steps >= 4) asm volatile("s_waitcnt vmcnt(24)" ::: "memory");
-  else if (STAGES == 4 && n_steps == 3) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-  else if (n_steps >= 2) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
-  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-  static_for<0, 2 * kFrags>([&](auto rc) __attribute__((always_inline)) { read(fa, rc, 0, 0); });
-  const char *ps = P + STAGES * 128, *qs = Q + STAGES * 128;   // of the copies that come next
-  uint32_t stage = 0;                                          // bytes from the first stage
-  // A step; MORE: with the copies of the step STAGES later, into this one's stage.  The barrier is ahead of the last part, whose operands are
-  // in registers then.
-  auto step = [&](auto more, bool last, int ahead) __attribute__((always_inline)) {
-    constexpr bool MORE = decltype(more)::value;
-#pragma unroll
-    for (int part = 0; part + 2 < kParts; part += 2) {
-      multiply(fa, fb, true, part + 1, stage, C0{}, C0{}, nullptr, nullptr, 0);
-      multiply(fb, fa, true, part + 2, stage, C0{}, C0{}, nullptr, nullptr, 0);
-    }
-    multiply(fa, fb, true, kParts - 1, stage, C0{}, C0{}, nullptr, nullptr, 0);
-    const uint32_t old = stage;
-    stage = stage == (STAGES - 1) * kNsStage ? 0 : stage + kNsStage;
-    if (!last) settle(ahead);
-    if constexpr (MORE) {
-      multiply(fb, fa, true, 0, stage, C0{}, C8{}, ps, qs, lds0 + old);
-      ps += 128;
-      qs += 128;
-    } else {
-      multiply(fb, fa, !last, 0, stage, C0{}, C0{}, nullptr, nullptr, 0);
-    }
-  };
-  int s = 0;
-  for (; s + STAGES < n_steps; ++s) step(std::true_type{}, false, STAGES - 2);
-  for (; s < n_steps; ++s) step(std::false_type{}, s + 1 == n_steps, n_steps - 2 - s);
+  tile128_multiply<SPLIT, true, STAGES>(p.P + (size_t)e * p.p_stride + (size_t)first_step * 128, p.Q + (size_t)e * p.q_stride + (size_t)first_step * 128,
+                                        row_bytes, p.rows, p.cols, i0, j0, n_steps, smem, acc, mix);
   if constexpr (SHARES) {
     float* dst = p.part + ((size_t)item * 4 + wave) * 4096 + lane;
 #pragma unroll
@@ -434,9 +321,6 @@ __device__ __forceinline__ void ns_tile128(const NsGemmParams& p, int e, int i0,
 #pragma unroll
         for (int r = 0; r < 16; ++r) dst[((i * 2 + j) * 16 + r) * 64] = SPLIT ? acc[i][j][r] + mix[i][j][r] * (1.0f / kNsLoScale) : acc[i][j][r];
   } else {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();          // every wave has read its last operands
-    asm volatile("" ::: "memory");
     ns_blocks128<EPI, SPLIT, SPLIT, T>(p, acc, mix, smem + wave * kNsRegion, wave, e, i0, j0);
   }
 }
@@ -491,7 +375,7 @@ template <bool SYM, bool QUARTERS> __device__ __forceinline__ bool ns_tile128_at
 template <int EPI, bool SPLIT, typename T, bool QUARTERS, int STAGES, bool SHARES>
 __global__ __launch_bounds__(256, STAGES == 2 ? 2 : 1) void ns_gemm128_kernel(NsGemmParams p) {
   static_assert(STAGES == 2 || STAGES == 4, "stages");
-  __shared__ __attribute__((aligned(1024))) char smem[STAGES * kNsStage];
+  __shared__ __attribute__((aligned(1024))) char smem[STAGES * kTile128Stage];
   // workgroups are dealt to the dies in turn: a die's take a contiguous eighth
   const int item = xcd_spread_tile(0, blockIdx.x, gridDim.x, SHARES ? p.tiles * p.splits : p.tiles);
   if (item < 0) return;

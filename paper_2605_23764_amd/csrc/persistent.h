@@ -458,17 +458,19 @@ __global__ __launch_bounds__(kRouteOneThreads) void route_one_kernel(SchedParams
 }
 
 // The same two with routing by scores (router_scores.h).
-template <bool GROUPS>
-__global__ __launch_bounds__(512) void route_scores_kernel(RouteParams p, ScoreParams sc) {
+template <bool GROUPS, int LPT, int KP, int THREADS>
+__global__ __launch_bounds__(THREADS) void route_scores_kernel(RouteParams p, ScoreParams sc) {
   __shared__ int32_t s_idx[kSub * kMaxK];
-  __shared__ float s_val[kSub * kMaxK];
-  __shared__ double s_slots[512 / kWave * kSlotWords];
-  route_chunk(p, blockIdx.x, s_idx, s_val, SelectScores<GROUPS>{sc, s_slots});
+  __shared__ double s_slots[THREADS / kWave * slot_words(KP)];
+  route_chunk(p, blockIdx.x, s_idx, nullptr, SelectScores<GROUPS, LPT, KP>{sc, s_slots});
 }
+// One launch as long as a token has a wave: 256 experts in 8 groups, k = 8, on the device, T = 8 10.7 us against 10.7 + 4.4 in two launches,
+// T = 16 14.1 against 12.8 + 4.4; with two tokens to a wave T = 64 32 against 19 + 4.4.
+constexpr int kScoresOneT = kRouteOneThreads / kWave;
 template <bool BF16, bool GROUPS>
 __global__ __launch_bounds__(kRouteOneThreads) void route_scores_one_kernel(SchedParams<BF16> sp, ScoreParams sc) {
-  __shared__ double s_slots[kRouteOneThreads / kWave * kSlotWords];
-  route_one_launch(sp, SelectScores<GROUPS>{sc, s_slots});
+  __shared__ double s_slots[kRouteOneThreads / kWave * kFewSlotWords];
+  route_one_launch(sp, SelectScoresFew<GROUPS>{sc, s_slots});
 }
 
 // SCATTER (bf16): GEMM-2 tiles add their weighted rows into the zeroed layer output from their epilogue

@@ -31,15 +31,36 @@ __device__ __forceinline__ void local_mask(const int32_t* idx, int k, int base, 
   }
 }
 
-// The selection of moe_route: top-k of the logits themselves.  (A selection is called with a wave's four tokens' keys as route_load
-// leaves them, and with the wave's kMaxK words per token for ids and values.)
+// The selection of moe_route: top-k of the logits themselves, four tokens to a wave.  A selection leaves the experts of a sub-chunk's tokens
+// (tokens), or of all of up to 64 tokens by a workgroup of 16 waves (few), kMaxK words per token, in s_idx; s_val as large, for its own use.
 struct SelectLogits {
-  template <int KP>
-  __device__ __forceinline__ void operator()(const RouteParams& p, int t_first, int lane, uint32_t (&key)[KP], int32_t* s_idx, float* s_val) const {
-    route_select(p, t_first, lane, key, s_idx, s_val);
+  __device__ __forceinline__ void tokens(const RouteParams& p, int t0, int32_t* s_idx, float* s_val) const {
+    const int lane = lane_id();
+    const int wave = threadIdx.x / kWave;
+    const int n_waves = blockDim.x / kWave;
+    const int step = n_waves * kRouteTokensPerWave;
+    with_route_keys(p.E, [&](auto kp) __attribute__((always_inline)) {
+      constexpr int KP = decltype(kp)::value;
+      uint32_t key[KP], key_next[KP];
+      int i = wave * kRouteTokensPerWave;
+      if (i < kSub && t0 + i < p.T) route_load<KP>(p, t0 + i, lane, key);
+      for (; i < kSub && t0 + i < p.T; i += step) {
+        const bool more = i + step < kSub && t0 + i + step < p.T;
+        if (more) route_load<KP>(p, t0 + i + step, lane, key_next);
+        route_select<KP>(p, t0 + i, lane, key, s_idx + i * kMaxK, s_val + i * kMaxK);
+#pragma unroll
+        for (int q = 0; q < KP; ++q) key[q] = key_next[q];
+      }
+    });
   }
   __device__ __forceinline__ void few(const RouteParams& p, int wave, int lane, int32_t* s_idx, float* s_val) const {
-    select_four(p, wave, lane, s_idx, s_val, *this);
+    const int t0 = wave * kRouteTokensPerWave;
+    if (t0 < p.T)
+      with_route_keys(p.E, [&](auto kp) __attribute__((always_inline)) {
+        uint32_t key[decltype(kp)::value];
+        route_load(p, t0, lane, key);
+        route_select(p, t0, lane, key, s_idx + t0 * kMaxK, s_val + t0 * kMaxK);
+      });
   }
 };
 
@@ -51,22 +72,8 @@ template <typename SELECT>
 __device__ __forceinline__ void route_chunk(const RouteParams& p, int sub, int32_t* s_idx, float* s_val, const SELECT& select) {
   const int lane = lane_id();
   const int wave = threadIdx.x / kWave;
-  const int n_waves = blockDim.x / kWave;
   const int t0 = sub * kSub;
-  const int step = n_waves * kRouteTokensPerWave;
-  with_route_keys(p.E, [&](auto kp) __attribute__((always_inline)) {
-    constexpr int KP = decltype(kp)::value;
-    uint32_t key[KP], key_next[KP];
-    int i = wave * kRouteTokensPerWave;
-    if (i < kSub && t0 + i < p.T) route_load<KP>(p, t0 + i, lane, key);
-    for (; i < kSub && t0 + i < p.T; i += step) {
-      const bool more = i + step < kSub && t0 + i + step < p.T;
-      if (more) route_load<KP>(p, t0 + i + step, lane, key_next);
-      select(p, t0 + i, lane, key, s_idx + i * kMaxK, s_val + i * kMaxK);
-#pragma unroll
-      for (int q = 0; q < KP; ++q) key[q] = key_next[q];
-    }
-  });
+  select.tokens(p, t0, s_idx, s_val);
   __syncthreads();
   if (wave == 0) {
     uint64_t mask[kMaskWords];

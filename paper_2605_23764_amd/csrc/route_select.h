@@ -148,17 +148,4 @@ __device__ __forceinline__ void with_route_keys(int E, F&& f) {
   else f(std::integral_constant<int, 16>{});
 }
 
-// Four tokens of a launch of up to 64 tokens by each of its 16 waves.
-constexpr int kRouteFewWaves = 16;
-template <typename SELECT>
-__device__ __forceinline__ void select_four(const RouteParams& p, int wave, int lane, int32_t* s_idx, float* s_val, const SELECT& select) {
-  const int t0 = wave * kRouteTokensPerWave;
-  if (t0 < p.T)
-    with_route_keys(p.E, [&](auto kp) __attribute__((always_inline)) {
-      uint32_t key[decltype(kp)::value];
-      route_load(p, t0, lane, key);
-      select(p, t0, lane, key, s_idx + t0 * kMaxK, s_val + t0 * kMaxK);
-    });
-}
-
 }  // namespace moe

@@ -14,7 +14,7 @@
 #pragma once
 #include <type_traits>
 
-#include "common.h"
+#include "tile128.h"
 
 namespace moe {
 
@@ -147,36 +147,75 @@ template <typename T, bool KC, int R> struct ProjSide {
   }
 };
 
-// Four columns of a result from `at` on, n of them there.  One load and one store where all four are, at any element's address.
-template <typename OUT> __device__ __forceinline__ void proj_put(const ProjParams& p, size_t at, int n, f32x4 v) {
-  typedef OUT vec __attribute__((ext_vector_type(4), aligned(sizeof(OUT))));
-  const OUT* add = static_cast<const OUT*>(p.add);
-  OUT* out = static_cast<OUT*>(p.out);
+// Four columns from `at` on, n of them there: one access where all four are, at any element's address.
+template <typename T> __device__ __forceinline__ f32x4 proj_get(const T* src, size_t at, int n) {
+  typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (n >= 4) {
-    if (add) {
-      const vec a = *reinterpret_cast<const vec*>(add + at);
+    const vec a = *reinterpret_cast<const vec*>(src + at);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) v[x] += (float)a[x];
-    }
-    vec o;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) o[x] = (OUT)v[x];
-    *reinterpret_cast<vec*>(out + at) = o;
+    for (int x = 0; x < 4; ++x) v[x] = (float)a[x];
   } else {
 #pragma unroll
     for (int x = 0; x < 3; ++x)
-      if (x < n) out[at + x] = (OUT)(add ? (float)add[at + x] + v[x] : v[x]);
+      if (x < n) v[x] = (float)src[at + x];
+  }
+  return v;
+}
+template <typename T> __device__ __forceinline__ void proj_put(T* dst, size_t at, int n, f32x4 v) {
+  typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  if (n >= 4) {
+    vec o;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o[x] = (T)v[x];
+    *reinterpret_cast<vec*>(dst + at) = o;
+  } else {
+#pragma unroll
+    for (int x = 0; x < 3; ++x)
+      if (x < n) dst[at + x] = (T)v[x];
   }
 }
 
+// A wave's 32 rows x 64 columns of a result, whole lines, by way of the wave's place in LDS (kProjRegion bytes).
+constexpr int kProjRow = 64 * 4 + 16, kProjRegion = 32 * kProjRow;
+template <typename OUT> __device__ __forceinline__ void proj_store_rows(const ProjParams& p, const f32x16 (&acc)[2], int r0, int c0, char* region) {
+  const int lane = lane_id(), l32 = lane & 31, lh = lane >> 5;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4*>(region + l32 * kProjRow + (j * 32 + q * 8 + lh * 4) * 4) =
+          f32x4{acc[j][q * 4], acc[j][q * 4 + 1], acc[j][q * 4 + 2], acc[j][q * 4 + 3]};
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  // everything that is added ahead of the first store: add may be out, so no load passes a store by itself
+  const int c = c0 + (lane & 15) * 4, rl = r0 + (lane >> 4), left = p.cols - c;
+  const OUT* add = static_cast<const OUT*>(p.add);
+  const size_t at = (size_t)rl * p.cols + c, step = (size_t)4 * p.cols;
+  f32x4 v[8];
+#pragma unroll
+  for (int it = 0; it < 8; ++it)
+    v[it] = add && rl + it * 4 < p.rows && left > 0 ? proj_get(add, at + it * step, left) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int it = 0; it < 8; ++it) v[it] += *reinterpret_cast<const f32x4*>(region + (it * 4 + (lane >> 4)) * kProjRow + (lane & 15) * 16);
+#pragma unroll
+  for (int it = 0; it < 8; ++it)
+    if (rl + it * 4 < p.rows && left > 0) proj_put(static_cast<OUT*>(p.out), at + it * step, left, v[it]);
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // NP, NQ: pieces of a value of each side.  TN: columns of a tile, 128 or 32.  OUT: storage of the result of dx, void: partial sums in fp32.
+// Two workgroups to a CU where their LDS allows it (all but fp32's pairs of three pieces): they cover each other's waits (dx, 8192 x 7168 x 256, 260
+// registers and one workgroup: 312 us).
 template <typename TP, bool KCP, int NP, typename TQ, bool KCQ, int NQ, int TN, typename OUT>
-__global__ __launch_bounds__(kProjThreads) void project_kernel(ProjParams p) {
+__global__ __launch_bounds__(kProjThreads, NP * kProjTile + NQ * TN <= 512 ? 2 : 1) void project_kernel(ProjParams p) {
   constexpr int kOrder = NP > NQ ? NP : NQ, kPieceP = kProjTile * 128, kPieceQ = TN * 128;
   constexpr int BI = TN == 128 ? 2 : 1, BJ = BI;                 // blocks of 32 x 32 of a wave
-  constexpr int kRow = 64 * 4 + 16, kRegion = 32 * kRow;
   constexpr int kStage = NP * kPieceP + NQ * kPieceQ;
-  constexpr int kLds = !std::is_void<OUT>::value && kStage < 4 * kRegion ? 4 * kRegion : kStage;
+  constexpr int kLds = !std::is_void<OUT>::value && kStage < 4 * kProjRegion ? 4 * kProjRegion : kStage;
   __shared__ __attribute__((aligned(1024))) char smem[kLds];
   // the splits of a tile go to different dies, a split's tiles to the same ones: there its part of W stays in the L2
   int b = blockIdx.x;
@@ -209,6 +248,7 @@ __global__ __launch_bounds__(kProjThreads) void project_kernel(ProjParams p) {
     }
 #pragma unroll
     for (int ks = 0; ks < kProjK / 16; ++ks) {
+      if (ks * 16 >= k_end - k) break;       // the rest of the step is zeros
       bf16x8 fp[BI][NP], fq[BJ][NQ];
 #pragma unroll
       for (int x = 0; x < BI; ++x) {
@@ -251,30 +291,56 @@ __global__ __launch_bounds__(kProjThreads) void project_kernel(ProjParams p) {
             for (int x = 0; x < 3; ++x)
               if (c + x < p.cols) dst[c + x] = acc[i][j][q * 4 + x];
         }
-    } else {                               // whole lines, by way of the wave's place in LDS
+    } else {
       static_assert(std::is_void<OUT>::value || TN == 128, "64 columns of a wave");
-      char* region = smem + wave * kRegion;
-#pragma unroll
-      for (int j = 0; j < BJ; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          *reinterpret_cast<f32x4*>(region + l32 * kRow + (j * 32 + q * 8 + lh * 4) * 4) =
-              f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      const int c = j0 + qr + (lane & 15) * 4;
-#pragma unroll
-      for (int it = 0; it < 8; ++it) {
-        const int r = it * 4 + (lane >> 4);
-        const f32x4 v = *reinterpret_cast<const f32x4*>(region + r * kRow + (lane & 15) * 16);
-        if (r0 + r < p.rows && c < p.cols) proj_put<OUT>(p, (size_t)(r0 + r) * p.cols + c, p.cols - c, v);
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      proj_store_rows<OUT>(p, acc[i], r0, j0 + qr, smem + wave * kProjRegion);
     }
   }
+}
+
+// dx in bf16: both sides as pairs of bf16 (project_pairs_kernel), [rows][Ep / 32][hi 32 | lo 32], which copies to LDS take as they are.
+__global__ __launch_bounds__(256, 2) void project_dx_kernel(ProjParams p, int Ep) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * kTile128Stage];
+  static_assert(4 * kProjRegion <= 2 * kTile128Stage, "regions");
+  // 32 tile columns by 8 tile rows to a die's turn: what runs on it at a time shares operands in its L2
+  const int tiles_i = (p.rows + 127) / 128, tile = xcd_spread_tile(0, blockIdx.x, gridDim.x, tiles_i * p.tj);
+  if (tile < 0) return;
+  const int strip = __builtin_amdgcn_readfirstlane(tile / (8 * p.tj)), h = min(8, tiles_i - 8 * strip), r = tile - strip * 8 * p.tj;
+  const int j = __builtin_amdgcn_readfirstlane(r / h), i = strip * 8 + r - j * h;
+  f32x16 acc[2][2], mix[2][2];
+  tile128_multiply<true, false, 2>(static_cast<const char*>(p.P), static_cast<const char*>(p.Q), Ep * 4, p.rows, p.cols, i * 128, j * 128, Ep / 32, smem, acc,
+                                   mix);
+  const int wave = threadIdx.x / kWave;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) acc[x][y] += mix[x][y];
+    proj_store_rows<__bf16>(p, acc[x], i * 128 + (wave >> 1) * 64 + x * 32, j * 128 + (wave & 1) * 64, smem + wave * kProjRegion);
+  }
+}
+
+// Pairs of the rows [na,E] of a and, behind them, those [nb,E] of b: eight values per thread; columns past E are zeros.
+__global__ __launch_bounds__(256) void project_pairs_kernel(const float* a, int na, const float* b, int nb, int E, int Ep, char* out) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int chunks = Ep / 8, c = (int)(i % chunks) * 8;
+  const size_t row = i / chunks;
+  if (row >= (size_t)na + nb) return;
+  const float* src = (row < (size_t)na ? a + row * E : b + (row - na) * E) + c;
+  ProjChunk<float> v = {};
+  if (c + 8 <= E) {
+    const f32x4_any lo = reinterpret_cast<const f32x4_any*>(src)[0], hi = reinterpret_cast<const f32x4_any*>(src)[1];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) { v.v[x] = lo[x]; v.v[4 + x] = hi[x]; }
+  } else {
+#pragma unroll
+    for (int x = 0; x < 7; ++x)
+      if (c + x < E) v.v[x] = src[x];
+  }
+  u32x4 piece[2];
+  proj_pieces<2>(v, piece);
+  char* dst = out + row * ((size_t)Ep * 4) + (c >> 5) * 128 + (c & 31) * 2;
+  *reinterpret_cast<u32x4*>(dst) = piece[0];
+  *reinterpret_cast<u32x4*>(dst + 64) = piece[1];
 }
 
 // out[i] = sum over the splits of part[split][i], n of them: 256 / PARTS values per workgroup, whose PARTS shares take every PARTS-th split

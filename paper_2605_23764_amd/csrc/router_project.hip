@@ -39,6 +39,10 @@ Split split_of(int rows, int cols, int K) {
   s.n = ceil_div(K, s.k);
   return s;
 }
+// Experts in pairs, and the bytes of both sides' pairs.
+int pad_pairs(int E) { return ceil_div(E, 32) * 32; }
+constexpr int kProjRows = 1 << 21;         // rows of dx at a time: 32-bit offsets into their pairs of up to 1 KB
+size_t pairs_bytes(int T, int H, int E) { return ((size_t)std::min(T, kProjRows) + H) * pad_pairs(E) * 4; }
 size_t part_bytes(const Split& s, int rows, int cols) { return s.n > 1 ? (size_t)s.n * rows * cols * 4 : 0; }
 
 int join(const float* part, int splits, size_t n, float* out, hipStream_t s) {
@@ -76,7 +80,7 @@ int moe_router_project_workspace_bytes(int32_t T, int32_t H, int32_t E, size_t* 
   const int st = check(T, H, E, MOE_F32);
   if (st != MOE_OK) return st;
   if (!bytes) return MOE_ERR_INVALID_ARG;
-  *bytes = T == 0 ? 16 : std::max<size_t>(16, std::max(part_bytes(split_of(T, E, H), T, E), part_bytes(split_of(H, E, T), H, E)));
+  *bytes = T == 0 ? 16 : std::max({pairs_bytes(T, H, E), part_bytes(split_of(T, E, H), T, E), part_bytes(split_of(H, E, T), H, E)});
   return MOE_OK;
 }
 
@@ -106,12 +110,12 @@ int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, cons
     if (!d_dw) return MOE_OK;
     return join(nullptr, 0, (size_t)H * E, d_dw, s);   // sums over nothing
   }
-  if (!good(d_dlogits) || (d_dx && !good(d_w)) || (d_dw && !good(d_x))) return MOE_ERR_INVALID_ARG;
+  if (!d_dx && !d_dw) return MOE_OK;
+  if (!good(d_dlogits) || (d_dx && !good(d_w)) || (d_dw && !good(d_x)) || !good(d_workspace)) return MOE_ERR_INVALID_ARG;
+  size_t need = 0;
+  moe_router_project_workspace_bytes(T, H, E, &need);
+  if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
   if (d_dw) {
-    size_t need = 0;
-    moe_router_project_workspace_bytes(T, H, E, &need);
-    if (!good(d_workspace)) return MOE_ERR_INVALID_ARG;
-    if (workspace_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
     ProjParams p{};                        // ahead of dx, which may be x
     p.P = d_x; p.Q = d_dlogits;
     p.ld_p = H; p.ld_q = E;
@@ -121,16 +125,33 @@ int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, cons
   }
   if (d_dx) {
     ProjParams p{};
-    p.P = d_dlogits; p.Q = d_w;
-    p.ld_p = p.ld_q = E;
-    p.rows = T; p.cols = H; p.K = E;
-    p.k_split = ceil_div(E, kProjK) * kProjK;
-    p.splits = 1;
+    p.rows = T; p.cols = H;
     p.tj = ceil_div(H, kProjTile);
     p.add = d_dres; p.out = d_dx;
-    const dim3 grid((unsigned)((size_t)ceil_div(T, kProjTile) * p.tj));
-    if (dtype == MOE_BF16) hipLaunchKernelGGL((project_kernel<float, true, 2, float, true, 2, 128, __bf16>), grid, dim3(kProjThreads), 0, s, p);
-    else hipLaunchKernelGGL((project_kernel<float, true, 3, float, true, 3, 128, float>), grid, dim3(kProjThreads), 0, s, p);
+    if (dtype == MOE_BF16) {
+      const int Ep = pad_pairs(E);
+      char* pairs = static_cast<char*>(d_workspace);               // W's, then dlogits'
+      p.Q = pairs;
+      p.P = pairs + (size_t)H * Ep * 4;
+      for (int t0 = 0; t0 < T; t0 += kProjRows) {
+        const int n = std::min(T - t0, kProjRows), w_rows = t0 ? 0 : H;
+        hipLaunchKernelGGL(project_pairs_kernel, dim3((unsigned)(((size_t)n + w_rows) * (Ep / 8) / 256 + 1)), dim3(256), 0, s, d_w, w_rows,
+                           d_dlogits + (size_t)t0 * E, n, E, Ep, pairs + (size_t)(H - w_rows) * Ep * 4);
+        p.rows = n;
+        p.add = d_dres ? static_cast<const uint16_t*>(d_dres) + (size_t)t0 * H : nullptr;
+        p.out = static_cast<uint16_t*>(d_dx) + (size_t)t0 * H;
+        const size_t tiles = (size_t)ceil_div(n, kProjTile) * p.tj;
+        hipLaunchKernelGGL(project_dx_kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), 0, s, p, Ep);
+        if (T - t0 <= kProjRows) break;
+      }
+    } else {
+      p.P = d_dlogits; p.Q = d_w;
+      p.ld_p = p.ld_q = p.K = E;
+      p.k_split = ceil_div(E, kProjK) * kProjK;
+      p.splits = 1;
+      hipLaunchKernelGGL((project_kernel<float, true, 3, float, true, 3, 128, float>), dim3((unsigned)((size_t)ceil_div(T, kProjTile) * p.tj)),
+                         dim3(kProjThreads), 0, s, p);
+    }
     st = launched();
   }
   return st;

@@ -10,18 +10,16 @@
 // select others).  Weights are rounded once.  Keys, and groups' sums of them, are rounded to 44 bits, and the lowest 8 are the expert's number, so
 // that one maximum finds the key, the expert and the lowest of equals.
 //
-// Bound by instructions, and where a wave has few tokens by fetching them: a line of eight that no wave has run yet costs some 300 clocks, so
-// what is done per expert is a loop on the token's keys in LDS where a lane has more than four (all unrolled: T = 8192, 256 experts
-// 41 us, T = 64 61; this: MEASURED).  A token takes 16 lanes; each lane sorts its experts' keys (a network of maxima and minima), and a
-// round of the selection is a maximum over the lanes' first keys, behind which the winner's move up.  Up to 16 tokens, a wave to each, take
-// all 64 lanes.
+// Bound by instructions and their latency: about 30 in 64 bits per expert for its score, and a round of the selection is a maximum over the
+// token's lanes' first keys (each lane sorts its own, by a network of maxima and minima), behind which the winner's move up.  What is done per
+// expert is a loop on the token's keys in LDS where a lane has more than four, for the code's length: a line of it that no wave has run yet
+// costs some 300 clocks.  A token takes 16 lanes up to 128 experts, 32 beyond, of twice as many waves (8192 tokens of 256 experts in 8 groups,
+// k = 8: 20.5 us both ways, without groups 16.9; 30001 tokens of 64 experts in 4 groups, k = 6: 17.8, 28.0 with the LDS of 256), in a launch of up to 16 tokens, a wave to each, 64.
 #pragma once
 #include "route_select.h"
 #include "scores_math.h"
 
 namespace moe {
-
-constexpr int kMaxGroups = 16;             // a lane of the token's row to a group
 
 struct ScoreParams {
   const float* bias;     // [E] or null
@@ -59,14 +57,16 @@ template <int LPT, typename OP> __device__ __forceinline__ double lanes_reduce(d
   }
   MOE_STEP(0xB1) MOE_STEP(0x4E) MOE_STEP(0x141) MOE_STEP(0x140)
 #undef MOE_STEP
-  if constexpr (LPT == 64) {
+  if constexpr (LPT >= 32) {
     auto join = [&](auto a, auto b) __attribute__((always_inline)) {
       v = op(__builtin_bit_cast(double, (uint64_t)(uint32_t)b[0] << 32 | (uint32_t)a[0]), __builtin_bit_cast(double, (uint64_t)(uint32_t)b[1] << 32 | (uint32_t)a[1]));
     };
     uint64_t u = __builtin_bit_cast(uint64_t, v);
     join(__builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false), __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
-    u = __builtin_bit_cast(uint64_t, v);
-    join(__builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
+    if constexpr (LPT == 64) {
+      u = __builtin_bit_cast(uint64_t, v);
+      join(__builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
+    }
   }
   return v;
 }
@@ -94,17 +94,30 @@ template <int N> __device__ __forceinline__ void sort_keys(double (&v)[N]) {
           }
 }
 
-// 64 / LPT tokens by one wave, LPT lanes to each, KP experts to a lane; l: the logits of the lane's, -inf where there is none.
-// slots: the wave's kSlotWords (a token by itself has those of all).
-constexpr int kSlotWords = kRouteTokensPerWave * (kMaxE + 16);
+// Words of LDS of a wave whose lanes have KP experts: a word beside each lane's, so that the lanes' lie in all banks.
+constexpr int slot_words(int kp) { return kWave * (kp + 1); }
+// 64 / LPT tokens from t_first on by one wave, LPT lanes to each, KP experts to a lane (LPT KP >= E).
 template <int LPT, int KP, bool GROUPS>
-__device__ __forceinline__ void route_scores_select(const RouteParams& p, const ScoreParams& sc, int t_first, int lane, const float (&l)[KP],
-                                                    int32_t* s_idx, double* slots) {
+__device__ __forceinline__ void route_scores_select(const RouteParams& p, const ScoreParams& sc, int t_first, int lane, int32_t* s_idx, double* slots) {
   constexpr int kUnroll = KP <= 4 ? KP : 1;
   const int row = lane / LPT, s = lane % LPT, e0 = s * KP, n = p.E - e0, tok = t_first + row;
   const float none = -__builtin_huge_valf();
-  double* mine = slots + row * (kSlotWords / kRouteTokensPerWave);
-  auto at = [](int e) __attribute__((always_inline)) { return e + e / KP; };   // a word beside each lane's, so that the lanes' lie in all banks
+  double* mine = slots + row * (LPT * (KP + 1));
+  auto at = [](int e) __attribute__((always_inline)) { return e + e / KP; };
+  float l[KP];                                                   // -inf where the lane has no expert
+  {
+    const float* logits = p.logits + (size_t)min(tok, p.T - 1) * p.E;   // tokens past the end repeat the last one
+    if (KP >= 4 && (p.E & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i + 3 < KP; i += 4) __builtin_memcpy(l + i, logits + min(e0 + i, p.E - 4), 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < KP; ++i) l[i] = logits[min(e0 + i, p.E - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < KP; ++i)
+      if (i >= n || l[i] != l[i]) l[i] = none;
+  }
   auto settled = []() __attribute__((always_inline)) {           // a wave's LDS accesses, seen by its other lanes
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -114,7 +127,7 @@ __device__ __forceinline__ void route_scores_select(const RouteParams& p, const 
 #pragma unroll
   for (int i = 0; i < KP; ++i) {
     m = __builtin_fmaxf(m, l[i]);
-    mine[at(e0) + i] = (double)l[i];                             // also where the lane has no expert: -inf, in the token's words
+    mine[at(e0) + i] = (double)l[i];                             // where there is no expert, too
   }
   // scores, -1 for the dead; softmax: not yet over their sum
   double inv = 1.0;
@@ -208,40 +221,43 @@ __device__ __forceinline__ void route_scores_select(const RouteParams& p, const 
   settled();                                                     // the next tokens' go to the same places
 }
 
-// The selection as route_chunk and route_one call it.  s_slots: the workgroup's, kSlotWords per wave.
-template <bool GROUPS> struct SelectScores {
+// The selection as route_chunk calls it: LPT lanes per token and KP experts per lane as with_score_lanes has them.  s_slots: slot_words per wave.
+template <bool GROUPS, int LPT, int KP> struct SelectScores {
   const ScoreParams& sc;
   double* s_slots;
-  __device__ __forceinline__ double* slots() const { return s_slots + (threadIdx.x / kWave) * kSlotWords; }
-  template <int KP>
-  __device__ __forceinline__ void operator()(const RouteParams& p, int t_first, int lane, uint32_t (&order)[KP], int32_t* s_idx, float*) const {
-    float l[KP];
-#pragma unroll
-    for (int i = 0; i < KP; ++i) l[i] = order[i] ? float_from_order_key(order[i]) : -__builtin_huge_valf();   // 0: no expert there
-    route_scores_select<16, KP, GROUPS>(p, sc, t_first, lane, l, s_idx, slots());
+  __device__ __forceinline__ void tokens(const RouteParams& p, int t0, int32_t* s_idx, float*) const {
+    constexpr int kTokens = kWave / LPT;
+    const int wave = threadIdx.x / kWave, n_waves = blockDim.x / kWave;
+#pragma unroll 1
+    for (int i = wave * kTokens; i < kSub && t0 + i < p.T; i += n_waves * kTokens)
+      route_scores_select<LPT, KP, GROUPS>(p, sc, t0 + i, lane_id(), s_idx + i * kMaxK, s_slots + wave * slot_words(KP));
   }
-  // All tokens of a launch of up to 64, by its 16 waves: a wave to a token as long as there are as many.
-  __device__ __forceinline__ void few(const RouteParams& p, int wave, int lane, int32_t* s_idx, float* s_val) const {
-    if (p.T > kRouteFewWaves) {
-      select_four(p, wave, lane, s_idx, s_val, *this);
-      return;
-    }
+};
+// The selection as route_one calls it, for as many tokens as it has waves: a wave to each.
+constexpr int kFewSlotWords = slot_words(kMaxE / kWave);
+template <bool GROUPS> struct SelectScoresFew {
+  const ScoreParams& sc;
+  double* s_slots;
+  __device__ __forceinline__ void few(const RouteParams& p, int wave, int lane, int32_t* s_idx, float*) const {
     if (wave >= p.T) return;
     auto one = [&](auto kp) __attribute__((always_inline)) {
-      constexpr int KP = decltype(kp)::value;
-      float l[KP];
-#pragma unroll
-      for (int i = 0; i < KP; ++i) {
-        const int e = lane * KP + i;
-        l[i] = p.logits[(size_t)wave * p.E + min(e, p.E - 1)];
-        if (e >= p.E || l[i] != l[i]) l[i] = -__builtin_huge_valf();
-      }
-      route_scores_select<64, KP, GROUPS>(p, sc, wave, lane, l, s_idx + wave * kMaxK, slots());
+      route_scores_select<kWave, decltype(kp)::value, GROUPS>(p, sc, wave, lane, s_idx + wave * kMaxK, s_slots + wave * kFewSlotWords);
     };
     if (p.E <= 64) one(std::integral_constant<int, 1>{});
     else if (p.E <= 128) one(std::integral_constant<int, 2>{});
     else one(std::integral_constant<int, 4>{});
   }
 };
+
+// f(lanes per token, experts per lane, threads per workgroup) for E experts.
+template <typename F> void with_score_lanes(int E, F&& f) {
+  typedef std::integral_constant<int, 16> L16;
+  typedef std::integral_constant<int, 512> W8;
+  if (E <= 16) f(L16{}, std::integral_constant<int, 1>{}, W8{});
+  else if (E <= 32) f(L16{}, std::integral_constant<int, 2>{}, W8{});
+  else if (E <= 64) f(L16{}, std::integral_constant<int, 4>{}, W8{});
+  else if (E <= 128) f(L16{}, std::integral_constant<int, 8>{}, W8{});
+  else f(std::integral_constant<int, 32>{}, std::integral_constant<int, 8>{}, std::integral_constant<int, 1024>{});
+}
 
 }  // namespace moe

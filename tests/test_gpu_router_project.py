@@ -52,13 +52,13 @@ def test_forward_and_backward(T, H, E, dtype):
     close(dx, R + raw, e + (U + HALF[dtype]) * (np.abs(R + raw) + e), "dx")
     # without the other gradient, the residual's part, and over the inputs
     alone, dw2 = _new(T, H, dtype=TORCH[dtype]), _new(H, E)
-    moe.moe_router_project_backward(d, x, w, dres, alone, None, None)
+    moe.moe_router_project_backward(d, x, w, dres, alone, None, ws)
     moe.moe_router_project_backward(d, x, w, None, None, dw2, ws)
     assert torch.equal(alone, dx) and torch.equal(dw2, dw)
-    moe.moe_router_project_backward(d, x, w, None, alone, None, None)
+    moe.moe_router_project_backward(d, x, w, None, alone, None, ws)
     close(alone, raw, e + (U + HALF[dtype]) * (np.abs(raw) + e), "dx without a residual")
     over = dres.clone()
-    moe.moe_router_project_backward(d, x, w, over, over, None, None)
+    moe.moe_router_project_backward(d, x, w, over, over, None, ws)
     assert torch.equal(over, dx)
     over = x.clone()
     moe.moe_router_project_backward(d, over, w, dres, over, dw2, ws)

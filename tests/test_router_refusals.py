@@ -111,7 +111,8 @@ def test_router_project(lib, want, change):
 
 @pytest.mark.parametrize("want,change", SIZES + [(INVALID, {n: None}) for n in ("d", "x", "w", "ws")] +
                          [(INVALID, {n: at(8, 4)}) for n in ("d", "x", "w", "dres", "dx", "dw", "ws")] + [(SMALL, dict(size=15)),
-                          (INVALID, dict(dw=None, w=None)), (INVALID, dict(dx=None, x=None)), (INVALID, dict(dw=None, d=None))])
+                          (INVALID, dict(dw=None, w=None)), (INVALID, dict(dx=None, x=None)), (INVALID, dict(dw=None, d=None)), (INVALID, dict(dw=None, ws=None)),
+                          (SMALL, dict(dw=None, size=15))])
 def test_router_project_backward(lib, want, change):
     assert project_backward(lib, **change) == want
 
