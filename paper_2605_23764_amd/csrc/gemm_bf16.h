@@ -353,6 +353,13 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
+// F16: the operands' 16 bits are fp16 (tile128.h), the same loop otherwise.
+template <bool F16>
+__device__ __forceinline__ f32x16 mfma_16bit(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  static_assert(!F16, "tile128.h has the product of fp16 operands");
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
 // The slice of a wave with four row blocks (tiles of more than 192 rows, matrix bound), with the copies LOAD0 ..
 // LOAD0 + 3 of the load group.  A wave is alone on its SIMD and issues one instruction every four clocks, eight under a
 // 32-clock MFMA, so what stands between two MFMAs decides: here at most one operand read or one copy, the copies evenly
@@ -363,13 +370,6 @@ __device__ __forceinline__ void static_for(F&& f) {
 // launch 1320 -> 1250; T = 4096, H = 2048, I = 1408, 16 experts: forward 401 -> 386, backward 731 -> 705.  With the copies
 // masked through exec instead of repeated past the end: 10 % slower than the general loop.  Waves with fewer row blocks
 // keep the general loop: those launches wait for the weights (this slice: 0 to 2 % slower at 64..125 rows per expert).
-// F16: the operands' 16 bits are fp16 (newton_schulz.h), the same loop otherwise.
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-template <bool F16>
-__device__ __forceinline__ f32x16 mfma_16bit(const bf16x8& a, const bf16x8& b, const f32x16& c) {
-  if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
 template <int LAY, int NX, int LOAD0, bool STREAM, bool F16 = false>
 __device__ __forceinline__ void gemm_slice_full(f32x16 (&acc)[kMaxMT][4], const GemmFrags<LAY, kMaxMT>& cur, GemmFrags<LAY, kMaxMT>& nxt,
                                                 lds_cptr as_n, lds_cptr bs_n, int ks_n, const GemmTileCtx& t,

@@ -274,7 +274,9 @@ __device__ __forceinline__ void ns_tile256(const NsGemmParams& p, int e, int i0,
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   t.a_base = uniform_ptr(p.P + (size_t)e * p.p_stride);
   t.b_base = uniform_ptr(p.Q + (size_t)e * p.q_stride);
-  gemm_k_loop<kLayNT, kMaxMT, false, 0, false, true>(acc, accx, t, smem, p.K / kBK);
+  int n_steps = p.K / kBK;
+  asm volatile("" : "+s"(n_steps));        // else what follows from it is kept over the tiles, beyond the registers
+  gemm_k_loop<kLayNT, kMaxMT, false, 0, false, true>(acc, accx, t, smem, n_steps);
   // The regions of epilogue_region lie clear of the next tile's first copies, so waves go on to it one by one; rows of fp32 need more.
   char* region = EPI == kNsOut ? smem + wave * kNsRegion : epilogue_region(smem, wave);
   if (EPI == kNsOut) __builtin_amdgcn_s_barrier();         // every wave has read its last operands, its copies have landed
@@ -282,8 +284,10 @@ __device__ __forceinline__ void ns_tile256(const NsGemmParams& p, int e, int i0,
 #pragma unroll
   for (int mt = 0; mt < kMaxMT; ++mt) {
     const int r0 = i0 + wm * 128 + mt * 32;
-    if (r0 < p.rows && c0 < p.cols)
-      ns_block<EPI, false, false, T, 4>(p, acc[mt], acc[mt], region, e, r0, c0, EPI == kNsNext || i0 != j0);
+    if (r0 >= p.rows || c0 >= p.cols) continue;
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) asm volatile("" : "+a"(acc[mt][nt]));   // until here they stay in the accumulators
+    ns_block<EPI, false, false, T, 4>(p, acc[mt], acc[mt], region, e, r0, c0, EPI == kNsNext || i0 != j0);
   }
   if (EPI == kNsOut) __builtin_amdgcn_s_barrier();         // the next tile's copies go to the same places
 }

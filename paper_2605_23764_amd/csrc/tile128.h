@@ -9,6 +9,12 @@
 
 namespace moe {
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+template <>                                // 16 bits of any kind travel as bf16x8
+__device__ __forceinline__ f32x16 mfma_16bit<true>(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
 constexpr int kTile128 = 128, kTile128Stage = 2 * kTile128 * 128;
 
 // P, Q: the matrices from the first step's columns on, row_bytes (below 2^32 / rows) from row to row; F16: fp16, else bf16.
