@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kProjThreads, NP * kProjTile + NQ * TN <= 512 ? 2 :
   const int split = b % p.splits;
   b /= p.splits;
   const int j0 = (b % p.tj) * TN, i0 = (b / p.tj) * kProjTile;
-  const int k0 = split * p.k_split, k_end = min(p.K, k0 + p.k_split);
+  const int k0 = split * p.k_split, k_end = k0 + min(p.K - k0, p.k_split);   // of up to 2^31 tokens
   const int lane = lane_id(), wave = threadIdx.x / kWave, l32 = lane & 31, lh = lane >> 5;
   const int pr = TN == 128 ? (wave >> 1) * 64 : wave * 32, qr = TN == 128 ? (wave & 1) * 64 : 0;   // the wave's first row of each side
   const TP* P = static_cast<const TP*>(p.P);
