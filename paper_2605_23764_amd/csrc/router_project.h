@@ -14,11 +14,11 @@
 #pragma once
 #include <type_traits>
 
-#include "tile128.h"
+#include "rows.h"
 
 namespace moe {
 
-constexpr int kProjTile = 128, kProjK = 64, kProjThreads = 256;
+constexpr int kProjTile = 128, kProjK = 64, kProjThreads = 256, kLdsBytes = 160 * 1024;
 
 struct ProjParams {
   const void *P, *Q;             // P(i,k): k-contiguous P[i ld_p + k], else P[k ld_p + i]
@@ -211,9 +211,9 @@ template <typename OUT> __device__ __forceinline__ void proj_store_rows(const Pr
 // Two workgroups to a CU where their LDS allows it (all but fp32's pairs of three pieces): they cover each other's waits (dx, 8192 x 7168 x 256, 260
 // registers and one workgroup: 312 us).
 template <typename TP, bool KCP, int NP, typename TQ, bool KCQ, int NQ, int TN, typename OUT>
-__global__ __launch_bounds__(kProjThreads, NP * kProjTile + NQ * TN <= 512 ? 2 : 1) void project_kernel(ProjParams p) {
+__global__ __launch_bounds__(kProjThreads, (NP * kProjTile + NQ * TN) * 256 <= kLdsBytes ? 2 : 1) void project_kernel(ProjParams p) {
   constexpr int kOrder = NP > NQ ? NP : NQ, kPieceP = kProjTile * 128, kPieceQ = TN * 128;
-  constexpr int BI = TN == 128 ? 2 : 1, BJ = BI;                 // blocks of 32 x 32 of a wave
+  constexpr int BI = TN == 128 ? 2 : 1, BJ = TN == 32 ? 1 : 2;   // blocks of 32 x 32 of a wave
   constexpr int kStage = NP * kPieceP + NQ * kPieceQ;
   constexpr int kLds = !std::is_void<OUT>::value && kStage < 4 * kProjRegion ? 4 * kProjRegion : kStage;
   __shared__ __attribute__((aligned(1024))) char smem[kLds];
@@ -251,14 +251,15 @@ __global__ __launch_bounds__(kProjThreads, NP * kProjTile + NQ * TN <= 512 ? 2 :
       if (ks * 16 >= k_end - k) break;       // the rest of the step is zeros
       bf16x8 fp[BI][NP], fq[BJ][NQ];
 #pragma unroll
-      for (int x = 0; x < BI; ++x) {
+      for (int x = 0; x < BI; ++x)
 #pragma unroll
         for (int n = 0; n < NP; ++n)
           fp[x][n] = *reinterpret_cast<const bf16x8*>(smem + n * kPieceP + proj_chunk(pr + x * 32 + l32, ks * 2 + lh));
 #pragma unroll
+      for (int x = 0; x < BJ; ++x)
+#pragma unroll
         for (int n = 0; n < NQ; ++n)
           fq[x][n] = *reinterpret_cast<const bf16x8*>(smem + NP * kPieceP + n * kPieceQ + proj_chunk(qr + x * 32 + l32, ks * 2 + lh));
-      }
       // smallest products first
 #pragma unroll
       for (int o = kOrder - 1; o >= 0; --o)
@@ -292,55 +293,10 @@ __global__ __launch_bounds__(kProjThreads, NP * kProjTile + NQ * TN <= 512 ? 2 :
               if (c + x < p.cols) dst[c + x] = acc[i][j][q * 4 + x];
         }
     } else {
-      static_assert(std::is_void<OUT>::value || TN == 128, "64 columns of a wave");
+      static_assert(std::is_void<OUT>::value || BJ == 2, "64 columns of a wave");
       proj_store_rows<OUT>(p, acc[i], r0, j0 + qr, smem + wave * kProjRegion);
     }
   }
-}
-
-// dx in bf16: both sides as pairs of bf16 (project_pairs_kernel), [rows][Ep / 32][hi 32 | lo 32], which copies to LDS take as they are.
-__global__ __launch_bounds__(256, 2) void project_dx_kernel(ProjParams p, int Ep) {
-  __shared__ __attribute__((aligned(1024))) char smem[2 * kTile128Stage];
-  static_assert(4 * kProjRegion <= 2 * kTile128Stage, "regions");
-  // 32 tile columns by 8 tile rows to a die's turn: what runs on it at a time shares operands in its L2
-  const int tiles_i = (p.rows + 127) / 128, tile = xcd_spread_tile(0, blockIdx.x, gridDim.x, tiles_i * p.tj);
-  if (tile < 0) return;
-  const int strip = __builtin_amdgcn_readfirstlane(tile / (8 * p.tj)), h = min(8, tiles_i - 8 * strip), r = tile - strip * 8 * p.tj;
-  const int j = __builtin_amdgcn_readfirstlane(r / h), i = strip * 8 + r - j * h;
-  f32x16 acc[2][2], mix[2][2];
-  tile128_multiply<true, false, 2>(static_cast<const char*>(p.P), static_cast<const char*>(p.Q), Ep * 4, p.rows, p.cols, i * 128, j * 128, Ep / 32, smem, acc,
-                                   mix);
-  const int wave = threadIdx.x / kWave;
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-#pragma unroll
-    for (int y = 0; y < 2; ++y) acc[x][y] += mix[x][y];
-    proj_store_rows<__bf16>(p, acc[x], i * 128 + (wave >> 1) * 64 + x * 32, j * 128 + (wave & 1) * 64, smem + wave * kProjRegion);
-  }
-}
-
-// Pairs of the rows [na,E] of a and, behind them, those [nb,E] of b: eight values per thread; columns past E are zeros.
-__global__ __launch_bounds__(256) void project_pairs_kernel(const float* a, int na, const float* b, int nb, int E, int Ep, char* out) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const int chunks = Ep / 8, c = (int)(i % chunks) * 8;
-  const size_t row = i / chunks;
-  if (row >= (size_t)na + nb) return;
-  const float* src = (row < (size_t)na ? a + row * E : b + (row - na) * E) + c;
-  ProjChunk<float> v = {};
-  if (c + 8 <= E) {
-    const f32x4_any lo = reinterpret_cast<const f32x4_any*>(src)[0], hi = reinterpret_cast<const f32x4_any*>(src)[1];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) { v.v[x] = lo[x]; v.v[4 + x] = hi[x]; }
-  } else {
-#pragma unroll
-    for (int x = 0; x < 7; ++x)
-      if (c + x < E) v.v[x] = src[x];
-  }
-  u32x4 piece[2];
-  proj_pieces<2>(v, piece);
-  char* dst = out + row * ((size_t)Ep * 4) + (c >> 5) * 128 + (c & 31) * 2;
-  *reinterpret_cast<u32x4*>(dst) = piece[0];
-  *reinterpret_cast<u32x4*>(dst + 64) = piece[1];
 }
 
 // out[i] = sum over the splits of part[split][i], n of them: 256 / PARTS values per workgroup, whose PARTS shares take every PARTS-th split

@@ -1,6 +1,8 @@
 // Host side of the router's projection (include/moe_ffn.h): argument checks and launches on the caller's stream.
 #include "../../include/moe_ffn.h"
 
+#include <math.h>
+
 #include <algorithm>
 
 #include "router_project.h"
@@ -10,7 +12,8 @@ using namespace moe;
 namespace {
 
 constexpr int kProjMaxE = 256;
-constexpr int kProjWorkgroups = 512;       // two per CU
+constexpr int kProjCUs = 256;
+constexpr int kProjTiles = 48;             // of 128 columns, at least
 constexpr int kProjMaxSplits = 256;
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -22,27 +25,35 @@ int check(int T, int H, int E, int dtype) {
   if (dtype != MOE_F32 && dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
   if (T < 0 || H < 1 || H > (1 << 18) || E < 1 || E > kProjMaxE) return MOE_ERR_UNSUPPORTED_SHAPE;
   // a launch holds 2^32 work-items at most
-  if ((size_t)ceil_div(T, kProjTile) * ceil_div(std::max(H, E), kProjTile) >= ((size_t)1 << 24)) return MOE_ERR_UNSUPPORTED_SHAPE;
+  if ((size_t)ceil_div(T, kProjTile) * ceil_div(std::max(H, E), 64) >= ((size_t)1 << 24)) return MOE_ERR_UNSUPPORTED_SHAPE;
   return MOE_OK;
 }
 
-// Columns of a tile: 32 for up to as many experts.
-int tile_cols(int cols) { return cols <= 32 ? 32 : kProjTile; }
+// Columns of a tile: as many as there are where that is up to 64, which leaves none of a tile's empty (4096 x 2048 x 64: 128 columns 21.4 and 24.2 us
+// forward and for dW, 64 18.6 and 21.2).  Above, 128 in bf16 with enough such tiles (8192 x 7168 x 256: 94 and 102, with 64 116 and 143; but 1024 x 4096 x
+// 128 27 and 24, with 64 22 and 19), and 64 in fp32, whose three pieces of 128 columns leave a CU one workgroup (8192 x 7168 x 256: 217 and 244, with
+// 64 195 and 205).
+int tile_cols(int rows, int cols, int dtype) {
+  if (cols <= 32) return 32;
+  return cols <= 64 || dtype == MOE_F32 || (long)ceil_div(rows, kProjTile) * ceil_div(cols, kProjTile) < kProjTiles ? 64 : 128;
+}
 
-// k's per workgroup and workgroups along k of a product of rows x cols over K.
+// k's per workgroup and workgroups along k of a product of rows x cols over K: two workgroups to a CU, but no more than pay.  A step of a
+// workgroup takes about as long as the whole chip takes to write 2^20 partial sums and read them again, so s splits cost steps / s + s rows cols / 2^20,
+// least at the root of the quotient (128 x 7168 x 256, bf16: with two to a CU, 112 splits, 17.6 us, with 58 14.4; its dW 16.2 and 8.6).  What is left
+// of two to a CU by that, but leaves most CUs one, is one each (4096 x 2048 x 64: dW in 352 workgroups 21.5 us, in 256 15.9).
 struct Split { int k, n; };
-Split split_of(int rows, int cols, int K) {
-  const long tiles = (long)ceil_div(rows, kProjTile) * ceil_div(cols, tile_cols(cols));
-  const int want = (int)std::max<long>(1, std::min<long>(kProjMaxSplits, kProjWorkgroups / std::max<long>(tiles, 1)));
+Split split_of(int rows, int cols, int K, int dtype) {
+  const int tiles = (int)std::min<long>((long)ceil_div(rows, kProjTile) * ceil_div(cols, tile_cols(rows, cols, dtype)), 1 << 20);
+  const double most = sqrt((double)ceil_div(K, kProjK) * (1 << 20) / ((double)rows * cols));
+  int want = std::min({kProjMaxSplits, 2 * kProjCUs / tiles, (int)std::min(most + 0.5, 1e6)});
+  if (want * tiles < kProjCUs * 3 / 2) want = std::min(want, kProjCUs / tiles);
+  want = std::max(want, 1);
   Split s;
   s.k = ceil_div(ceil_div(K, want), kProjK) * kProjK;
   s.n = ceil_div(K, s.k);
   return s;
 }
-// Experts in pairs, and the bytes of both sides' pairs.
-int pad_pairs(int E) { return ceil_div(E, 32) * 32; }
-constexpr int kProjRows = 1 << 21;         // rows of dx at a time: 32-bit offsets into their pairs of up to 1 KB
-size_t pairs_bytes(int T, int H, int E) { return ((size_t)std::min(T, kProjRows) + H) * pad_pairs(E) * 4; }
 size_t part_bytes(const Split& s, int rows, int cols) { return s.n > 1 ? (size_t)s.n * rows * cols * 4 : 0; }
 
 int join(const float* part, int splits, size_t n, float* out, hipStream_t s) {
@@ -56,7 +67,7 @@ int join(const float* part, int splits, size_t n, float* out, hipStream_t s) {
 }
 
 template <typename TP, bool KCP, int NP, int NQ, int TN> int run_sums(ProjParams p, float* out, void* ws, hipStream_t s) {
-  const Split sp = split_of(p.rows, p.cols, p.K);
+  const Split sp = split_of(p.rows, p.cols, p.K, sizeof(TP) == 2 ? MOE_BF16 : MOE_F32);
   p.k_split = sp.k;
   p.splits = sp.n;
   p.tj = ceil_div(p.cols, TN);
@@ -68,8 +79,10 @@ template <typename TP, bool KCP, int NP, int NQ, int TN> int run_sums(ProjParams
 }
 // P in the storage type, k-contiguous or not, against fp32 row-contiguous.
 template <bool KCP> int run_sums(const ProjParams& p, int dtype, float* out, void* ws, hipStream_t s) {
-  if (p.cols <= 32) return dtype == MOE_BF16 ? run_sums<__bf16, KCP, 1, 3, 32>(p, out, ws, s) : run_sums<float, KCP, 3, 3, 32>(p, out, ws, s);
-  return dtype == MOE_BF16 ? run_sums<__bf16, KCP, 1, 3, 128>(p, out, ws, s) : run_sums<float, KCP, 3, 3, 128>(p, out, ws, s);
+  const int tn = tile_cols(p.rows, p.cols, dtype);
+  if (tn == 32) return dtype == MOE_BF16 ? run_sums<__bf16, KCP, 1, 3, 32>(p, out, ws, s) : run_sums<float, KCP, 3, 3, 32>(p, out, ws, s);
+  if (tn == 64) return dtype == MOE_BF16 ? run_sums<__bf16, KCP, 1, 3, 64>(p, out, ws, s) : run_sums<float, KCP, 3, 3, 64>(p, out, ws, s);
+  return run_sums<__bf16, KCP, 1, 3, 128>(p, out, ws, s);
 }
 
 }  // namespace
@@ -80,7 +93,8 @@ int moe_router_project_workspace_bytes(int32_t T, int32_t H, int32_t E, size_t* 
   const int st = check(T, H, E, MOE_F32);
   if (st != MOE_OK) return st;
   if (!bytes) return MOE_ERR_INVALID_ARG;
-  *bytes = T == 0 ? 16 : std::max({pairs_bytes(T, H, E), part_bytes(split_of(T, E, H), T, E), part_bytes(split_of(H, E, T), H, E)});
+  *bytes = T == 0 ? 16 : std::max({(size_t)16, part_bytes(split_of(T, E, H, MOE_F32), T, E), part_bytes(split_of(H, E, T, MOE_F32), H, E),
+                                part_bytes(split_of(T, E, H, MOE_BF16), T, E), part_bytes(split_of(H, E, T, MOE_BF16), H, E)});
   return MOE_OK;
 }
 
@@ -125,33 +139,16 @@ int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, cons
   }
   if (d_dx) {
     ProjParams p{};
+    p.P = d_dlogits; p.Q = d_w;
+    p.ld_p = p.ld_q = p.K = E;
     p.rows = T; p.cols = H;
-    p.tj = ceil_div(H, kProjTile);
+    p.k_split = ceil_div(E, kProjK) * kProjK;
+    p.splits = 1;
+    p.tj = ceil_div(H, 64);
     p.add = d_dres; p.out = d_dx;
-    if (dtype == MOE_BF16) {
-      const int Ep = pad_pairs(E);
-      char* pairs = static_cast<char*>(d_workspace);               // W's, then dlogits'
-      p.Q = pairs;
-      p.P = pairs + (size_t)H * Ep * 4;
-      for (int t0 = 0; t0 < T; t0 += kProjRows) {
-        const int n = std::min(T - t0, kProjRows), w_rows = t0 ? 0 : H;
-        hipLaunchKernelGGL(project_pairs_kernel, dim3((unsigned)(((size_t)n + w_rows) * (Ep / 8) / 256 + 1)), dim3(256), 0, s, d_w, w_rows,
-                           d_dlogits + (size_t)t0 * E, n, E, Ep, pairs + (size_t)(H - w_rows) * Ep * 4);
-        p.rows = n;
-        p.add = d_dres ? static_cast<const uint16_t*>(d_dres) + (size_t)t0 * H : nullptr;
-        p.out = static_cast<uint16_t*>(d_dx) + (size_t)t0 * H;
-        const size_t tiles = (size_t)ceil_div(n, kProjTile) * p.tj;
-        hipLaunchKernelGGL(project_dx_kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), 0, s, p, Ep);
-        if (T - t0 <= kProjRows) break;
-      }
-    } else {
-      p.P = d_dlogits; p.Q = d_w;
-      p.ld_p = p.ld_q = p.K = E;
-      p.k_split = ceil_div(E, kProjK) * kProjK;
-      p.splits = 1;
-      hipLaunchKernelGGL((project_kernel<float, true, 3, float, true, 3, 128, float>), dim3((unsigned)((size_t)ceil_div(T, kProjTile) * p.tj)),
-                         dim3(kProjThreads), 0, s, p);
-    }
+    const dim3 grid((unsigned)((size_t)ceil_div(T, kProjTile) * p.tj)), threads(kProjThreads);
+    if (dtype == MOE_BF16) hipLaunchKernelGGL((project_kernel<float, true, 2, float, true, 2, 64, __bf16>), grid, threads, 0, s, p);
+    else hipLaunchKernelGGL((project_kernel<float, true, 3, float, true, 3, 64, float>), grid, threads, 0, s, p);
     st = launched();
   }
   return st;
