@@ -26,6 +26,7 @@ constexpr int kNsMaxParts = 256;           // partial sums of squares per matrix
 constexpr int kNsPad = 64;
 
 enum NsEpilogue { kNsGram = 0, kNsPoly = 1, kNsNext = 2, kNsOut = 3 };
+constexpr bool ns_symmetric(int epi) { return epi == kNsGram || epi == kNsPoly; }
 
 // Matrices in between: fp16 [rows][k]; as pairs [rows][k / 32][hi 32 | lo 32], so that a line of 128 bytes has both.
 struct NsGemmParams {
@@ -109,7 +110,7 @@ template <typename T, bool VEC> __device__ __forceinline__ void ns_put_rows(cons
 #pragma unroll
     for (int it = 0; it < 8; ++it) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) o[it][x] = p.w_keep * w[it][x] - p.w_step * o[it][x];
+      for (int x = 0; x < 4; ++x) o[it][x] = __builtin_fmaf(p.w_keep, w[it][x], -(p.w_step * o[it][x]));
       if (p.master && it < rows) ns_put<float, VEC>(p.master, at + it * step, n, p.N, o[it]);
     }
   }
@@ -123,15 +124,15 @@ template <typename T, bool VEC> __device__ __forceinline__ void ns_put_rows(cons
 // MIX: with the sums of the small products of pairs.
 constexpr int kNsRegion = 16384;
 template <int EPI, bool SPLIT, bool MIX, typename T, int NB>
-__device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&acc)[NB], const f32x16 (&mix)[NB], char* region, int e, int r0, int c0,
-                                         bool mirror) {
+__device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&acc)[NB], const f32x16 (&mix)[NB], char* region, int e, int r0, int c0) {
   int lane = lane_id();
   asm volatile("" : "+v"(lane));           // see store_block_via_lds
   const int l32 = lane & 31, lh = lane >> 5;
   const lds_ptr base = (lds_ptr)region;
+  // Fused by hand, here and below, so that a matrix's result is the same bits whichever tiles it goes through.
   auto value = [&](int nt, int q, int x) __attribute__((always_inline)) {
     const float v = acc[nt][q * 4 + x];
-    return (MIX ? v + mix[nt][q * 4 + x] * (1.0f / kNsLoScale) : v) * p.s_acc;
+    return MIX ? __builtin_fmaf(mix[nt][q * 4 + x], 1.0f / kNsLoScale, v) : v;
   };
   if constexpr (EPI == kNsOut) {           // rows of fp32, 64 columns at a time
     constexpr int kRow = 64 * 4 + 16;
@@ -143,7 +144,7 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           *(lds_f32x4_ptr)(base + l32 * kRow + (nt * 32 + q * 8 + lh * 4) * 4) =
-              f32x4{value(2 * h + nt, q, 0), value(2 * h + nt, q, 1), value(2 * h + nt, q, 2), value(2 * h + nt, q, 3)};
+              f32x4{value(2 * h + nt, q, 0), value(2 * h + nt, q, 1), value(2 * h + nt, q, 2), value(2 * h + nt, q, 3)} * p.s_acc;
       lds_settled();
       const int ch = lane & 15, r4 = lane >> 4, n = c0 + h * 64 + ch * 4;
       f32x4 o[8];
@@ -159,7 +160,10 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
     static_assert((SPLIT ? 2 : 1) * kHalf <= kNsRegion, "region");
     const int cols_valid = p.cols - c0;    // a multiple of 64
     const int r = lane / kLanes, ch = lane % kLanes;
-    const bool col_ok = ch * 8 < cols_valid;
+    // Of a symmetric matrix: the blocks of 64 x 64 on the diagonal and above it, the latter also as those below (sums with the operands exchanged
+    // differ by a last bit now and then: that way the matrix is symmetric, and the same whichever tiles it is made of).
+    constexpr bool SYM = ns_symmetric(EPI);
+    const bool col_ok = ch * 8 < cols_valid && (!SYM || (c0 + ch * 8) >> 6 >= r0 >> 6);
     // bytes from a matrix's first to element (row, col) of 8-column chunk `col`, col a multiple of 8
     auto offset = [&](int row, int col, int ld) __attribute__((always_inline)) {
       return SPLIT ? (size_t)row * ld * 4 + (size_t)(col >> 5) * 128 + (col & 31) * 2 : ((size_t)row * ld + col) * 2;
@@ -171,7 +175,7 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
         u32x4 v[kIts];
 #pragma unroll
         for (int it = 0; it < kIts; ++it)
-          v[it] = *reinterpret_cast<const u32x4*>(A + offset(r0 + it * kRows + r, col_ok ? c0 + ch * 8 : c0, p.ld_c) + h * 64);
+          v[it] = *reinterpret_cast<const u32x4*>(A + offset(r0 + it * kRows + r, ch * 8 < cols_valid ? c0 + ch * 8 : c0, p.ld_c) + h * 64);
 #pragma unroll
         for (int it = 0; it < kIts; ++it) *(lds_u32x4_ptr)(base + h * kHalf + (it * kRows + r) * kRow + ch * 16) = v[it];
       }
@@ -190,7 +194,11 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
           if constexpr (SPLIT) unpack_f16x4(*(lds_u32x2_ptr)(at + kHalf), b);
           const int d = r0 + l32 - (c0 + nt * 32 + q * 8 + lh * 4);      // the column of the diagonal
 #pragma unroll
-          for (int x = 0; x < 4; ++x) v[x] += p.s_a * (SPLIT ? a[x] + b[x] * (1.0f / kNsLoScale) : a[x]) + (d == x ? p.diag : 0.f);
+          for (int x = 0; x < 4; ++x)
+            v[x] = __builtin_fmaf(v[x], p.s_acc, __builtin_fmaf(p.s_a, SPLIT ? __builtin_fmaf(b[x], 1.0f / kNsLoScale, a[x]) : a[x], d == x ? p.diag : 0.f));
+        } else {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] *= p.s_acc;
         }
         const u32x2 hi = pack_f16x4(v);
         *(lds_u32x2_ptr)at = hi;
@@ -213,7 +221,7 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
 #pragma unroll
       for (int it = 0; it < kIts; ++it)
         if (col_ok) *reinterpret_cast<u32x4*>(C + offset(r0 + it * kRows + r, c0 + ch * 8, p.ld_c) + h * 64) = v[it];
-      if (mirror) {
+      if (!SYM || (c0 + NB * 32 - 1) >> 6 > r0 >> 6) {
         // 16 lanes read 4 rows x 16 columns and get a column's 4 rows each; lane (g, i): rows 8 g .. 8 g + 7 of column i
         const int g = lane >> 4, i = lane & 15;
         const lds_ptr at = base + h * kHalf + (8 * g + (i >> 2)) * kRow + (i & 3) * 8;
@@ -226,7 +234,8 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
         }
 #pragma unroll
         for (int cg = 0; cg < NB * 2; ++cg)
-          if (cg * 16 < cols_valid) *reinterpret_cast<u32x4*>(CT + offset(c0 + cg * 16 + i, r0 + 8 * g, p.ld_ct) + h * 64) = t[cg];
+          if (cg * 16 < cols_valid && (!SYM || (c0 + cg * 16) >> 6 > r0 >> 6))
+            *reinterpret_cast<u32x4*>(CT + offset(c0 + cg * 16 + i, r0 + 8 * g, p.ld_ct) + h * 64) = t[cg];
       }
     }
     wait_lgkmcnt0();                       // the region is free again
@@ -287,45 +296,43 @@ __device__ __forceinline__ void ns_tile256(const NsGemmParams& p, int e, int i0,
     if (r0 >= p.rows || c0 >= p.cols) continue;
 #pragma unroll
     for (int nt = 0; nt < 4; ++nt) asm volatile("" : "+a"(acc[mt][nt]));   // until here they stay in the accumulators
-    ns_block<EPI, false, false, T, 4>(p, acc[mt], acc[mt], region, e, r0, c0, EPI == kNsNext || i0 != j0);
+    ns_block<EPI, false, false, T, 4>(p, acc[mt], acc[mt], region, e, r0, c0);
   }
   if (EPI == kNsOut) __builtin_amdgcn_s_barrier();         // the next tile's copies go to the same places
 }
 
-// A wave's 64 x 64 of a tile of 128 x 128.
-template <int EPI, bool SPLIT, bool MIX, typename T>
-__device__ __forceinline__ void ns_blocks128(const NsGemmParams& p, const f32x16 (&acc)[2][2], const f32x16 (&mix)[2][2], char* region, int wave, int e,
-                                             int i0, int j0) {
-  const int c0 = j0 + (wave & 1) * 64;
+// A wave's blocks of 32 x 64 of a result, from row r0 of its BI blocks on.
+template <int EPI, bool SPLIT, bool MIX, typename T, int BI>
+__device__ __forceinline__ void ns_blocks(const NsGemmParams& p, const f32x16 (&acc)[BI][2], const f32x16 (&mix)[BI][2], char* region, int e, int r0, int c0) {
 #pragma unroll
-  for (int mt = 0; mt < 2; ++mt) {
-    const int r0 = i0 + (wave >> 1) * 64 + mt * 32;
-    if (r0 < p.rows && c0 < p.cols)
-      ns_block<EPI, SPLIT, MIX, T, 2>(p, acc[mt], mix[mt], region, e, r0, c0, EPI == kNsNext || i0 != j0);
-  }
+  for (int mt = 0; mt < BI; ++mt)
+    if (r0 + mt * 32 < p.rows && c0 < p.cols) ns_block<EPI, SPLIT, MIX, T, 2>(p, acc[mt], mix[mt], region, e, r0 + mt * 32, c0);
 }
 
-// One tile of 128 x 128 (tile128.h).  share, item: with splits > 1 the tile's k's are dealt to that many workgroups, of which this is number
+// One tile of SIDE x SIDE (tile128.h).  share, item: with splits > 1 the tile's k's are dealt to that many workgroups, of which this is number
 // `share`; its sums go to place `item`.
-template <int EPI, bool SPLIT, typename T, int STAGES, bool SHARES>
-__device__ __forceinline__ void ns_tile128(const NsGemmParams& p, int e, int i0, int j0, int share, int item, char* smem) {
+template <int SIDE, int EPI, bool SPLIT, typename T, int STAGES, bool SHARES>
+__device__ __forceinline__ void ns_tile(const NsGemmParams& p, int e, int i0, int j0, int share, int item, char* smem) {
+  constexpr int BI = SIDE / 64;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
   const int row_bytes = p.K * (SPLIT ? 4 : 2), all_steps = row_bytes / 128;
   const int first_step = SHARES ? all_steps * share / p.splits : 0;
   const int n_steps = SHARES ? all_steps * (share + 1) / p.splits - first_step : all_steps;
-  f32x16 acc[2][2], mix[2][2];
-  tile128_multiply<SPLIT, true, STAGES>(p.P + (size_t)e * p.p_stride + (size_t)first_step * 128, p.Q + (size_t)e * p.q_stride + (size_t)first_step * 128,
-                                        row_bytes, p.rows, p.cols, i0, j0, n_steps, smem, acc, mix);
+  f32x16 acc[BI][2], mix[BI][2];
+  tile_multiply<SIDE, SPLIT, STAGES>(p.P + (size_t)e * p.p_stride + (size_t)first_step * 128, p.Q + (size_t)e * p.q_stride + (size_t)first_step * 128,
+                                     row_bytes, p.rows, p.cols, i0, j0, n_steps, smem, acc, mix);
   if constexpr (SHARES) {
+    static_assert(SIDE == 128, "shares");
     float* dst = p.part + ((size_t)item * 4 + wave) * 4096 + lane;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < BI; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dst[((i * 2 + j) * 16 + r) * 64] = SPLIT ? acc[i][j][r] + mix[i][j][r] * (1.0f / kNsLoScale) : acc[i][j][r];
+        for (int r = 0; r < 16; ++r) dst[((i * 2 + j) * 16 + r) * 64] = SPLIT ? __builtin_fmaf(mix[i][j][r], 1.0f / kNsLoScale, acc[i][j][r]) : acc[i][j][r];
   } else {
-    ns_blocks128<EPI, SPLIT, SPLIT, T>(p, acc, mix, smem + wave * kNsRegion, wave, e, i0, j0);
+    ns_blocks<EPI, SPLIT, SPLIT, T, BI>(p, acc, mix, smem + wave * kNsRegion, e, i0 + (SIDE == 128 ? (wave >> 1) * 64 : wave * 32),
+                                        j0 + (SIDE == 128 ? (wave & 1) * 64 : 0));
   }
 }
 
@@ -343,7 +350,6 @@ template <bool SYM> __device__ __forceinline__ void ns_tile_at(int r, int ti, in
     i = strip * 4 + r - j * h;
   }
 }
-constexpr bool ns_symmetric(int epi) { return epi == kNsGram || epi == kNsPoly; }
 
 // Whole tiles of 256 x 256, by workgroups that walk on in strides.
 template <int EPI, typename T>
@@ -379,34 +385,55 @@ template <bool SYM, bool QUARTERS> __device__ __forceinline__ bool ns_tile128_at
 template <int EPI, bool SPLIT, typename T, bool QUARTERS, int STAGES, bool SHARES>
 __global__ __launch_bounds__(256, STAGES == 2 ? 2 : 1) void ns_gemm128_kernel(NsGemmParams p) {
   static_assert(STAGES == 2 || STAGES == 4, "stages");
-  __shared__ __attribute__((aligned(1024))) char smem[STAGES * kTile128Stage];
+  __shared__ __attribute__((aligned(1024))) char smem[STAGES * tile_stage(128)];
   // workgroups are dealt to the dies in turn: a die's take a contiguous eighth
   const int item = xcd_spread_tile(0, blockIdx.x, gridDim.x, SHARES ? p.tiles * p.splits : p.tiles);
   if (item < 0) return;
   const int tile = SHARES ? __builtin_amdgcn_readfirstlane(item / p.splits) : item;
   int e, i, j;
   if (!ns_tile128_at<ns_symmetric(EPI), QUARTERS>(p, p.first + tile, e, i, j)) return;
-  ns_tile128<EPI, SPLIT, T, STAGES, SHARES>(p, e, i * 128, j * 128, SHARES ? item - tile * p.splits : 0, item, smem);
+  ns_tile<128, EPI, SPLIT, T, STAGES, SHARES>(p, e, i * 128, j * 128, SHARES ? item - tile * p.splits : 0, item, smem);
 }
 
-// The shares of a tile joined, in their order: a workgroup of one wave for each of the tile's four 64 x 64, as few tiles are left over and a CU
-// pulls in only some 50 bytes a nanosecond (four waves in one workgroup, 16 shares: 16 us).
+// Tiles of 64 x 64, one to a workgroup.
+template <int EPI, bool SPLIT, typename T>
+__global__ __launch_bounds__(128, 2) void ns_gemm64_kernel(NsGemmParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[4 * tile_stage(64)];
+  const int tile = xcd_spread_tile(0, blockIdx.x, gridDim.x, p.tiles);
+  if (tile < 0) return;
+  constexpr bool SYM = ns_symmetric(EPI);
+  const int ti = p.rows / 64, tj = p.cols / 64, per = SYM ? ti * (ti + 1) / 2 : ti * tj;
+  const int e = __builtin_amdgcn_readfirstlane(tile / per);
+  int i, j;
+  ns_tile_at<SYM>(tile - e * per, ti, tj, i, j);
+  ns_tile<64, EPI, SPLIT, T, 4, false>(p, e, i * 64, j * 64, 0, 0, smem);
+}
+
+// The shares of a tile joined, in their order: a workgroup of one wave for each of the tile's eight blocks of 32 x 64, as few tiles are left over and
+// a CU pulls in only some 50 bytes a nanosecond, four shares' loads ahead of the first sum (four waves in one workgroup, a share at a time, 16 shares:
+// 16 us).
 template <int EPI, bool SPLIT, typename T, bool QUARTERS>
 __global__ __launch_bounds__(64) void ns_join_kernel(NsGemmParams p) {
   __shared__ __attribute__((aligned(1024))) char smem[kNsRegion];
-  const int tile = blockIdx.x >> 2, wave = blockIdx.x & 3;
+  const int tile = blockIdx.x >> 3, wave = (blockIdx.x >> 1) & 3, mt = blockIdx.x & 1;
   int e, i, j;
   if (!ns_tile128_at<ns_symmetric(EPI), QUARTERS>(p, p.first + tile, e, i, j)) return;
-  const float* src = p.part + ((size_t)tile * p.splits * 4 + wave) * 4096 + lane_id();
-  f32x16 acc[2][2];
+  const float* src = p.part + ((size_t)tile * p.splits * 4 + wave) * 4096 + mt * 2048 + lane_id();
+  f32x16 acc[1][2];
 #pragma unroll
-  for (int x = 0; x < 64; ++x) acc[x >> 5][(x >> 4) & 1][x & 15] = src[x * 64];
-  for (int s = 1; s < p.splits; ++s) {
-    src += 4 * 4096;
+  for (int x = 0; x < 32; ++x) acc[0][x >> 4][x & 15] = 0.f;
+  for (int s = 0; s < p.splits; s += 4) {
+    float v[4][32];
 #pragma unroll
-    for (int x = 0; x < 64; ++x) acc[x >> 5][(x >> 4) & 1][x & 15] += src[x * 64];
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int x = 0; x < 32; ++x) v[u][x] = src[(size_t)min(s + u, p.splits - 1) * 4 * 4096 + x * 64];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int x = 0; x < 32; ++x) acc[0][x >> 4][x & 15] += s + u < p.splits ? v[u][x] : 0.f;
   }
-  ns_blocks128<EPI, SPLIT, false, T>(p, acc, acc, smem, wave, e, i * 128, j * 128);
+  ns_blocks<EPI, SPLIT, false, T, 1>(p, acc, acc, smem, e, i * 128 + (wave >> 1) * 64 + mt * 32, j * 128 + (wave & 1) * 64);
 }
 
 // ---- momentum, norm, and the first X ----

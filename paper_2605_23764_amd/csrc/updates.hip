@@ -3,6 +3,7 @@
 #include "../../include/moe_ffn.h"
 
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
@@ -12,6 +13,8 @@
 using namespace moe;
 
 namespace {
+
+int env(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
 
 constexpr int kMaxSteps = 16;
 // Matrices are worked on in groups whose workspace stays below this, one at least: enough tiles at a time for the whole chip.
@@ -129,7 +132,7 @@ template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGe
     p.first = first + p.tiles;
     p.tiles = rest;
     hipLaunchKernelGGL((ns_gemm128_kernel<EPI, SPLIT, T, QUARTERS, 4, true>), grid(rest * p.splits), dim3(256), 0, s, p);
-    hipLaunchKernelGGL((ns_join_kernel<EPI, SPLIT, T, QUARTERS>), dim3(4 * rest), dim3(64), 0, s, p);
+    hipLaunchKernelGGL((ns_join_kernel<EPI, SPLIT, T, QUARTERS>), dim3(8 * rest), dim3(64), 0, s, p);
   }
 }
 
@@ -155,6 +158,12 @@ template <int EPI, typename T> void run_product(NsGemmParams p, int cus, hipStre
       }
       return;
     }
+  }
+  const int small = tiles(64), steps = p.K * (SPLIT ? 4 : 2) / 128;
+  if (small <= env("NS64", 256) && steps <= env("NSK", 16)) {
+    p.tiles = small;
+    hipLaunchKernelGGL((ns_gemm64_kernel<EPI, SPLIT, T>), dim3((unsigned)((small + 7) / 8 * 8)), dim3(128), 0, s, p);
+    return;
   }
   p.tiles = tiles(128);
   run_tiles128<EPI, SPLIT, T, false>(p, cus, s);
