@@ -3,7 +3,6 @@
 #include "../../include/moe_ffn.h"
 
 #include <math.h>
-#include <stdlib.h>
 
 #include <algorithm>
 
@@ -14,12 +13,12 @@ using namespace moe;
 
 namespace {
 
-int env(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
 
 constexpr int kMaxSteps = 16;
 // Matrices are worked on in groups whose workspace stays below this, one at least: enough tiles at a time for the whole chip.
 constexpr size_t kNsGroupBytes = (size_t)4 << 30;
 constexpr int kNsMaxShares = 256;          // partial tiles of a product's remainder
+constexpr int kNsSmallSteps = 40;          // K steps of a tile of 64 x 64 where tiles of 128 x 128 could share them
 constexpr int kNsShareSteps = 4, kNsMaxSplits = 8;   // K steps of a share, at least; shares of a tile, at most
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -116,7 +115,9 @@ struct Update {
 };
 
 // Tiles of 128 x 128 from p.first on, p.tiles of them, with fewer than one to a CU left over at the end of whole rounds.  A remainder that
-// would leave half of the CUs idle is dealt out along k as well and joined by a second launch.
+// would leave half of the CUs idle is dealt out along k as well and joined by a second launch (4 matrices of 1408 x 2048 in fp32, 264 tiles for A: 256 of
+// them 53 us, the 8 left over 9 + 6; in one launch with two workgroups to a CU the whole lasted 85).  Up to a tile per CU four stages, beyond two and
+// two workgroups (2048 x 2048 bf16 with four everywhere 308 us, so 306; 10 of 704 x 1088 in fp32 575 and 529).
 template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGemmParams p, int cus, hipStream_t s) {
   auto grid = [](int n) { return dim3((unsigned)((n + 7) / 8 * 8)); };
   const int n_steps = p.K * (SPLIT ? 4 : 2) / 128, first = p.first, tiles = p.tiles;
@@ -136,8 +137,12 @@ template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGe
   }
 }
 
-// One product of every matrix of the group.  Whole rounds of tiles of 256 x 256, one to a CU, as long as they fill the chip; what is left
-// over, and everything of a product with too few of them (or in pairs), as tiles of 128 x 128.
+// One product of every matrix of the group.  In bf16 whole rounds of tiles of 256 x 256, one to a CU, as long as they fill the chip: half the operand
+// bytes of those of 128 x 128, which two steps' pairs of fp32 would not leave registers for (4096 x 4096 and more: 1.17 PFLOP/s, with 128 x 128 0.75).
+// What is left over, and everything of a product with too few of them, as tiles of 128 x 128; a small product, whose launches wait for
+// each other's latency and not for the matrix cores, as tiles of 64 x 64 as long as two to a CU hold all (all steps of one matrix in bf16: 200 x 330
+// 105 us with 128 x 128, 71 with 64 x 64; 512 x 512 146 and 87; 1024 x 1024 233 and 132; 1408 x 1408 277 and 160; but 4 of 1024 x 2048, 544 tiles for A,
+// 279 and 335), unless the sums are long and so few that shares of them pay (256 x 4096: 113 and 147).
 template <int EPI, typename T> void run_product(NsGemmParams p, int cus, hipStream_t s) {
   constexpr bool SPLIT = sizeof(T) == 4, SYM = ns_symmetric(EPI);
   auto tiles = [&](int side) {
@@ -160,7 +165,7 @@ template <int EPI, typename T> void run_product(NsGemmParams p, int cus, hipStre
     }
   }
   const int small = tiles(64), steps = p.K * (SPLIT ? 4 : 2) / 128;
-  if (small <= env("NS64", 256) && steps <= env("NSK", 16)) {
+  if (small <= 2 * cus && (steps <= kNsSmallSteps || 2 * small > cus)) {
     p.tiles = small;
     hipLaunchKernelGGL((ns_gemm64_kernel<EPI, SPLIT, T>), dim3((unsigned)((small + 7) / 8 * 8)), dim3(128), 0, s, p);
     return;
