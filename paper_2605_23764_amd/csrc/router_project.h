@@ -148,27 +148,24 @@ template <typename T, bool KC, int R> struct ProjSide {
 };
 
 // Four columns from `at` on, n of them there: one access where all four are, at any element's address.
-template <typename T> __device__ __forceinline__ f32x4 proj_get(const T* src, size_t at, int n) {
-  typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+template <typename T> using ProjVec __attribute__((aligned(sizeof(T)))) = T __attribute__((ext_vector_type(4)));
+template <typename T> __device__ __forceinline__ ProjVec<T> proj_get(const T* src, size_t at, int n) {
+  ProjVec<T> v = {};
   if (n >= 4) {
-    const vec a = *reinterpret_cast<const vec*>(src + at);
-#pragma unroll
-    for (int x = 0; x < 4; ++x) v[x] = (float)a[x];
+    v = *reinterpret_cast<const ProjVec<T>*>(src + at);
   } else {
 #pragma unroll
     for (int x = 0; x < 3; ++x)
-      if (x < n) v[x] = (float)src[at + x];
+      if (x < n) v[x] = src[at + x];
   }
   return v;
 }
 template <typename T> __device__ __forceinline__ void proj_put(T* dst, size_t at, int n, f32x4 v) {
-  typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
   if (n >= 4) {
-    vec o;
+    ProjVec<T> o;
 #pragma unroll
     for (int x = 0; x < 4; ++x) o[x] = (T)v[x];
-    *reinterpret_cast<vec*>(dst + at) = o;
+    *reinterpret_cast<ProjVec<T>*>(dst + at) = o;
   } else {
 #pragma unroll
     for (int x = 0; x < 3; ++x)
@@ -176,36 +173,44 @@ template <typename T> __device__ __forceinline__ void proj_put(T* dst, size_t at
   }
 }
 
-// A wave's 32 rows x 64 columns of a result, whole lines, by way of the wave's place in LDS (kProjRegion bytes).
+// A wave's 32 rows x 64 columns of a result, whole lines, by way of the wave's place in LDS (kProjRegion bytes).  What is added comes ahead of
+// the sums: its way from HBM is longer than they take (dx of 8192 x 7168 x 256 with dres in HBM: 160 us, with it behind them 184).
 constexpr int kProjRow = 64 * 4 + 16, kProjRegion = 32 * kProjRow;
-template <typename OUT> __device__ __forceinline__ void proj_store_rows(const ProjParams& p, const f32x16 (&acc)[2], int r0, int c0, char* region) {
-  const int lane = lane_id(), l32 = lane & 31, lh = lane >> 5;
+template <typename OUT> struct ProjRows {
+  ProjVec<OUT> add[8];
+  __device__ __forceinline__ void fetch(const ProjParams& p, int r0, int c0) {
+    const OUT* src = static_cast<const OUT*>(p.add);
+    const int c = c0 + (lane_id() & 15) * 4, r = r0 + (lane_id() >> 4), left = p.cols - c;
+    const size_t at = (size_t)r * p.cols + c, step = (size_t)4 * p.cols;
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+    for (int it = 0; it < 8; ++it) {
+      add[it] = ProjVec<OUT>{};
+      if (src && r + it * 4 < p.rows && left > 0) add[it] = proj_get(src, at + it * step, left);
+    }
+  }
+  __device__ __forceinline__ void store(const ProjParams& p, const f32x16 (&acc)[2], int r0, int c0, char* region) const {
+    const int lane = lane_id(), l32 = lane & 31, lh = lane >> 5;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<f32x4*>(region + l32 * kProjRow + (j * 32 + q * 8 + lh * 4) * 4) =
-          f32x4{acc[j][q * 4], acc[j][q * 4 + 1], acc[j][q * 4 + 2], acc[j][q * 4 + 3]};
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  // everything that is added ahead of the first store: add may be out, so no load passes a store by itself
-  const int c = c0 + (lane & 15) * 4, rl = r0 + (lane >> 4), left = p.cols - c;
-  const OUT* add = static_cast<const OUT*>(p.add);
-  const size_t at = (size_t)rl * p.cols + c, step = (size_t)4 * p.cols;
-  f32x4 v[8];
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-  for (int it = 0; it < 8; ++it)
-    v[it] = add && rl + it * 4 < p.rows && left > 0 ? proj_get(add, at + it * step, left) : f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(region + l32 * kProjRow + (j * 32 + q * 8 + lh * 4) * 4) =
+            f32x4{acc[j][q * 4], acc[j][q * 4 + 1], acc[j][q * 4 + 2], acc[j][q * 4 + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const int c = c0 + (lane & 15) * 4, r = r0 + (lane >> 4), left = p.cols - c;
+    const size_t at = (size_t)r * p.cols + c, step = (size_t)4 * p.cols;
 #pragma unroll
-  for (int it = 0; it < 8; ++it) v[it] += *reinterpret_cast<const f32x4*>(region + (it * 4 + (lane >> 4)) * kProjRow + (lane & 15) * 16);
+    for (int it = 0; it < 8; ++it) {
+      f32x4 v = *reinterpret_cast<const f32x4*>(region + (it * 4 + (lane >> 4)) * kProjRow + (lane & 15) * 16);
 #pragma unroll
-  for (int it = 0; it < 8; ++it)
-    if (rl + it * 4 < p.rows && left > 0) proj_put(static_cast<OUT*>(p.out), at + it * step, left, v[it]);
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
+      for (int x = 0; x < 4; ++x) v[x] += (float)add[it][x];
+      if (r + it * 4 < p.rows && left > 0) proj_put(static_cast<OUT*>(p.out), at + it * step, left, v);
+    }
+  }
+};
+struct ProjNoRows {};
 
 // NP, NQ: pieces of a value of each side.  TN: columns of a tile, 128 or 32.  OUT: storage of the result of dx, void: partial sums in fp32.
 // Two workgroups to a CU where their LDS allows it (all but fp32's pairs of three pieces): they cover each other's waits (dx, 8192 x 7168 x 256, 260
@@ -234,6 +239,8 @@ __global__ __launch_bounds__(kProjThreads, (NP * kProjTile + NQ * TN) * 256 <= k
     for (int j = 0; j < BJ; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  typename std::conditional<std::is_void<OUT>::value, ProjNoRows, ProjRows<OUT>>::type rows;
+  if constexpr (!std::is_void<OUT>::value) rows.fetch(p, i0 + pr, j0 + qr);
   ProjSide<TP, KCP, kProjTile> sp;
   ProjSide<TQ, KCQ, TN> sq;
   sp.fetch(P, p.ld_p, p.rows, i0, k0, k_end);
@@ -293,8 +300,8 @@ __global__ __launch_bounds__(kProjThreads, (NP * kProjTile + NQ * TN) * 256 <= k
               if (c + x < p.cols) dst[c + x] = acc[i][j][q * 4 + x];
         }
     } else {
-      static_assert(std::is_void<OUT>::value || BJ == 2, "64 columns of a wave");
-      proj_store_rows<OUT>(p, acc[i], r0, j0 + qr, smem + wave * kProjRegion);
+      static_assert(BI == 1 && BJ == 2, "32 rows and 64 columns of a wave");
+      rows.store(p, acc[i], r0, j0 + qr, smem + wave * kProjRegion);
     }
   }
 }
