@@ -424,9 +424,10 @@ typedef struct MoeScores {
  *   with the largest keys are selected, in that order (ties: the lowest expert), and
  *   topk_w[t,j] = scale * s[t,e_j] / (renormalize ? sum over the selected of s : 1),  0 / 0 = 0
  * Scores are computed in 64 bits; keys and groups' sums of them are rounded to 44 and compared (roundings to fp32 would decide between
- * near ones); the weights are rounded once.  The bias takes part in the selection alone.  A logit of NaN counts as -inf, as in moe_route.  An expert whose logit or key is
- * -inf (or whose key is NaN) comes behind all others, with weight 0 where it is selected all the same (logit -inf); in a group's score
- * it counts 0 beside a living one.  Several logits of +inf share a softmax's probability evenly.  Keys beyond +-1e300 are equal.
+ * near ones); the weights are rounded once.  The bias takes part in the selection alone.  A logit of NaN counts as -inf, as in
+ * moe_route.  An expert whose logit or key is -inf (or whose key is NaN) comes behind all others, with weight 0 where it is selected
+ * all the same (logit -inf); in a group's score it counts 0 beside a living one.  Several logits of +inf share a softmax's probability
+ * evenly.  Keys beyond +-1e300 are equal.
  *   d_logits [T,E] f32;  d_bias [E] f32 or NULL: 0
  *   saved, d_workspace   filled as by moe_route: moe_dispatch_to_combine, moe_dispatch_to_combine_w4 or the stage entry points
  *                        follow, then moe_ffn_backward, and moe_route_scores_backward on its d_dtopk_w
@@ -457,7 +458,7 @@ int moe_bias_update(int32_t E, const int32_t* d_counts, float rate, const float*
  * logits = x W in fp32 from hidden rows in either storage type, and its backward, with fp32 sums in a fixed order.  The products under
  * them are exact where x is bf16, off by less than 2^-21 where both sides are fp32 (2^-24 on average), and by less than 2^-13 in dx in
  * bf16, ahead of its rounding.  An infinity in x, W or dlogits gives NaN in the sums that it takes part in.
- * 1 <= H <= 262144, 1 <= E <= 256.
+ * 1 <= H <= 262144, 1 <= E <= 256, T / 128 * max(H, E) / 64 (both rounded up) below 2^24.
  *   d_x [T,H] dtype;  d_w [H,E] f32;  d_logits, d_dlogits [T,E] f32
  *   d_workspace  >= moe_router_project_workspace_bytes(T, H, E)
  */

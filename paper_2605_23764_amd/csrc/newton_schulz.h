@@ -3,7 +3,10 @@
 //   X0 = u / (|u| + eps) (Frobenius norm), turned so that it has S <= L rows;  per step with its coefficients a, b, c
 //   A = X X^T;  B = a I + b A + c A^2;  X <- B X          every singular value s of X becomes a s + b s^3 + c s^5
 //
-// Per step 3 S^2 L + S^3 multiply-adds' flops, as A and B are symmetric and half of their tiles are computed: bound by the matrix cores.
+// Per step 3 S^2 L + S^3 multiply-adds' flops, as A and B are symmetric and half of their tiles are computed: bound by the matrix cores where
+// matrices are large (bf16 storage, the next X of 4 x 4096 x 7168: 822 us = 1.17 PFLOP/s with the cores busy for 73 % of the clocks, which the
+// power limit holds at 1.5 GHz; library products of that size reach 1.09 to 1.29), by the latency of a chain of 2 + 3 steps launches where they
+// are small (200 x 330: 4.1 to 5.6 us each).
 //
 // All products are of one form, C[i,j] = sum over k of P[i,k] Q[j,k] with both operands k-contiguous, which the copies to LDS and the
 // operand reads like best: A = X X^T, A^2 = A A^T, and B X = B (X^T)^T, for which X is kept together with its transpose.  A tile's
@@ -351,7 +354,8 @@ template <bool SYM> __device__ __forceinline__ void ns_tile_at(int r, int ti, in
   }
 }
 
-// Whole tiles of 256 x 256, by workgroups that walk on in strides.
+// Whole tiles of 256 x 256, by workgroups that walk on in strides.  One of the last product with its weights takes some 34 us more than one of
+// the others (1062 us for 1792 tiles, the next X 822): ten bytes per value at HBM's rate, during which the CU's matrix cores rest.
 template <int EPI, typename T>
 __global__ __launch_bounds__(kGemmThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void ns_gemm256_kernel(NsGemmParams p) {
   __shared__ __attribute__((aligned(1024))) char smem[kGemmLdsBytes];
@@ -454,7 +458,7 @@ struct NsPrepParams {
 };
 
 // Sums of squares in 64 bits, so that no update is too large or too small for them; momentum on the way.  A workgroup takes every
-// parts-th piece of 2048 values, a thread eight of them.
+// parts-th piece of 2048 values, a thread eight of them.  Bound by HBM: 4 x 4096 x 7168 in bf16 with momentum 203 us, 5.8 TB/s.
 template <typename T> __global__ __launch_bounds__(256) void ns_norm_kernel(NsPrepParams p) {
   __shared__ double s_sum[4];
   const int e = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
@@ -501,7 +505,7 @@ template <typename T> __global__ __launch_bounds__(256) void ns_norm_kernel(NsPr
 }
 
 // Tiles of 64 x 64 of the padded matrix: fp16 straight, and transposed by way of LDS; a thread has eight columns of two rows, then
-// eight rows of two columns.
+// eight rows of two columns.  Bound by HBM: 4 x 4096 x 7168 in bf16 with momentum 255 us, 4.6 TB/s.
 template <typename T, bool SPLIT> __global__ __launch_bounds__(256) void ns_first_kernel(NsPrepParams p) {
   __shared__ float s[64][65];
   __shared__ double s_norm[4];

@@ -7,14 +7,15 @@
 //
 // Scores, keys and weights are in 64 bits: between two experts whose keys differ by less than a rounding to 32 bits, the rounding would
 // decide, and with a bias the order of the logits does not (8192 tokens of 256 experts have a few such pairs; every implementation would
-// select others).  Weights are rounded once.  Keys, and groups' sums of them, are rounded to 44 bits, and the lowest 8 are the expert's number, so
-// that one maximum finds the key, the expert and the lowest of equals.
+// select others).  Weights are rounded once.  Keys, and groups' sums of them, are rounded to 44 bits, and the lowest 8 are the expert's
+// number, so that one maximum finds the key, the expert and the lowest of equals.
 //
 // Bound by instructions and their latency: about 30 in 64 bits per expert for its score, and a round of the selection is a maximum over the
 // token's lanes' first keys (each lane sorts its own, by a network of maxima and minima), behind which the winner's move up.  What is done per
 // expert is a loop on the token's keys in LDS where a lane has more than four, for the code's length: a line of it that no wave has run yet
-// costs some 300 clocks.  A token takes 16 lanes up to 128 experts, 32 beyond, of twice as many waves (8192 tokens of 256 experts in 8 groups,
-// k = 8: 20.5 us both ways, without groups 16.9; 30001 tokens of 64 experts in 4 groups, k = 6: 17.8, 28.0 with the LDS of 256), in a launch of up to 16 tokens, a wave to each, 64.
+// costs some 300 clocks.  A token takes 16 lanes up to 128 experts, 32 beyond, of twice as many waves, and 64 in a launch of up to 16 tokens,
+// a wave to each.  8192 tokens of 256 experts in 8 groups, k = 8: 20.5 us either way, without groups 16.9, where their logits' 8.4 MB take
+// 1.6; 30001 tokens of 64 experts in 4 groups, k = 6: 17.8, with the LDS that 256 need 28.0.
 #pragma once
 #include "route_select.h"
 #include "scores_math.h"
@@ -59,13 +60,16 @@ template <int LPT, typename OP> __device__ __forceinline__ double lanes_reduce(d
 #undef MOE_STEP
   if constexpr (LPT >= 32) {
     auto join = [&](auto a, auto b) __attribute__((always_inline)) {
-      v = op(__builtin_bit_cast(double, (uint64_t)(uint32_t)b[0] << 32 | (uint32_t)a[0]), __builtin_bit_cast(double, (uint64_t)(uint32_t)b[1] << 32 | (uint32_t)a[1]));
+      v = op(__builtin_bit_cast(double, (uint64_t)(uint32_t)b[0] << 32 | (uint32_t)a[0]),
+             __builtin_bit_cast(double, (uint64_t)(uint32_t)b[1] << 32 | (uint32_t)a[1]));
     };
     uint64_t u = __builtin_bit_cast(uint64_t, v);
-    join(__builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false), __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
+    join(__builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false),
+         __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
     if constexpr (LPT == 64) {
       u = __builtin_bit_cast(uint64_t, v);
-      join(__builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false), __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
+      join(__builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false),
+           __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false));
     }
   }
   return v;
