@@ -246,8 +246,85 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
   }
 }
 
+// The update's 128 x 128 of a wave from (r0, c0) on, by 32 rows x 64 columns.  W: type of the weights that are read (float: the master, else p.w), or
+// void.  Their blocks are fetched eight, or of four bytes three, ahead: a block's way from HBM each time took 34 us per tile (4 x 7168 x 4096: 1062 us,
+// so OUT_NOW).
+template <typename T, typename W, bool VEC>
+__device__ __forceinline__ void ns_out128(const NsGemmParams& p, f32x16 (&acc)[kMaxMT][4], char* region, int e, int r0, int c0) {
+  constexpr bool kWeights = !std::is_void<W>::value, kMaster = std::is_same<W, float>::value;
+  constexpr int kRow = 64 * 4 + 16, kBlocks = 2 * kMaxMT, kAhead = kMaster ? 3 : VEC ? kBlocks : kBlocks / 2;
+  typedef typename std::conditional<kWeights, W, float>::type WS;
+  typedef WS W4 __attribute__((ext_vector_type(4)));
+  int lane = lane_id();
+  asm volatile("" : "+v"(lane));
+  const int l32 = lane & 31, lh = lane >> 5, ch = lane & 15, r4 = lane >> 4;
+  const lds_ptr base = (lds_ptr)region;
+  const WS* src = kMaster ? reinterpret_cast<const WS*>(p.master) : static_cast<const WS*>(p.w);
+  W4 w[kAhead][8];
+  auto place = [&](int b, int it, int& n) __attribute__((always_inline)) {
+    const int m = r0 + (b >> 1) * 32 + r4 + it * 4;
+    n = c0 + (b & 1) * 64 + ch * 4;
+    return m < p.M && n < p.N ? ((size_t)e * p.M + m) * p.N + n : ~(size_t)0;
+  };
+  auto fetch = [&](auto bc) __attribute__((always_inline)) {
+    constexpr int b = decltype(bc)::value;
+    if constexpr (kWeights && b < kBlocks) {
+#pragma unroll
+      for (int it = 0; it < 8; ++it) {
+        int n;
+        const size_t at = place(b, it, n);
+        W4 v = {};
+        if (at != ~(size_t)0) {
+          if constexpr (VEC) {
+            v = *reinterpret_cast<const W4*>(src + at);
+          } else {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (n + x < p.N) v[x] = src[at + x];
+          }
+        }
+        w[b % kAhead][it] = v;
+      }
+    }
+  };
+  static_for<0, kAhead>([&](auto bc) __attribute__((always_inline)) { fetch(bc); });
+  __builtin_amdgcn_s_barrier();            // every wave has read its last operands, its copies have landed
+  static_for<0, kBlocks>([&](auto bc) __attribute__((always_inline)) {
+    constexpr int b = decltype(bc)::value, mt = b >> 1, h = b & 1;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      asm volatile("" : "+a"(acc[mt][2 * h + nt]));          // until here they stay in the accumulators
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x16& a = acc[mt][2 * h + nt];
+        *(lds_f32x4_ptr)(base + l32 * kRow + (nt * 32 + q * 8 + lh * 4) * 4) = f32x4{a[q * 4], a[q * 4 + 1], a[q * 4 + 2], a[q * 4 + 3]} * p.s_acc;
+      }
+    }
+    lds_settled();
+    f32x4 o[8];
+#pragma unroll
+    for (int it = 0; it < 8; ++it) o[it] = *(lds_f32x4_ptr)(base + (it * 4 + r4) * kRow + ch * 16);
+#pragma unroll
+    for (int it = 0; it < 8; ++it) {
+      int n;
+      const size_t at = place(b, it, n);
+      if constexpr (kWeights) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[it][x] = __builtin_fmaf(p.w_keep, (float)w[b % kAhead][it][x], -(p.w_step * o[it][x]));
+      }
+      if (at != ~(size_t)0) {
+        if constexpr (kMaster) ns_put<float, VEC>(p.master, at, n, p.N, o[it]);
+        ns_put<T, VEC>(static_cast<T*>(p.out), at, n, p.N, o[it]);
+      }
+    }
+    wait_lgkmcnt0();
+    lds_settled();
+    fetch(std::integral_constant<int, b + kAhead>{});
+  });
+}
+
 // One tile of 256 x 256 by four waves of 128 x 128 (the K loop of the grouped products): rows from i0, columns from j0 of matrix e.
-template <int EPI, typename T>
+template <int EPI, typename T, typename W, bool VEC>
 __device__ __forceinline__ void ns_tile256(const NsGemmParams& p, int e, int i0, int j0, char* smem) {
   int lane = lane_id();
   asm volatile("" : "+v"(lane));
@@ -289,19 +366,22 @@ __device__ __forceinline__ void ns_tile256(const NsGemmParams& p, int e, int i0,
   int n_steps = p.K / kBK;
   asm volatile("" : "+s"(n_steps));        // else what follows from it is kept over the tiles, beyond the registers
   gemm_k_loop<kLayNT, kMaxMT, false, 0, false, true>(acc, accx, t, smem, n_steps);
-  // The regions of epilogue_region lie clear of the next tile's first copies, so waves go on to it one by one; rows of fp32 need more.
-  char* region = EPI == kNsOut ? smem + wave * kNsRegion : epilogue_region(smem, wave);
-  if (EPI == kNsOut) __builtin_amdgcn_s_barrier();         // every wave has read its last operands, its copies have landed
   const int c0 = j0 + wn * 128;
+  if constexpr (EPI == kNsOut) {
+    ns_out128<T, W, VEC>(p, acc, smem + wave * kNsRegion, e, i0 + wm * 128, c0);
+    __builtin_amdgcn_s_barrier();                            // the next tile's copies go to the same places
+  } else {
+    // The regions of epilogue_region lie clear of the next tile's first copies, so waves go on to it one by one; rows of fp32 need more.
+    char* region = epilogue_region(smem, wave);
 #pragma unroll
-  for (int mt = 0; mt < kMaxMT; ++mt) {
-    const int r0 = i0 + wm * 128 + mt * 32;
-    if (r0 >= p.rows || c0 >= p.cols) continue;
+    for (int mt = 0; mt < kMaxMT; ++mt) {
+      const int r0 = i0 + wm * 128 + mt * 32;
+      if (r0 >= p.rows || c0 >= p.cols) continue;
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) asm volatile("" : "+a"(acc[mt][nt]));   // until here they stay in the accumulators
-    ns_block<EPI, false, false, T, 4>(p, acc[mt], acc[mt], region, e, r0, c0);
+      for (int nt = 0; nt < 4; ++nt) asm volatile("" : "+a"(acc[mt][nt]));   // until here they stay in the accumulators
+      ns_block<EPI, false, false, T, 4>(p, acc[mt], acc[mt], region, e, r0, c0);
+    }
   }
-  if (EPI == kNsOut) __builtin_amdgcn_s_barrier();         // the next tile's copies go to the same places
 }
 
 // A wave's blocks of 32 x 64 of a result, from row r0 of its BI blocks on.
@@ -354,9 +434,8 @@ template <bool SYM> __device__ __forceinline__ void ns_tile_at(int r, int ti, in
   }
 }
 
-// Whole tiles of 256 x 256, by workgroups that walk on in strides.  One of the last product with its weights takes some 34 us more than one of
-// the others (1062 us for 1792 tiles, the next X 822): ten bytes per value at HBM's rate, during which the CU's matrix cores rest.
-template <int EPI, typename T>
+// Whole tiles of 256 x 256, by workgroups that walk on in strides.
+template <int EPI, typename T, typename W, bool VEC>
 __global__ __launch_bounds__(kGemmThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void ns_gemm256_kernel(NsGemmParams p) {
   __shared__ __attribute__((aligned(1024))) char smem[kGemmLdsBytes];
   constexpr bool SYM = ns_symmetric(EPI);
@@ -368,7 +447,7 @@ __global__ __launch_bounds__(kGemmThreads) __attribute__((amdgpu_waves_per_eu(1,
     const int at = p.first + tile, e = __builtin_amdgcn_readfirstlane(at / per);
     int i, j;
     ns_tile_at<SYM>(at - e * per, ti, tj, i, j);
-    ns_tile256<EPI, T>(p, e, i * kBM, j * kBN, smem);
+    ns_tile256<EPI, T, W, VEC>(p, e, i * kBM, j * kBN, smem);
   }
 }
 

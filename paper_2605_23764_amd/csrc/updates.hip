@@ -155,7 +155,12 @@ template <int EPI, typename T> void run_product(NsGemmParams p, int cus, hipStre
     if (whole >= cus) {
       const bool quarters = rest > 0 && 2 * rest <= cus;
       p.tiles = quarters ? whole - rest : whole;
-      hipLaunchKernelGGL((ns_gemm256_kernel<EPI, T>), dim3(cus), dim3(kGemmThreads), 0, s, p);
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(cus), dim3(kGemmThreads), 0, s, p); };
+      const bool vec = p.N % 4 == 0;
+      if constexpr (EPI != kNsOut) launch(ns_gemm256_kernel<EPI, T, void, true>);
+      else if (p.master) launch(vec ? ns_gemm256_kernel<EPI, T, float, true> : ns_gemm256_kernel<EPI, T, float, false>);
+      else if (p.w) launch(vec ? ns_gemm256_kernel<EPI, T, T, true> : ns_gemm256_kernel<EPI, T, T, false>);
+      else launch(vec ? ns_gemm256_kernel<EPI, T, void, true> : ns_gemm256_kernel<EPI, T, void, false>);
       if (quarters) {
         p.first = 4 * p.tiles;
         p.tiles = 4 * rest;

@@ -178,6 +178,34 @@ def test_step(n, M, N, dtype):
             assert off <= f(lr) * f(scale) * err + (HALF[dtype] + 4 * U) * np.linalg.norm(W1), (e, off)
 
 
+@pytest.mark.parametrize("M,N", [(130, 200), (200, 130), (260, 203)])
+@pytest.mark.parametrize("master", [False, True], ids=["weights", "master"])
+def test_step_of_many_is_each_ones(M, N, master):
+    """As many matrices as make whole tiles: weights and fp32 ones, fetched ahead, apart and in place, sides that end inside a block and rows
+    at odd addresses; the bits of each alone, and nothing beside them."""
+    n = 270
+    gen = torch.Generator("cuda").manual_seed(M)
+    g, w = (torch.randn(n, M, N, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    m, top = torch.randn(n, M, N, generator=gen, device="cuda"), torch.randn(n, M, N, generator=gen, device="cuda")
+    ws, ws1 = _ws(n, M, N, "bf16"), _ws(1, M, N, "bf16")
+    kw = dict(lr=0.3, mu=0.9, weight_decay=0.1)
+    rim = torch.full((n * M * N + 512,), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = rim[256:-256].view(n, M, N)
+    m_out, big = torch.empty_like(m), top.clone()
+    moe.moe_muon_step(g, m, None if master else w, m_out, out, ws, master=big if master else None, **kw)
+    assert (rim[:256] == 7).all() and (rim[-256:] == 7).all()
+    same = w.clone()
+    if not master:
+        moe.moe_muon_step(g, m, same, m_out, same, ws, **kw)
+        assert torch.equal(same, out)
+    for e in (0, 1, 100, 255, 256, n - 1):
+        one, t, m1 = torch.empty(1, M, N, dtype=torch.bfloat16, device="cuda"), top[e:e + 1].clone(), torch.empty(1, M, N, device="cuda")
+        moe.moe_muon_step(g[e:e + 1].clone(), m[e:e + 1].clone(), None if master else w[e:e + 1].clone(), m1, one, ws1, master=t if master else None, **kw)
+        assert torch.equal(one[0], out[e]) and torch.equal(m1[0], m_out[e]), e
+        if master:
+            assert torch.equal(t[0], big[e]) and torch.equal(big[e].to(torch.bfloat16), out[e]), e
+
+
 def test_more_matrices_than_a_group():
     """Beyond the matrices that are worked on at a time, each is what it is alone."""
     n, M, N = 16500, 6, 20
