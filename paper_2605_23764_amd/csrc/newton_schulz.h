@@ -248,7 +248,7 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
 
 // The update's 128 x 128 of a wave from (r0, c0) on, by 32 rows x 64 columns.  W: type of the weights that are read (float: the master, else p.w), or
 // void.  Their blocks are fetched eight, or of four bytes three, ahead: a block's way from HBM each time took 34 us per tile (4 x 7168 x 4096: 1062 us,
-// so OUT_NOW).
+// so 864).
 template <typename T, typename W, bool VEC>
 __device__ __forceinline__ void ns_out128(const NsGemmParams& p, f32x16 (&acc)[kMaxMT][4], char* region, int e, int r0, int c0) {
   constexpr bool kWeights = !std::is_void<W>::value, kMaster = std::is_same<W, float>::value;
