@@ -47,17 +47,20 @@ __device__ __forceinline__ int key_number(double v) {
 }
 __device__ __forceinline__ double key_without(double v) { return __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, v) & ~255ull); }
 
+// The value of the lane that `CTRL` names: kLane1, its neighbour's; then, once lanes of one such set hold the same, that of the other two, four, eight.
+constexpr int kLane1 = 0xB1, kLane2 = 0x4E, kLane4 = 0x141, kLane8 = 0x140;
+template <int CTRL> __device__ __forceinline__ double lane_value(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xf, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
 // Over the LPT lanes of a token, in all of them.
 template <int LPT, typename OP> __device__ __forceinline__ double lanes_reduce(double v, OP op) {
-#define MOE_STEP(ctrl)                                                                                                          \
-  {                                                                                                                             \
-    const uint64_t u = __builtin_bit_cast(uint64_t, v);                                                                         \
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, ctrl, 0xf, 0xf, false);                      \
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), ctrl, 0xf, 0xf, false);              \
-    v = op(v, __builtin_bit_cast(double, (uint64_t)hi << 32 | lo));                                                             \
-  }
-  MOE_STEP(0xB1) MOE_STEP(0x4E) MOE_STEP(0x141) MOE_STEP(0x140)
-#undef MOE_STEP
+  v = op(v, lane_value<kLane1>(v));
+  v = op(v, lane_value<kLane2>(v));
+  v = op(v, lane_value<kLane4>(v));
+  v = op(v, lane_value<kLane8>(v));
   if constexpr (LPT >= 32) {
     auto join = [&](auto a, auto b) __attribute__((always_inline)) {
       v = op(__builtin_bit_cast(double, (uint64_t)(uint32_t)b[0] << 32 | (uint32_t)a[0]),
@@ -166,9 +169,20 @@ __device__ __forceinline__ void route_scores_select(const RouteParams& p, const 
     mine[at(e0) + i] = key_with(v, e0 + i);
   }
   settled();
-  uint32_t keep = ~0u;
-  if constexpr (GROUPS) {
-    double group = kKeyNone;                                     // of group s
+  double key[KP];
+#pragma unroll
+  for (int i = 0; i < KP; ++i) {
+    const double v = mine[at(e0) + i];
+    key[i] = i < n ? v : kKeyNone;
+  }
+  // a group's score of its two best keys, whose own numbers go from the sum; kKeyDead stays below every living group
+  auto group_key = [](double best, double second, int g) __attribute__((always_inline)) {
+    return key_with(best < -1e300 ? kKeyDead : key_without(best) + (second < -1e300 ? 0.0 : key_without(second)), g);
+  };
+  // lanes of a group; 0 where groups begin or end inside a lane's experts, or are no power of two up to 16 of them
+  const int whole = sc.per_group / KP, lanes = sc.per_group % KP == 0 && (whole & (whole - 1)) == 0 && whole <= 16 ? whole : 0;
+  if (GROUPS && lanes == 0) {                                    // lane s for group s
+    double group = kKeyNone;
     if (s < sc.n_group) {
       double best = kKeyNone, second = kKeyNone;
       int e = s * sc.per_group;
@@ -178,37 +192,53 @@ __device__ __forceinline__ void route_scores_select(const RouteParams& p, const 
         second = __builtin_fmax(second, __builtin_fmin(best, v));
         best = __builtin_fmax(best, v);
       }
-      // a key's own number is gone from the sum; kKeyDead stays below every living group
-      group = best < -1e300 ? kKeyDead : key_without(best) + (second < -1e300 ? 0.0 : key_without(second));
-      group = key_with(group, s);
+      group = group_key(best, second, s);
     }
-    keep = 0;
+    uint32_t keep = 0;
     for (int j = 0; j < sc.topk_group; ++j) {
       const double best = lanes_max<LPT>(group);
       keep |= 1u << key_number(best);
       if (group == best) group = kKeyNone;
     }
-  }
-  double key[KP];
 #pragma unroll
-  for (int i = 0; i < KP; ++i) {
-    const double v = mine[at(e0) + i];
-    const bool stays = !GROUPS || ((keep >> (((uint32_t)(e0 + i) * (uint32_t)sc.group_mul) >> 16)) & 1);
-    key[i] = i < n && stays ? v : kKeyNone;
+    for (int i = 0; i < KP; ++i)
+      if (!((keep >> (((uint32_t)(e0 + i) * (uint32_t)sc.group_mul) >> 16)) & 1)) key[i] = kKeyNone;
   }
   sort_keys(key);
+  double top = key[0];
+  if (GROUPS && lanes != 0) {                                    // every lane for its own group
+    double best = top, second = KP > 1 ? key[KP > 1 ? 1 : 0] : kKeyNone;
+    auto join = [&](double b, double c) __attribute__((always_inline)) {
+      second = __builtin_fmax(__builtin_fmin(best, b), __builtin_fmax(second, c));
+      best = __builtin_fmax(best, b);
+    };
+    if (lanes >= 2) join(lane_value<kLane1>(best), lane_value<kLane1>(second));
+    if (lanes >= 4) join(lane_value<kLane2>(best), lane_value<kLane2>(second));
+    if (lanes >= 8) join(lane_value<kLane4>(best), lane_value<kLane4>(second));
+    if (lanes >= 16) join(lane_value<kLane8>(best), lane_value<kLane8>(second));
+    double group = n > 0 ? group_key(best, second, ((uint32_t)e0 * (uint32_t)sc.group_mul) >> 16) : kKeyNone;
+    bool stays = false;
+    for (int j = 0; j < sc.topk_group; ++j)
+      if (group == lanes_max<LPT>(group)) {
+        stays = true;
+        group = kKeyNone;
+      }
+    top = stays ? top : kKeyNone;
+  }
+  // the lane's keys behind its first, and none behind them, for the rounds to come
+  double* rest = mine + at(e0);
+  if constexpr (KP > 1) {
+#pragma unroll
+    for (int i = 1; i < KP; ++i) rest[i - 1] = key[i];
+    rest[KP - 1] = kKeyNone;
+  }
   double chosen = kKeyNone;                                      // of slot s
   for (int j = 0; j < p.k; ++j) {
-    const double best = lanes_max<LPT>(key[0]);
+    const double best = lanes_max<LPT>(top);
     chosen = s == j ? best : chosen;
-    const bool winner = key[0] == best;
-    double up = kKeyNone;
-#pragma unroll
-    for (int i = KP - 1; i >= 0; --i) {
-      double v = key[i];
-      asm("" : "+v"(v));                                         // as a value: a choice between two places of the array becomes one by number
-      key[i] = winner ? up : v;
-      up = v;
+    if (top == best) {
+      if constexpr (KP == 1) top = kKeyNone;
+      else top = *rest++;
     }
   }
   const bool slot = s < p.k;
