@@ -464,8 +464,8 @@ __global__ __launch_bounds__(THREADS) void route_scores_kernel(RouteParams p, Sc
   __shared__ double s_slots[THREADS / kWave * slot_words(KP)];
   route_chunk(p, blockIdx.x, s_idx, nullptr, SelectScores<GROUPS, LPT, KP>{sc, s_slots});
 }
-// One launch as long as a token has a wave: 256 experts in 8 groups, k = 8, on the device, T = 8 10.7 us against 10.7 + 4.4 in two launches,
-// T = 16 14.1 against 12.8 + 4.4; with two tokens to a wave T = 64 32 against 19 + 4.4.
+// One launch as long as a token has a wave: 256 experts in 8 groups, k = 8, T = 1 7.4 us against 12.4 in two launches, T = 8 9.3 against 14.4,
+// T = 16 11.8 against 15.9; with more tokens to a wave T = 64 32 against 23 (20 since then).
 constexpr int kScoresOneT = kRouteOneThreads / kWave;
 template <bool BF16, bool GROUPS>
 __global__ __launch_bounds__(kRouteOneThreads) void route_scores_one_kernel(SchedParams<BF16> sp, ScoreParams sc) {

@@ -11,11 +11,12 @@
 // number, so that one maximum finds the key, the expert and the lowest of equals.
 //
 // Bound by instructions and their latency: about 30 in 64 bits per expert for its score, and a round of the selection is a maximum over the
-// token's lanes' first keys (each lane sorts its own, by a network of maxima and minima), behind which the winner's move up.  What is done per
-// expert is a loop on the token's keys in LDS where a lane has more than four, for the code's length: a line of it that no wave has run yet
-// costs some 300 clocks.  A token takes 16 lanes up to 128 experts, 32 beyond, of twice as many waves, and 64 in a launch of up to 16 tokens,
-// a wave to each.  8192 tokens of 256 experts in 8 groups, k = 8: 20.5 us either way, without groups 16.9, where their logits' 8.4 MB take
-// 1.6; 30001 tokens of 64 experts in 4 groups, k = 6: 17.8, with the LDS that 256 need 28.0.
+// token's lanes' first keys (each lane sorts its own, by a network of maxima and minima), behind which the winner takes its next from LDS
+// (moved up in registers instead, and groups scored by a loop over their experts: 8192 x 256 21.6 us, so 18.4).  Groups of whole lanes are
+// scored from the lanes' two best, joined; others by that loop.  What is done per expert is a loop on the token's keys in LDS where a lane
+// has more than four, for the code's length: a line of it that no wave has run yet costs some 300 clocks.  A token takes 16 lanes up to 128 experts, 32 beyond, of twice as many waves, and 64 in a launch of up to 16 tokens,
+// a wave to each.  8192 tokens of 256 experts in 8 groups, k = 8: 18.4 us, without groups 17, where their logits' 8.4 MB take 1.6; 30001
+// tokens of 64 experts in 4 groups, k = 6: 17.4 (in another form 17.8, and 28.0 with the LDS that 256 need).
 #pragma once
 #include "route_select.h"
 #include "scores_math.h"

@@ -5,8 +5,9 @@
 // steps under way.  Lines and their swizzle are those of the grouped products.  Pairs: a row is [k / 32][hi 32 | lo 32], so that a line of
 // 128 bytes has both halves of 32 k, and every fragment read serves three products: hi hi into acc, lo hi and hi lo into mix.
 //
-// With pairs, 264 tiles of 64 steps in 53 us: the MFMAs alone would take 25, with launch and epilogue 35, the copies alone 30, without copies 42,
-// without operand reads 41; one wave on a SIMD does not cover what a step's barrier costs it.
+// With pairs, 256 tiles of 128 x 128 of 64 steps in 53 us: the MFMAs alone would take 25, with launch and epilogue 35, the copies alone 30,
+// without copies 42, without operand reads 41.  A step's 64 KB of operand reads and 32 KB of copies keep LDS busy for as many clocks as its MFMAs
+// last, and one wave on a SIMD does not cover what the barrier costs it.
 #pragma once
 #include "gemm_bf16.h"
 
