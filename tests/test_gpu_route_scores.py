@@ -91,6 +91,43 @@ def test_selection_tables_weights_and_gradient(T, E, k, G, top, El, base, kind, 
             assert torch.equal(same, got), over
 
 
+@pytest.mark.parametrize("kind", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("E,G,top,k", [(256, 2, 1, 16), (256, 4, 3, 8), (256, 16, 5, 8), (160, 8, 2, 8), (128, 2, 1, 5), (128, 8, 8, 6), (96, 6, 2, 8), (64, 2, 2, 6),
+                                       (64, 16, 3, 4), (48, 4, 1, 12), (32, 16, 4, 8), (32, 4, 2, 1), (24, 2, 1, 3), (16, 16, 7, 7), (16, 4, 3, 5), (8, 2, 1, 4)])
+def test_groups_of_every_width(E, G, top, k, kind):
+    """Groups of whole lanes, one to sixteen of them, of more, of no power of two, that end inside a lane; few tokens and many; holes, ties of
+    groups and of keys."""
+    r = np.random.default_rng(E + G)
+    bias = (r.integers(-2, 3, size=E) / 8).astype(np.float32)
+    for T in (1, 16, 37, 200):
+        L = (2 * r.normal(size=(T, E))).astype(np.float32)
+        L[r.random((T, E)) < 0.2] = -np.inf
+        L[::3] = np.round(L[::3])                                    # ties
+        if T > 20:
+            L[5] = 0.0
+            L[6, : E // G] = -np.inf
+            L[7, E // G:] = np.nan
+            L[8] = -np.inf
+        for b in (None, bias):
+            _, saved, _ = _route(torch.from_numpy(L).cuda(), moe.make_scores(kind, G, top, True, 1.0), None if b is None else torch.from_numpy(b).cuda(), k, E, 0)
+            idx, s = ro.select(L, kind, k, b, G, top)
+            got = saved.topk_idx.cpu().numpy()
+            # Two groups' sums that are equal as real numbers (s + 1/8 and s - 1/8 against s and s) are not after roundings, the oracle's neither.
+            # Keys below 2 are rounded to 44 bits behind the point's first, off by 2^-45 at most, a sum of two of them below 4 by another 2^-44:
+            # two groups are in doubt, and only then, within 2 (2 * 2^-45 + 2^-44) = 2^-42.
+            for t in np.flatnonzero((got != idx).any(1)):
+                key = np.where(np.isnan(L[t]) | (L[t] == -np.inf), -np.inf, s[t] + (0.0 if b is None else b.astype(np.float64)))
+                two = np.sort(key.reshape(G, -1), axis=1)[:, ::-1][:, :2]
+                value = two[:, 0] + np.where(two[:, 1:].max(axis=1, initial=-np.inf) > -np.inf, two[:, 1:].max(axis=1, initial=-np.inf), 0.0)
+                order = np.sort(value)[::-1]
+                assert order[top - 1] - order[top] <= 2.0 ** -42, (T, t)
+                stay = set(got[t] // (E // G))
+                assert all(value[g] >= order[top - 1] - 2.0 ** -42 for g in stay) and (np.diff(key[got[t]]) <= 0).all(), (T, t)
+                idx[t] = got[t]
+            w = ro.weights(s, idx, True, 1.0)
+            close(saved.topk_w, w, U * w * 1.001 + 2.0 ** -149, "topk_w")
+
+
 def test_keys_that_fp32_cannot_tell_apart():
     """Biased scores that differ by less than a rounding to fp32: the order is the definition's."""
     T, E, k = 500, 64, 6
