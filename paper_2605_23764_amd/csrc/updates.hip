@@ -116,7 +116,7 @@ struct Update {
 
 // Tiles of 128 x 128 from p.first on, p.tiles of them, with fewer than one to a CU left over at the end of whole rounds.  A remainder that
 // would leave half of the CUs idle is dealt out along k as well and joined by a second launch (4 matrices of 1408 x 2048 in fp32, 264 tiles for A: 256 of
-// them 53 us, the 8 left over 9 + 6; in one launch with two workgroups to a CU the whole lasted 85).  Up to a tile per CU four stages, beyond two and
+// them 53 us, the 8 left over 9 + 6; all in one launch with two workgroups to a CU 81).  Up to a tile per CU four stages, beyond two and
 // two workgroups (2048 x 2048 bf16 with four everywhere 308 us, so 306; 10 of 704 x 1088 in fp32 575 and 529).
 template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGemmParams p, int cus, hipStream_t s) {
   auto grid = [](int n) { return dim3((unsigned)((n + 7) / 8 * 8)); };
@@ -138,7 +138,7 @@ template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGe
 }
 
 // One product of every matrix of the group.  In bf16 whole rounds of tiles of 256 x 256, one to a CU, as long as they fill the chip: half the operand
-// bytes of those of 128 x 128, which two steps' pairs of fp32 would not leave registers for (4096 x 4096 and more: 1.17 PFLOP/s, with 128 x 128 0.75).
+// bytes of those of 128 x 128, which two steps' pairs of fp32 would not leave registers for (the next X of 4 x 4096 x 7168 822 us, 1.17 PFLOP/s, with 128 x 128 1073).
 // What is left over, and everything of a product with too few of them, as tiles of 128 x 128; a small product, whose launches wait for
 // each other's latency and not for the matrix cores, as tiles of 64 x 64 as long as two to a CU hold all (all steps of one matrix in bf16: 200 x 330
 // 105 us with 128 x 128, 71 with 64 x 64; 512 x 512 146 and 87; 1024 x 1024 233 and 132; 1408 x 1408 277 and 160; but 4 of 1024 x 2048, 544 tiles for A,
