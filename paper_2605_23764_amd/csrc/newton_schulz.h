@@ -17,14 +17,14 @@
 // the usual ones), so fp16's range suffices and its 11 bits are worth eight times bf16's 8: the error of a step's roundings is
 // multiplied by up to a per later step (3.4^4 = 140 for the first).  Every matrix is stored times a power of two that brings its
 // entries near 1 where they are typical, clear of both ends of the range: X by about sqrt(L), A and B by about S.
-// fp32 storage: operands are pairs of fp16 (hi, and the rest times 2^11), products hi hi + hi lo + lo hi, so 22 bits.
+// fp32 storage: operands are pairs of fp16, hi and the rest, products hi hi + hi lo + lo hi in one sum, so 22 bits.  Their scale brings the
+// bound of the entries, not the entries, to the top of the range, 2^14: a rest is then off by 2^-25 at most, below 2^-32 of a typical entry.
 #pragma once
 #include "rows.h"
 #include "tile128.h"
 
 namespace moe {
 
-constexpr float kNsLoScale = 2048.0f;      // what the second half of a pair is stored times
 constexpr int kNsMaxParts = 256;           // partial sums of squares per matrix
 constexpr int kNsPad = 64;
 
@@ -124,18 +124,16 @@ template <typename T, bool VEC> __device__ __forceinline__ void ns_put_rows(cons
 
 // A wave's 32 rows x 32 NB columns of a result from (r0, c0) on, by way of its LDS region (kNsRegion bytes).
 // acc[nt]: lane (l32, lh) holds row l32 and, per q, columns 32 nt + 8 q + 4 lh .. + 3.
-// MIX: with the sums of the small products of pairs.
 constexpr int kNsRegion = 16384;
-template <int EPI, bool SPLIT, bool MIX, typename T, int NB>
-__device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&acc)[NB], const f32x16 (&mix)[NB], char* region, int e, int r0, int c0) {
+template <int EPI, bool SPLIT, typename T, int NB>
+__device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&acc)[NB], char* region, int e, int r0, int c0) {
   int lane = lane_id();
   asm volatile("" : "+v"(lane));           // see store_block_via_lds
   const int l32 = lane & 31, lh = lane >> 5;
   const lds_ptr base = (lds_ptr)region;
   // Fused by hand, here and below, so that a matrix's result is the same bits whichever tiles it goes through.
   auto value = [&](int nt, int q, int x) __attribute__((always_inline)) {
-    const float v = acc[nt][q * 4 + x];
-    return MIX ? __builtin_fmaf(mix[nt][q * 4 + x], 1.0f / kNsLoScale, v) : v;
+    return acc[nt][q * 4 + x];
   };
   if constexpr (EPI == kNsOut) {           // rows of fp32, 64 columns at a time
     constexpr int kRow = 64 * 4 + 16;
@@ -198,7 +196,7 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
           const int d = r0 + l32 - (c0 + nt * 32 + q * 8 + lh * 4);      // the column of the diagonal
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            v[x] = __builtin_fmaf(v[x], p.s_acc, __builtin_fmaf(p.s_a, SPLIT ? __builtin_fmaf(b[x], 1.0f / kNsLoScale, a[x]) : a[x], d == x ? p.diag : 0.f));
+            v[x] = __builtin_fmaf(v[x], p.s_acc, __builtin_fmaf(p.s_a, SPLIT ? a[x] + b[x] : a[x], d == x ? p.diag : 0.f));
         } else {
 #pragma unroll
           for (int x = 0; x < 4; ++x) v[x] *= p.s_acc;
@@ -209,7 +207,7 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
           float h[4];
           unpack_f16x4(hi, h);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) h[x] = (v[x] - h[x]) * kNsLoScale;
+          for (int x = 0; x < 4; ++x) h[x] = v[x] - h[x];
           *(lds_u32x2_ptr)(at + kHalf) = pack_f16x4(h);
         }
       }
@@ -379,17 +377,17 @@ __device__ __forceinline__ void ns_tile256(const NsGemmParams& p, int e, int i0,
       if (r0 >= p.rows || c0 >= p.cols) continue;
 #pragma unroll
       for (int nt = 0; nt < 4; ++nt) asm volatile("" : "+a"(acc[mt][nt]));   // until here they stay in the accumulators
-      ns_block<EPI, false, false, T, 4>(p, acc[mt], acc[mt], region, e, r0, c0);
+      ns_block<EPI, false, T, 4>(p, acc[mt], region, e, r0, c0);
     }
   }
 }
 
 // A wave's blocks of 32 x 64 of a result, from row r0 of its BI blocks on.
-template <int EPI, bool SPLIT, bool MIX, typename T, int BI>
-__device__ __forceinline__ void ns_blocks(const NsGemmParams& p, const f32x16 (&acc)[BI][2], const f32x16 (&mix)[BI][2], char* region, int e, int r0, int c0) {
+template <int EPI, bool SPLIT, typename T, int BI>
+__device__ __forceinline__ void ns_blocks(const NsGemmParams& p, const f32x16 (&acc)[BI][2], char* region, int e, int r0, int c0) {
 #pragma unroll
   for (int mt = 0; mt < BI; ++mt)
-    if (r0 + mt * 32 < p.rows && c0 < p.cols) ns_block<EPI, SPLIT, MIX, T, 2>(p, acc[mt], mix[mt], region, e, r0 + mt * 32, c0);
+    if (r0 + mt * 32 < p.rows && c0 < p.cols) ns_block<EPI, SPLIT, T, 2>(p, acc[mt], region, e, r0 + mt * 32, c0);
 }
 
 // One tile of SIDE x SIDE (tile128.h).  share, item: with splits > 1 the tile's k's are dealt to that many workgroups, of which this is number
@@ -401,9 +399,9 @@ __device__ __forceinline__ void ns_tile(const NsGemmParams& p, int e, int i0, in
   const int row_bytes = p.K * (SPLIT ? 4 : 2), all_steps = row_bytes / 128;
   const int first_step = SHARES ? all_steps * share / p.splits : 0;
   const int n_steps = SHARES ? all_steps * (share + 1) / p.splits - first_step : all_steps;
-  f32x16 acc[BI][2], mix[BI][2];
+  f32x16 acc[BI][2];
   tile_multiply<SIDE, SPLIT, STAGES>(p.P + (size_t)e * p.p_stride + (size_t)first_step * 128, p.Q + (size_t)e * p.q_stride + (size_t)first_step * 128,
-                                     row_bytes, p.rows, p.cols, i0, j0, n_steps, smem, acc, mix);
+                                     row_bytes, p.rows, p.cols, i0, j0, n_steps, smem, acc);
   if constexpr (SHARES) {
     static_assert(SIDE == 128, "shares");
     float* dst = p.part + ((size_t)item * 4 + wave) * 4096 + lane;
@@ -412,9 +410,9 @@ __device__ __forceinline__ void ns_tile(const NsGemmParams& p, int e, int i0, in
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dst[((i * 2 + j) * 16 + r) * 64] = SPLIT ? __builtin_fmaf(mix[i][j][r], 1.0f / kNsLoScale, acc[i][j][r]) : acc[i][j][r];
+        for (int r = 0; r < 16; ++r) dst[((i * 2 + j) * 16 + r) * 64] = acc[i][j][r];
   } else {
-    ns_blocks<EPI, SPLIT, SPLIT, T, BI>(p, acc, mix, smem + wave * kNsRegion, e, i0 + (SIDE == 128 ? (wave >> 1) * 64 : wave * 32),
+    ns_blocks<EPI, SPLIT, T, BI>(p, acc, smem + wave * kNsRegion, e, i0 + (SIDE == 128 ? (wave >> 1) * 64 : wave * 32),
                                         j0 + (SIDE == 128 ? (wave & 1) * 64 : 0));
   }
 }
@@ -478,6 +476,33 @@ __global__ __launch_bounds__(256, STAGES == 2 ? 2 : 1) void ns_gemm128_kernel(Ns
   ns_tile<128, EPI, SPLIT, T, STAGES, SHARES>(p, e, i * 128, j * 128, SHARES ? item - tile * p.splits : 0, item, smem);
 }
 
+// Tiles of 256 x 256 of pairs, one to a workgroup: 4 x 4096 x 4096, the next X 1273 us, 1.30 PFLOP/s of its three products.
+template <int EPI, typename T>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void ns_gemm256_pairs_kernel(NsGemmParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * tile_stage(256)];
+  constexpr bool SYM = ns_symmetric(EPI);
+  const int tile = xcd_spread_tile(0, blockIdx.x, gridDim.x, p.tiles);
+  if (tile < 0) return;
+  const int ti = (p.rows + 255) / 256, tj = (p.cols + 255) / 256, per = SYM ? ti * (ti + 1) / 2 : ti * tj;
+  const int at = p.first + tile, e = __builtin_amdgcn_readfirstlane(at / per);
+  int i, j;
+  ns_tile_at<SYM>(at - e * per, ti, tj, i, j);
+  f32x16 acc[4][4];
+  tile_multiply<256, true, 2>(p.P + (size_t)e * p.p_stride, p.Q + (size_t)e * p.q_stride, p.K * 4, p.rows, p.cols, i * 256, j * 256, p.K / 32, smem, acc);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+  for (int mt = 0; mt < 4; ++mt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r0 = i * 256 + (wave >> 1) * 128 + mt * 32, c0 = j * 256 + (wave & 1) * 128 + h * 64;
+      if (r0 >= p.rows || c0 >= p.cols) continue;
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) asm volatile("" : "+a"(acc[mt][2 * h + nt]));   // until here they stay in the accumulators
+      const f32x16 block[2] = {acc[mt][2 * h], acc[mt][2 * h + 1]};
+      ns_block<EPI, true, T, 2>(p, block, smem + wave * kNsRegion, e, r0, c0);
+    }
+}
+
 // Tiles of 64 x 64, one to a workgroup.
 template <int EPI, bool SPLIT, typename T>
 __global__ __launch_bounds__(128, 2) void ns_gemm64_kernel(NsGemmParams p) {
@@ -516,7 +541,7 @@ __global__ __launch_bounds__(64) void ns_join_kernel(NsGemmParams p) {
 #pragma unroll
       for (int x = 0; x < 32; ++x) acc[0][x >> 4][x & 15] += s + u < p.splits ? v[u][x] : 0.f;
   }
-  ns_blocks<EPI, SPLIT, false, T, 1>(p, acc, acc, smem, e, i * 128 + (wave >> 1) * 64 + mt * 32, j * 128 + (wave & 1) * 64);
+  ns_blocks<EPI, SPLIT, T, 1>(p, acc, smem, e, i * 128 + (wave >> 1) * 64 + mt * 32, j * 128 + (wave & 1) * 64);
 }
 
 // ---- momentum, norm, and the first X ----
@@ -642,7 +667,7 @@ template <typename T, bool SPLIT> __global__ __launch_bounds__(256) void ns_firs
       unpack_f16x4(h0, c);
       unpack_f16x4(h1, d);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) { c[x] = (a[x] - c[x]) * kNsLoScale; d[x] = (b[x] - d[x]) * kNsLoScale; }
+      for (int x = 0; x < 4; ++x) { c[x] = a[x] - c[x]; d[x] = b[x] - d[x]; }
       const u32x2 l0 = pack_f16x4(c), l1 = pack_f16x4(d);
       *reinterpret_cast<u32x4*>(at + 64) = u32x4{l0.x, l0.y, l1.x, l1.y};
     }

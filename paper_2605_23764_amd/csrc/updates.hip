@@ -70,12 +70,12 @@ struct Steps {
   int ex, ea[kMaxSteps], eb[kMaxSteps];    // stored: X 2^ex, A 2^ea, B 2^eb
 };
 int floor_log2(double v) { return (int)floor(log2(v)); }
-// false: the coefficients let singular values grow out of bounds
-bool make_steps(Steps& s, int n, const float* coefs, int S, int L) {
+// pairs: scales of pairs of fp16 (newton_schulz.h).  false: the coefficients let singular values grow out of bounds
+bool make_steps(Steps& s, int n, const float* coefs, int S, int L, bool pairs) {
   static const float usual[3] = {3.4445f, -4.7750f, 2.0315f};
   s.n = n;
   s.ex = floor_log2((double)L) / 2;
-  double top = 1.0;                        // largest singular value possible
+  double top = 1.0, largest = 1.0;         // largest singular value possible, now and in any step
   for (int i = 0; i < n; ++i) {
     for (int j = 0; j < 3; ++j) {
       s.c[i][j] = coefs ? coefs[3 * i + j] : usual[j];
@@ -95,11 +95,13 @@ bool make_steps(Steps& s, int n, const float* coefs, int S, int L) {
       pmax = std::max(pmax, p(-a / (3 * b)));
     }
     // entries are at most the largest singular value; 2^15 leaves a factor of two for roundings
-    s.ea[i] = std::min(floor_log2(S), 15 - (int)ceil(log2(t)));
-    s.eb[i] = std::min(floor_log2(S), 15 - (int)ceil(log2(std::max(qmax, 1e-6))));
+    s.ea[i] = pairs ? 14 - (int)ceil(log2(t)) : std::min(floor_log2(S), 15 - (int)ceil(log2(t)));
+    s.eb[i] = pairs ? 14 - (int)ceil(log2(std::max(qmax, 1e-6))) : std::min(floor_log2(S), 15 - (int)ceil(log2(std::max(qmax, 1e-6))));
     top = std::max(pmax, 1e-3) * 1.0001;
     if (!(qmax <= 1024.0) || !(top <= 32.0)) return false;
+    largest = std::max(largest, top);
   }
+  if (pairs) s.ex = 14 - (int)ceil(log2(largest));
   return true;
 }
 
@@ -137,12 +139,12 @@ template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGe
   }
 }
 
-// One product of every matrix of the group.  In bf16 whole rounds of tiles of 256 x 256, one to a CU, as long as they fill the chip: half the operand
-// bytes of those of 128 x 128, which two steps' pairs of fp32 would not leave registers for (the next X of 4 x 4096 x 7168 822 us, 1.17 PFLOP/s, with 128 x 128 1073).
-// What is left over, and everything of a product with too few of them, as tiles of 128 x 128; a small product, whose launches wait for
-// each other's latency and not for the matrix cores, as tiles of 64 x 64 as long as two to a CU hold all (all steps of one matrix in bf16: 200 x 330
-// 105 us with 128 x 128, 71 with 64 x 64; 512 x 512 146 and 87; 1024 x 1024 233 and 132; 1408 x 1408 277 and 160; but 4 of 1024 x 2048, 544 tiles for A,
-// 279 and 335), unless the sums are long and so few that shares of them pay (256 x 4096: 113 and 147).
+// One product of every matrix of the group.  Whole rounds of tiles of 256 x 256, one to a CU, as long as they fill the chip: half the operand bytes of
+// those of 128 x 128 (the next X of 4 x 4096 x 7168 in bf16 822 us, 1.17 PFLOP/s, with 128 x 128 1073; of 4 x 4096 x 4096 in fp32 1273, 1.30 PFLOP/s of
+// its three products, with 128 x 128 1487).  What is left over, and everything of a product with too few of them, as tiles of 128 x 128; a small
+// product, whose launches wait for each other's latency and not for the matrix cores, as tiles of 64 x 64 as long as two to a CU hold all (all steps
+// of one matrix in bf16: 200 x 330 105 us with 128 x 128, 71 with 64 x 64; 512 x 512 146 and 87; 1024 x 1024 233 and 132; 1408 x 1408 277 and 160; but
+// 4 of 1024 x 2048, 544 tiles for A, 279 and 335), unless the sums are long and so few that shares of them pay (256 x 4096: 113 and 147).
 template <int EPI, typename T> void run_product(NsGemmParams p, int cus, hipStream_t s) {
   constexpr bool SPLIT = sizeof(T) == 4, SYM = ns_symmetric(EPI);
   auto tiles = [&](int side) {
@@ -150,24 +152,26 @@ template <int EPI, typename T> void run_product(NsGemmParams p, int cus, hipStre
     return p.n * (SYM ? ti * (ti + 1) / 2 : ti * tj);
   };
   p.first = 0;
-  if constexpr (!SPLIT) {
-    const int whole = tiles(256), rest = whole % cus;
-    if (whole >= cus) {
-      const bool quarters = rest > 0 && 2 * rest <= cus;
-      p.tiles = quarters ? whole - rest : whole;
+  const int whole = tiles(256), rest = whole % cus;
+  if (whole >= cus) {
+    const bool quarters = rest > 0 && 2 * rest <= cus;
+    p.tiles = quarters ? whole - rest : whole;
+    if constexpr (SPLIT) {
+      hipLaunchKernelGGL((ns_gemm256_pairs_kernel<EPI, T>), dim3((unsigned)((p.tiles + 7) / 8 * 8)), dim3(256), 0, s, p);
+    } else {
       auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(cus), dim3(kGemmThreads), 0, s, p); };
       const bool vec = p.N % 4 == 0;
       if constexpr (EPI != kNsOut) launch(ns_gemm256_kernel<EPI, T, void, true>);
       else if (p.master) launch(vec ? ns_gemm256_kernel<EPI, T, float, true> : ns_gemm256_kernel<EPI, T, float, false>);
       else if (p.w) launch(vec ? ns_gemm256_kernel<EPI, T, T, true> : ns_gemm256_kernel<EPI, T, T, false>);
       else launch(vec ? ns_gemm256_kernel<EPI, T, void, true> : ns_gemm256_kernel<EPI, T, void, false>);
-      if (quarters) {
-        p.first = 4 * p.tiles;
-        p.tiles = 4 * rest;
-        run_tiles128<EPI, false, T, true>(p, cus, s);
-      }
-      return;
     }
+    if (quarters) {
+      p.first = 4 * p.tiles;
+      p.tiles = 4 * rest;
+      run_tiles128<EPI, SPLIT, T, true>(p, cus, s);
+    }
+    return;
   }
   const int small = tiles(64), steps = p.K * (SPLIT ? 4 : 2) / 128;
   if (small <= 2 * cus && (steps <= kNsSmallSteps || 2 * small > cus)) {
@@ -292,7 +296,7 @@ int moe_orthogonalize(int32_t B, int32_t M, int32_t N, int dtype, const void* d_
   int st = check_matrices(B, M, N, dtype);
   if (st != MOE_OK) return st;
   Steps s;
-  if (steps < 1 || steps > kMaxSteps || !(eps > 0.f) || isinf(eps) || !make_steps(s, steps, coefs, std::min(M, N), std::max(M, N)))
+  if (steps < 1 || steps > kMaxSteps || !(eps > 0.f) || isinf(eps) || !make_steps(s, steps, coefs, std::min(M, N), std::max(M, N), dtype == MOE_F32))
     return MOE_ERR_INVALID_ARG;
   if (B == 0) return MOE_OK;
   if (!good(d_u) || !good(d_out)) return MOE_ERR_INVALID_ARG;
@@ -311,7 +315,7 @@ int moe_muon_step(int32_t B, int32_t M, int32_t N, int dtype, const void* d_g, c
   int st = check_matrices(B, M, N, dtype);
   if (st != MOE_OK) return st;
   Steps s;
-  if (steps < 1 || steps > kMaxSteps || !(eps > 0.f) || isinf(eps) || !make_steps(s, steps, coefs, std::min(M, N), std::max(M, N)))
+  if (steps < 1 || steps > kMaxSteps || !(eps > 0.f) || isinf(eps) || !make_steps(s, steps, coefs, std::min(M, N), std::max(M, N), dtype == MOE_F32))
     return MOE_ERR_INVALID_ARG;
   if (!isfinite(mu) || !isfinite(lr) || !isfinite(weight_decay) || !isfinite(scale) || (nesterov != 0 && nesterov != 1))
     return MOE_ERR_INVALID_ARG;
