@@ -22,8 +22,8 @@ __device__ __forceinline__ f32x16 mfma_16bit<true>(const bf16x8& a, const bf16x8
 
 constexpr int tile_stage(int side) { return 2 * side * 128; }    // bytes
 
-// SIDE 256: by four waves of 128 x 128; 128: by four of 64 x 64; 64: by two of 32 x 64.  P, Q: the matrices from the first step's columns on, row_bytes (below 2^32 / rows)
-// from row to row.
+// SIDE 256: by four waves of 128 x 128; 128: by four of 64 x 64; 64: by two of 32 x 64.  P, Q: the matrices from the first step's columns on,
+// row_bytes (below 2^32 / rows) from row to row.
 template <int SIDE, bool PAIRS, int STAGES>
 __device__ __forceinline__ void tile_multiply(const char* Pv, const char* Qv, int row_bytes, int rows, int cols, int i0, int j0, int n_steps, char* smem,
                                               f32x16 (&acc)[SIDE / 64][SIDE == 256 ? 4 : 2]) {

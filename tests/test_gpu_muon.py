@@ -206,6 +206,37 @@ def test_step_of_many_is_each_ones(M, N, master):
             assert torch.equal(t[0], big[e]) and torch.equal(big[e].to(torch.bfloat16), out[e]), e
 
 
+@pytest.mark.parametrize("n,M,N", [(270, 130, 200), (270, 260, 203), (270, 70, 300), (270, 3, 90), (100, 300, 500)])
+def test_fp32_of_many_is_each_ones(n, M, N):
+    """fp32 matrices as many as make whole tiles, whose reductions are two to sixteen steps long, and what is left over of them in quarters: the
+    oracle's, and in whole tiles the bits of each alone; weights in place, and fp32 ones beside a copy."""
+    u = _dev(_u(n, M, N, M + n), "f32")
+    out, ws, ws1 = torch.full_like(u, float("nan")), _ws(n, M, N, "f32"), _ws(1, M, N, "f32")
+    moe.moe_orthogonalize(u, out, ws)
+    w = torch.randn(n, M, N, generator=torch.Generator("cuda").manual_seed(M), device="cuda")
+    m, m_out, same, top, copy = torch.ones_like(u), torch.empty_like(u), w.clone(), w.clone(), torch.full_like(u, float("nan"))
+    kw = dict(lr=0.3, mu=0.9, weight_decay=0.1)
+    moe.moe_muon_step(u, m, same, m_out, same, ws, **kw)
+    moe.moe_muon_step(u, m, None, m_out, copy, ws, master=top, **kw)
+    assert torch.equal(same, top) and torch.equal(same, copy)
+    one, m1 = torch.empty(1, M, N, device="cuda"), torch.empty(1, M, N, device="cuda")
+    # The last 14 of 270 are what is left over of a round of 256, and sums of eight steps are dealt out in two shares: added up in another
+    # order, so within the bound of each (its term of K / 8 + 8 roundings), not the same bits.
+    for e in (0, 1, n // 2, n - 2, n - 1):
+        moe.moe_orthogonalize(u[e:e + 1].clone(), one, ws1)
+        _, err = _bound(u[e], "f32")
+        assert torch.equal(one[0], out[e]) or (e >= 256 and torch.linalg.vector_norm(one[0] - out[e]) <= 2 * err), e
+        moe.moe_muon_step(u[e:e + 1].clone(), m[:1].clone(), w[e:e + 1].clone(), m1, one, ws1, **kw)
+        assert torch.equal(m1[0], m_out[e]), e
+        _, err = _bound(f64(u)[e] + f64(torch.tensor(0.9)) * f64(m_out)[e], "f32")
+        assert torch.equal(one[0], same[e]) or (e >= 256 and torch.linalg.vector_norm(one[0] - same[e]) <= 0.3 * 2 * err + 4 * U * float(torch.linalg.vector_norm(same[e]))), e
+    for e in (0, n - 1):
+        want, err = _bound(u[e], "f32")
+        want = want if M <= N else want.T
+        off = np.linalg.norm(f64(out)[e] - want)
+        assert off <= err + HALF["f32"] * (np.linalg.norm(want) + err), (e, off, err)
+
+
 def test_more_matrices_than_a_group():
     """Beyond the matrices that are worked on at a time, each is what it is alone."""
     n, M, N = 16500, 6, 20
