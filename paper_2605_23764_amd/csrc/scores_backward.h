@@ -71,11 +71,13 @@ template <int L, bool TAIL, bool FULL> __global__ __launch_bounds__(kRouterThrea
       }
       sum = token_sum<L>(sum);
     }
-    // the slots: selected scores (softmax: without the division by the row's sum, which is the same for all)
+    // the slots: selected scores (softmax: without the division by the row's sum, which is the same for all).  Where they are renormalised they
+    // come times 2^500, which the division takes off again: far below zero their sum is subnormal, and its reciprocal would overflow.
+    const double up = p.renorm ? 0x1p500 : 1.0;
     double ps[kSlots], total = 0.0, dot = 0.0;
 #pragma unroll
     for (int j = 0; j < kSlots; ++j) {
-      ps[j] = id[j] < 0 ? 0.0 : p.sigmoid ? sigmoid64(lv[j]) : exp_below(lv[j], m);
+      ps[j] = id[j] < 0 ? 0.0 : up * (p.sigmoid ? sigmoid64(lv[j]) : exp_below(lv[j], m));
       total += ps[j];
       dot += ps[j] * (double)dw[j];
     }
