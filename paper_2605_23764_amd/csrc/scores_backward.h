@@ -55,6 +55,7 @@ template <int L, bool TAIL, bool FULL> __global__ __launch_bounds__(kRouterThrea
       id[j] = in ? id[j] : -1;
       lv[j] = in ? q[id[j]] : none;
       if (lv[j] != lv[j]) lv[j] = none;
+      if (lv[j] == none) dw[j] = 0.f;      // no part, whatever it holds: not even 0 * NaN
     }
     float m = none, sum = 0.f;
     if (FULL) {

@@ -1,10 +1,11 @@
-"""The gradient of the routing by scores at its edges: selected scores whose sum is subnormal in 64 bits."""
+"""The gradient of the routing by scores at its edges: selected scores whose sum is subnormal in 64 bits, gradients of slots that have no part."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2605_23764_amd as moe
 from block_common import U, f64
+from oracle import router_oracle as ro
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +57,28 @@ def test_sums_that_are_subnormal(kind, E, k):
     moe.moe_route_scores(shape, moe.make_scores(kind, renormalize=True, scale=1.5), torch.from_numpy(L[:1]).cuda(), torch.from_numpy(bias).cuda(), saved, ws)
     np.testing.assert_array_equal(saved.topk_idx.cpu().numpy()[0], idx[0])
     assert (np.abs(f64(saved.topk_w)[0] - 1.5 * w[0]) <= 1.5 * w[0] * (r_w[0] * 1.01 + U)).all()
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("renorm", [True, False], ids=["renorm", "plain"])
+@pytest.mark.parametrize("T,E,k", [(70, 24, 4), (33, 256, 8), (5, 3, 2)])
+def test_slots_without_a_part_may_hold_anything(T, E, k, kind, renorm):
+    """Ids outside 0 .. E - 1, and experts whose logit is -inf: whatever their gradient holds, the others' are those of the slots that count."""
+    r = np.random.default_rng(T)
+    L = r.normal(size=(T, E)).astype(np.float32)
+    idx, _ = ro.select(L, kind, k)
+    dw = r.normal(size=(T, k)).astype(np.float32)
+    clean = dw.copy()
+    bad = [float("nan"), float("inf"), -float("inf"), 3e38]
+    for i, t in enumerate(range(0, T, 2)):
+        j = i % k
+        if i % 3 == 2:
+            L[t, idx[t, j]] = -np.inf if i % 2 else np.nan
+        else:
+            idx[t, j] = (-1, E, -7, 2 ** 31 - 1)[i % 4]
+        dw[t, j], clean[t, j] = bad[i % 4], 0.0
+    scores = moe.make_scores(kind, renormalize=renorm, scale=1.25)
+    got = _gradient(scores, L, idx, dw)
+    np.testing.assert_array_equal(got, _gradient(scores, L, idx, clean))
+    want = ro.weights_backward(L.astype(np.float64), kind, idx, clean.astype(np.float64), renorm, 1.25)
+    assert np.abs(got - want).max() <= 40 * U * np.abs(clean).max() * 1.25
