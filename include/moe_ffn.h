@@ -440,7 +440,7 @@ int moe_route_scores(const MoeShape* shape, const MoeScores* scores, const float
 /*
  * The gradient of its logits: d topk_w / d logits (the selection and the bias carry none) applied to dtopk_w, plus dadd.
  *   d_topk_idx [T,k] as selected (ids outside 0 .. E-1 and experts whose logit is -inf or NaN have no part, whatever their d_dtopk_w
- *              holds);  d_dtopk_w [T,k] f32
+ *              holds; the parts of an expert that a token names twice add up);  d_dtopk_w [T,k] f32
  *   d_dadd     [T,E] f32, NULL: 0.  moe_router_backward's without topk_w, for a balance loss; may be d_dlogits
  *   d_dlogits  [T,E] f32, overwritten (may be d_logits)
  */

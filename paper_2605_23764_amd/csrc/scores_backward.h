@@ -98,7 +98,7 @@ template <int L, bool TAIL, bool FULL> __global__ __launch_bounds__(kRouterThrea
       if (id[j] >= 0) {
         double v = (double)p.scale * ps[j] * norm * ((double)dw[j] - (p.renorm ? dot : 0.0));
         if (p.sigmoid) v *= sigmoid64(-lv[j]);
-        row[id[j]] = (float)v;
+        __hip_atomic_fetch_add(row + id[j], (float)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);   // an expert may be there twice
       }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const float off = FULL && !p.renorm ? (float)((double)p.scale * norm * dot) : 0.f;

@@ -1,4 +1,5 @@
-"""The gradient of the routing by scores at its edges: selected scores whose sum is subnormal in 64 bits, gradients of slots that have no part."""
+"""The gradient of the routing by scores at its edges: selected scores whose sum is subnormal in 64 bits, gradients of slots that have no part, an
+expert that two slots of a token name."""
 import numpy as np
 import pytest
 import torch
@@ -82,3 +83,22 @@ def test_slots_without_a_part_may_hold_anything(T, E, k, kind, renorm):
     np.testing.assert_array_equal(got, _gradient(scores, L, idx, clean))
     want = ro.weights_backward(L.astype(np.float64), kind, idx, clean.astype(np.float64), renorm, 1.25)
     assert np.abs(got - want).max() <= 40 * U * np.abs(clean).max() * 1.25
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("renorm", [True, False], ids=["renorm", "plain"])
+@pytest.mark.parametrize("E,k", [(3, 3), (8, 8), (24, 5), (64, 6), (256, 16)])
+def test_an_expert_named_twice(E, k, kind, renorm):
+    """Its slots' parts add up."""
+    T = 50
+    r = np.random.default_rng(E)
+    L = r.normal(size=(T, E)).astype(np.float32)
+    idx = r.integers(0, E, size=(T, k))
+    idx[:, 1] = idx[:, 0]
+    idx[::3] = idx[::3, :1]                                         # all the same
+    dw, dadd = (r.normal(size=s).astype(np.float32) for s in ((T, k), (T, E)))
+    scores = moe.make_scores(kind, renormalize=renorm, scale=1.25)
+    want = ro.weights_backward(L.astype(np.float64), kind, idx, dw.astype(np.float64), renorm, 1.25)
+    tol = 40 * U * np.abs(dw).max() * 1.25
+    assert np.abs(_gradient(scores, L, idx, dw) - want).max() <= tol * (1 + k)         # k parts, each rounded, and their sums
+    assert np.abs(_gradient(scores, L, idx, dw, dadd) - (want + dadd)).max() <= tol * (1 + k) + U * np.abs(dadd).max() * 2
