@@ -461,7 +461,7 @@ int moe_bias_update(int32_t E, const int32_t* d_counts, float rate, const float*
  * bf16, ahead of its rounding.  An infinity in x, W or dlogits gives NaN in the sums that it takes part in.
  * 1 <= H <= 262144, 1 <= E <= 256, T / 128 * max(H, E) / 64 (both rounded up) below 2^24.
  *   d_x [T,H] dtype;  d_w [H,E] f32;  d_logits, d_dlogits [T,E] f32
- *   d_workspace  >= moe_router_project_workspace_bytes(T, H, E)
+ *   d_workspace  >= moe_router_project_workspace_bytes(T, H, E), which does not fall as T grows: one of the largest T serves all
  */
 int moe_router_project_workspace_bytes(int32_t T, int32_t H, int32_t E, size_t* bytes);
 int moe_router_project(int32_t T, int32_t H, int32_t E, int dtype, const void* d_x, const float* d_w, float* d_logits,

@@ -42,19 +42,37 @@ int tile_cols(int rows, int cols, int dtype) {
 // workgroup takes about as long as the whole chip takes to write 2^20 partial sums and read them again, so s splits cost steps / s + s rows cols / 2^20,
 // least at the root of the quotient (128 x 7168 x 256, bf16: with two to a CU, 112 splits, 17.6 us, with 58 14.4; its dW 16.2 and 8.6).  What is left
 // of two to a CU by that, but leaves most CUs one, is one each (4096 x 2048 x 64: dW in 352 workgroups 21.5 us, in 256 15.9).
-struct Split { int k, n; };
-Split split_of(int rows, int cols, int K, int dtype) {
+int splits_wanted(int rows, int cols, int K, int dtype) {
   const int tiles = (int)std::min<long>((long)ceil_div(rows, kProjTile) * ceil_div(cols, tile_cols(rows, cols, dtype)), 1 << 20);
   const double most = sqrt((double)ceil_div(K, kProjK) * (1 << 20) / ((double)rows * cols));
   int want = std::min({kProjMaxSplits, 2 * kProjCUs / tiles, (int)std::min(most + 0.5, 1e6)});
   if (want * tiles < kProjCUs * 3 / 2) want = std::min(want, kProjCUs / tiles);
-  want = std::max(want, 1);
+  return std::max(want, 1);
+}
+struct Split { int k, n; };
+Split split_of(int rows, int cols, int K, int dtype) {
   Split s;
-  s.k = ceil_div(ceil_div(K, want), kProjK) * kProjK;
+  s.k = ceil_div(ceil_div(K, splits_wanted(rows, cols, K, dtype)), kProjK) * kProjK;
   s.n = ceil_div(K, s.k);
   return s;
 }
-size_t part_bytes(const Split& s, int rows, int cols) { return s.n > 1 ? (size_t)s.n * rows * cols * 4 : 0; }
+
+// Bytes of the partial sums of a call with T tokens and of every one with fewer: a program allocates for its largest call, and fewer tokens may
+// have more sums (8192 x 7168 x 256 33.5 MB, of 32768 tokens 29.4).  s splits, by split_of:
+//   logits  s T E values.  s is at most kProjMaxSplits, the steps of H, and the root above, rounded; times T E each of them grows with T.  It is at most
+//           2 kProjCUs / tiles, too, and T / tiles at most kProjTile / (tiles of 128 columns): the same for every T
+//   dW      s H E values.  splits_wanted and the steps of T, which s does not exceed, grow with T
+size_t logits_part_bound(int T, int H, int E) {
+  const double n = (double)T * E, steps = ceil_div(H, kProjK);
+  const double tile_bound = 2.0 * kProjCUs * kProjTile / ceil_div(E, kProjTile) * E;
+  const double most = sqrt(steps * (1 << 20) * n) + 0.5 * n;
+  const double values = std::min({kProjMaxSplits * n, steps * n, most, tile_bound});
+  return (size_t)ceil(values) * 4;
+}
+size_t dw_part_bound(int T, int H, int E, int dtype) {
+  const int n = std::min(splits_wanted(H, E, T, dtype), ceil_div(T, kProjK));
+  return n > 1 ? (size_t)n * H * E * 4 : 0;
+}
 
 int join(const float* part, int splits, size_t n, float* out, hipStream_t s) {
   if (splits > 0 && splits <= 8 && n % 4 == 0)
@@ -93,8 +111,7 @@ int moe_router_project_workspace_bytes(int32_t T, int32_t H, int32_t E, size_t* 
   const int st = check(T, H, E, MOE_F32);
   if (st != MOE_OK) return st;
   if (!bytes) return MOE_ERR_INVALID_ARG;
-  *bytes = T == 0 ? 16 : std::max({(size_t)16, part_bytes(split_of(T, E, H, MOE_F32), T, E), part_bytes(split_of(H, E, T, MOE_F32), H, E),
-                                part_bytes(split_of(T, E, H, MOE_BF16), T, E), part_bytes(split_of(H, E, T, MOE_BF16), H, E)});
+  *bytes = T == 0 ? 16 : std::max({(size_t)16, logits_part_bound(T, H, E), dw_part_bound(T, H, E, MOE_F32), dw_part_bound(T, H, E, MOE_BF16)});
   return MOE_OK;
 }
 
