@@ -490,7 +490,7 @@ int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, cons
  *   steps    1 .. 16;  eps > 0, finite
  *   coefs    host, [steps][3] a, b, c, read before the call returns; NULL: 3.4445, -4.7750, 2.0315 in each.  MOE_ERR_INVALID_ARG
  *            where they let singular values grow beyond 32 (from at most 1), or |a + b s^2 + c s^4| beyond 1024 on the way
- *   d_workspace  >= moe_muon_workspace_bytes(B, M, N, dtype)
+ *   d_workspace  >= moe_muon_workspace_bytes(B, M, N, dtype), which does not fall as B grows: one of the largest B serves all
  * Limits: 1 <= M, N <= 262144; the shorter side at most 32768; M x N (sides rounded up to 64) below 2^31 in bf16, 2^30 in fp32.
  * B == 0 is a no-op.
  */

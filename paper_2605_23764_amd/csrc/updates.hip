@@ -55,9 +55,11 @@ Plan make_plan(int B, int M, int N, int dtype) {
   p.group = std::max(1, (B + groups - 1) / groups);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
-  p.x = take(4 * p.x_bytes * p.group);
-  p.a = take(2 * p.a_bytes * p.group);
-  p.part = take((size_t)kNsMaxParts * 8 * p.group);
+  // of as many matrices as a group can have: groups of more matrices may be smaller, and a program allocates for its largest call
+  const size_t room = std::max(1, std::min(B, most));
+  p.x = take(4 * p.x_bytes * room);
+  p.a = take(2 * p.a_bytes * room);
+  p.part = take((size_t)kNsMaxParts * 8 * room);
   p.share = take((size_t)kNsMaxShares * 128 * 128 * 4);
   p.total = off;
   return p;

@@ -31,3 +31,20 @@ def test_router_project(largest, H, E, smaller, dtype):
             results.append((logits, dx, dw))
         assert all(torch.equal(a, b) for a, b in zip(*results))
         assert (behind == 0xA5).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_muon(dtype):
+    """16400 matrices go in groups of 8200, 16384 in one."""
+    M, N = 8, 40
+    u = torch.randn(16400, M, N, generator=torch.Generator("cuda").manual_seed(0), device="cuda").to(dtype)
+    ws, behind = _guarded(moe.moe_muon_workspace_bytes(16400, M, N, dtype))
+    for B in (16400, 16384, 8201, 3):
+        print(f"orthogonalize {B} of 16400 x {M} x {N} {dtype}", flush=True)
+        results = []
+        for space in (moe.alloc_muon_workspace(B, M, N, dtype), ws):
+            out = torch.empty_like(u[:B])
+            moe.moe_orthogonalize(u[:B], out, space)
+            results.append(out)
+        assert torch.equal(*results) and torch.isfinite(results[0]).all()
+        assert (behind == 0xA5).all()

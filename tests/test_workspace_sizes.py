@@ -1,5 +1,6 @@
 """Workspaces of the largest call serve every smaller one: their sizes never fall, at the borders of splits and groups neither (CPU only)."""
 import pytest
+import torch
 
 import paper_2605_23764_amd as moe
 
@@ -20,3 +21,13 @@ def test_router_project(H, E):
     assert sizes == sorted(sizes)
     # two workgroups to each of 256 CUs, of 128 x 128 sums at most, or as many splits of dW
     assert sizes[-1] <= 2 * 256 * 128 * 128 * 4 + 256 * H * E * 4
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("M,N", [(1, 1), (64, 64), (200, 330), (704, 1088), (2816, 2048), (7168, 4096), (4096, 7168), (16384, 32768), (30000, 30000)])
+def test_muon(M, N, dtype):
+    counts = sorted({*range(0, 400), *_around([1 << i for i in range(9, 18)], 1 << 20)})
+    sizes = [moe.moe_muon_workspace_bytes(B, M, N, dtype) for B in counts]
+    assert sizes == sorted(sizes)
+    assert sizes[-1] <= max(sizes[1], 5 << 30)                       # that of a group, or of a matrix that is larger
+    assert sizes == [moe.moe_muon_workspace_bytes(B, N, M, dtype) for B in counts]
