@@ -50,7 +50,8 @@ typedef enum MoeStatus {
   MOE_ERR_WORKSPACE_TOO_SMALL = -3,
   MOE_ERR_LAUNCH = -4,            /* a HIP launch or API call failed */
   MOE_ERR_SCHED_TIMEOUT = -5,     /* persistent scheduler: a bounded wait expired */
-  MOE_ERR_XCD_PLACEMENT = -6      /* microbenchmark modes 1 and 3: workgroups of one class (id % 8) span several XCDs */
+  MOE_ERR_XCD_PLACEMENT = -6,     /* microbenchmark modes 1 and 3: workgroups of one class (id % 8) span several XCDs */
+  MOE_ERR_NOT_PREPARED = -7       /* status word: MOE_MODE_PERSISTENT behind a routing for MOE_MODE_SERIALIZED; nothing was computed */
 } MoeStatus;
 
 typedef enum MoeDtype { MOE_F32 = 0, MOE_BF16 = 1 } MoeDtype;
@@ -202,8 +203,8 @@ int moe_ffn_backward_two_streams(const MoeShape* shape, const void* d_dy, const 
 
 /*
  * Reads the scheduler status word of a forward or backward workspace after the caller has
- * synchronised the stream (host-blocking 4-byte copy).  MOE_OK or
- * MOE_ERR_SCHED_TIMEOUT.
+ * synchronised the stream (host-blocking 4-byte copy).  MOE_OK,
+ * MOE_ERR_SCHED_TIMEOUT, or MOE_ERR_NOT_PREPARED (moe_dispatch_to_combine).
  */
 int moe_ffn_last_status(const MoeShape* shape, const void* d_workspace);
 
@@ -297,14 +298,16 @@ int moe_ffn_forward_scatter(const MoeShape* shape, const void* d_x, const float*
                             const void* d_w_down, void* d_out, const MoeSaved* saved, void* d_workspace,
                             size_t workspace_bytes, int mode, void* stream);
 
-/* Dispatch to Combine, the interval the paper times (Section 5.2), on the routing results moe_route left in the
+/* Dispatch to Combine, the interval the paper times (Section 5.2), on the routing results moe_route or moe_route_scores left in the
  * SAME `saved` and workspace: Dispatch permute, GEMM-1 + SwiGLU, GEMM-2, Combine.  mode MOE_MODE_SERIALIZED: one
  * launch per operator (Section 2.3's kernel-by-kernel execution); MOE_MODE_PERSISTENT: exactly one launch of
  * tile tasks with event counters (Sections 4.3-4.4; alignment rule at the top of this file; up to 64 tokens in
- * bf16 of weight streams), which consumes the counters and queues moe_route prepared: one call per moe_route call (a second one finds every ticket
+ * bf16 of weight streams), which consumes the counters and queues that routing prepared: one call per routing call (a second one finds every ticket
  * taken and does nothing).  Results are bit-identical.  moe_ffn_forward(mode) = moe_route + this, except that
  * its routing launches leave the counters and queues out when mode is MOE_MODE_SERIALIZED (nobody reads them
- * then): MOE_MODE_PERSISTENT here needs a moe_route call, or a MOE_MODE_PERSISTENT forward's routing, in front. */
+ * then), as moe_route_scores does for that mode: MOE_MODE_PERSISTENT here needs a moe_route call, a moe_route_scores call with
+ * MOE_MODE_PERSISTENT, or a MOE_MODE_PERSISTENT forward's routing, in front.  Behind a routing without them it computes nothing, leaves
+ * out as it was, and moe_ffn_last_status reports MOE_ERR_NOT_PREPARED. */
 int moe_dispatch_to_combine(const MoeShape* shape, const void* d_x, const void* d_w_gate_up, const void* d_w_down,
                             void* d_out, const MoeSaved* saved, void* d_workspace, size_t workspace_bytes, int mode,
                             void* stream);
@@ -432,7 +435,8 @@ typedef struct MoeScores {
  *   saved, d_workspace   filled as by moe_route: moe_dispatch_to_combine, moe_dispatch_to_combine_w4 or the stage entry points
  *                        follow, then moe_ffn_backward, and moe_route_scores_backward on its d_dtopk_w
  *   mode     MoeMode of the moe_dispatch_to_combine that follows.  MOE_MODE_SERIALIZED leaves the tile scheduler's counters and task
- *            tables out (nobody reads them then), as moe_ffn_forward's routing does: a MOE_MODE_PERSISTENT call may not follow
+ *            tables out (nobody reads them then), as moe_ffn_forward's routing does: a MOE_MODE_PERSISTENT call behind it computes
+ *            nothing and reports MOE_ERR_NOT_PREPARED
  */
 int moe_route_scores(const MoeShape* shape, const MoeScores* scores, const float* d_logits, const float* d_bias,
                      const MoeSaved* saved, void* d_workspace, size_t workspace_bytes, int mode, void* stream);

@@ -363,6 +363,7 @@ SchedParams<BF16> sched_params(const Ctx& c, const void* x, const float* logits,
   sp.force_device_scope = g_force_device_scope;
   sp.spin_limit = g_spin_limit;
   sp.timeout_status = MOE_ERR_SCHED_TIMEOUT;
+  sp.not_prepared_status = MOE_ERR_NOT_PREPARED;
   return sp;
 }
 
@@ -439,6 +440,8 @@ int run_stream_layer(const Ctx& c, const void* x, const void* w_gate_up, const v
   p.copy = c.keep_xp ? 1 : 0;
   p.spin_limit = g_spin_limit;
   p.timeout_status = MOE_ERR_SCHED_TIMEOUT;
+  p.not_prepared_status = MOE_ERR_NOT_PREPARED;
+  static_assert(kEvNotPrepared == kEvStreamStarted && kNotPrepared == (uint32_t)kStreamNotPrepared, "what a routing without tables leaves");
   hipLaunchKernelGGL(stream_layer_kernel, dim3(gemm_grid(c)), dim3(kGemmThreads), 0, c.stream, p);
   return launch_status();
 }
@@ -803,6 +806,7 @@ const char* moe_status_string(int status) {
     case MOE_ERR_WORKSPACE_TOO_SMALL: return "workspace too small";
     case MOE_ERR_LAUNCH: return "HIP launch failed";
     case MOE_ERR_SCHED_TIMEOUT: return "persistent scheduler wait timed out";
+    case MOE_ERR_NOT_PREPARED: return "single launch behind a routing without its counters and task tables";
     case MOE_ERR_XCD_PLACEMENT: return "workgroups of one class (id % 8) span several XCDs";
     default: return "unknown status";
   }

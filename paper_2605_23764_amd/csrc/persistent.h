@@ -89,6 +89,8 @@ enum EventId { kEvArrive = 0, kEvGemm2 = 3, kEvPerTile = 4 };
 //   kEvPerTile + m               rows of M tile m are in Xp      (PERMUTE parts of m)
 //   kEvPerTile + max_mtiles + m  A rows of M tile m are complete (GEMM-1 tiles of m)
 constexpr int kNoEvent = -1;             // dep_event of a task that waits for nothing
+constexpr int kEvNotPrepared = kEvPerTile + 16;   // the launch as streams: its workgroups started, eight words (kEvStreamStarted)
+constexpr uint32_t kNotPrepared = 1u << 30;       // more than any launch has
 
 enum QueueId { kQXcd0 = 0, kQCombine = kNumXcd, kNumQueues = 16 };
 
@@ -125,7 +127,7 @@ struct SchedParams {
   uint4* zero_dst;         // routing launch, optional: zero_n16 16-byte vectors that further workgroups of the launch
   size_t zero_n16;         // set to zero (the layer output ahead of a GEMM-2 that adds its rows into it)
   uint32_t spin_limit;     // polls before a wait gives up (MOE_ERR_SCHED_TIMEOUT)
-  int32_t timeout_status;
+  int32_t timeout_status, not_prepared_status;
 };
 
 // Optional per-task time stamps (100 MHz wall clock) for a tile-level timeline;
@@ -265,6 +267,19 @@ __device__ __forceinline__ void sched_trigger(const SchedParams<BF16>& sp, int e
   }
   __syncthreads();
   if (wave == 0) wave_atomic_add(&sp.events[ev], inc);
+}
+
+// A routing without counters and task tables: a single launch behind it finds no task, or every share drawn, and says so in the status word
+// instead of running an earlier routing's tasks or whatever the workspace held.  It loads no more for that than it does anyway.  By the workgroup's
+// last wave, ahead of the routing, which waits for others.
+template <bool BF16>
+__device__ __forceinline__ void leave_out_tables(const SchedParams<BF16>& sp) {
+  const int i = (int)threadIdx.x - ((int)blockDim.x - kWave);
+  if (i >= 0 && i < kNumXcd) {
+    sp.meta[kMetaQueueCount0 + i] = -1;
+    sp.events[kEvNotPrepared + i] = kNotPrepared;
+  }
+  if (i == kNumXcd) sp.meta[kMetaGemm2Total] = -1;
 }
 
 constexpr int kTableRows = 1024;
@@ -407,6 +422,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void sched_prepare_kernel(Sched
   __shared__ int32_t s_lds[kScanLds];
   static_assert(kRankThreads == kScanWaves * kWave, "workgroup 0 scans with all its waves");
   if (blockIdx.x == 0) {
+    if (sp.skip_tables) leave_out_tables(sp);
     scan_all(sp.route, s_lds, s_lds + kMaxE + 64);
     __threadfence_block();
     __syncthreads();   // tile map (written by wave 0) complete before every wave reads it
@@ -429,6 +445,7 @@ template <bool BF16>
 __global__ __launch_bounds__(kRankThreads) void sched_prepare_copy_kernel(SchedParams<BF16> sp, int tokens) {
   __shared__ int32_t s_lds[kScanLds];
   if (blockIdx.x == 0) {
+    leave_out_tables(sp);
     scan_all(sp.route, s_lds, s_lds + kMaxE + 64);
     return;
   }
@@ -446,6 +463,7 @@ __device__ __forceinline__ void route_one_launch(const SchedParams<BF16>& sp, co
       sp.zero_dst[i] = make_uint4(0, 0, 0, 0);
     return;
   }
+  if (sp.skip_tables) leave_out_tables(sp);
   route_one(sp.route, select);
   if (sp.skip_tables) return;
   __threadfence_block();
@@ -531,7 +549,7 @@ void persistent_forward_kernel(SchedParams<BF16> sp) {
     for (int qq = q; qq >= 0;) {
       const int count = __builtin_amdgcn_readfirstlane(sp.meta[kMetaQueueCount0 + qq]);
       const int t = sched_fetch(sp.qhead, kQXcd0 + qq, s_box, wave);
-      if (t >= count) {
+      if ((uint32_t)t >= (uint32_t)max(count, 0)) {   // below 0: not prepared, the ticket may be anything
         qq = far ? sched_fullest_queue(sp, s_box, wave) : -1;
         continue;
       }
@@ -553,6 +571,10 @@ void persistent_forward_kernel(SchedParams<BF16> sp) {
   bool yp_ready = false;   // every GEMM-2 tile seen and acquired: once per worker (Yp never changes afterwards)
   for (;;) {
     const int t = sched_fetch(sp.qhead, kQCombine, s_box, wave);
+    if ((int)g2_total < 0) {               // not prepared (leave_out_tables), the ticket may be anything
+      if (wave == 0) __hip_atomic_store(&sp.meta[kMetaStatus], sp.not_prepared_status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      return;
+    }
     if (t >= sp.n_comb_tasks) break;
     MOE_TRACE_FETCH(3, t, 0)
     if (!yp_ready && !sched_wait(sp, kEvGemm2, g2_total, s_box, wave)) continue;

@@ -23,8 +23,9 @@
 namespace moe {
 
 // Counters, zero at the start: where the tile tasks have their events; eight words each, on lines of their own.
-constexpr int kEvStreamDraw = kEvPerTile, kEvStreamDone1 = kEvPerTile + 32, kEvStreamDone2 = kEvPerTile + 64;
+constexpr int kEvStreamDraw = kEvPerTile, kEvStreamStarted = kEvStreamDraw + 16, kEvStreamDone1 = kEvPerTile + 32, kEvStreamDone2 = kEvPerTile + 64;
 constexpr int kStreamLayerEvents = kEvStreamDone2 + kNumXcd;
+constexpr int kStreamNotPrepared = 1 << 30;   // workgroups started, in a launch whose routing left the counters out (leave_out_tables)
 static_assert(kStreamLayerEvents <= kEvPerTile + 2 * (2 + kMapSlack), "the events of the smallest layer");
 
 struct StreamLayerParams {
@@ -35,7 +36,7 @@ struct StreamLayerParams {
   int32_t* meta;
   int copy;
   uint32_t spin_limit;
-  int32_t timeout_status;
+  int32_t timeout_status, not_prepared_status;
 };
 
 __global__ __launch_bounds__(kGemmThreads) __attribute__((amdgpu_waves_per_eu(1, 1)))
@@ -57,7 +58,12 @@ void stream_layer_kernel(StreamLayerParams sp) {
     s_box[2] = __builtin_amdgcn_readlane((int)mine, 2);
   }
   __syncthreads();
-  if (__builtin_amdgcn_readfirstlane(s_box[2]) >= W) return;       // a second launch on the same routing: nothing is left to do
+  const int started = __builtin_amdgcn_readfirstlane(s_box[2]);
+  if (started >= W) {                      // a second launch on the same routing: nothing is left to do; or one whose routing was for none
+    if (started >= kStreamNotPrepared && wave == 0)
+      __hip_atomic_store(&sp.meta[kMetaStatus], sp.not_prepared_status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return;
+  }
   const int first1 = __builtin_amdgcn_readfirstlane(s_box[0]), first2 = __builtin_amdgcn_readfirstlane(s_box[1]);
   // Every wave has read the box before wave 0 writes it again: with a drawn share of GEMM-1 that is somebody else's by now (>= W, as for
   // a workgroup that starts late) there is no work, and with it no barrier, in front of that.  Every later read has one behind it.
