@@ -100,14 +100,18 @@ class MoeBlock:
         self.forward(x, mask)
         return self.backward(dout, dz)
 
-    def update(self, lr=0.02, mu=0.95, weight_decay=0.0):
-        """After step(): the experts' weights by momentum and orthogonal updates, each expert's matrices by themselves; with scores the bias too."""
+    def update(self, lr=0.02, mu=0.95, weight_decay=0.0, scale=1.0):
+        """After step(): the experts' weights by momentum and orthogonal updates, w_gate_up [H, 2I] and w_down [I, H] of each expert by
+        themselves; with scores the bias too.  scale: of the orthogonal matrices, or "fan": max(1, fan_out / fan_in)^0.5 of each (weights are
+        [in, out])."""
         pairs = ((self.w_gate_up, self.dw_gate_up), (self.w_down, self.dw_down))
         if self.momentum is None:
             self.momentum = [torch.zeros(w.shape, device=w.device) for w, _ in pairs]
             self.ws_update = [moe.alloc_muon_workspace(*w.shape, w.dtype, w.device) for w, _ in pairs]
         for (w, dw), m, ws in zip(pairs, self.momentum, self.ws_update):
-            moe.moe_muon_step(dw, m, w, m, w, ws, lr=lr, mu=mu, weight_decay=weight_decay, scale=max(1.0, w.shape[1] / w.shape[2]) ** 0.5)
+            fan_in, fan_out = w.shape[1:]
+            s = max(1.0, fan_out / fan_in) ** 0.5 if scale == "fan" else scale
+            moe.moe_muon_step(dw, m, w, m, w, ws, lr=lr, mu=mu, weight_decay=weight_decay, scale=s)
         if self.scores is not None:
             moe.moe_bias_update(self.counts, self.rate, self.bias, self.bias)
 
@@ -163,7 +167,7 @@ def main():
     timed(f"training step, {a.tokens} tokens", lambda: block.step(x, dout, dz))
     print(f"balance loss {block.loss.item():.5f} ({block.coef} if even), busiest expert {block.counts[:-1].max().item()} of "
           f"{a.tokens * a.top_k // a.experts} selections on average")
-    timed("update of the experts", block.update)
+    timed("update of the experts", lambda: block.update(scale="fan"))
     block.quantize()
     for n in (1, 32):
         timed(f"decode step, {n} tokens, 4-bit experts", lambda: block.decode(x[:n]))
