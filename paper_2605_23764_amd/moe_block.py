@@ -5,7 +5,7 @@
 with the balance loss of the router.  Everything but the router's small projection (a library product) runs in the HIP library; the caller
 owns every buffer, as everywhere here.  With scores (make_scores) the router is another: its projection runs in the library too, experts
 are selected by sigmoid or softmax scores and a bias that moves towards balance.  update() is the optimiser's step of the experts: momentum
-and orthogonal updates.
+and orthogonal updates, of gate and up apart or as one matrix.
 
     python -m paper_2605_23764_amd.moe_block [--tokens 4096 --hidden 2048 --width 1408 --experts 16 --top-k 4 --dropout 0.1]
                                              [--scores sigmoid --groups 4 --top-groups 2]
@@ -100,18 +100,33 @@ class MoeBlock:
         self.forward(x, mask)
         return self.backward(dout, dz)
 
-    def update(self, lr=0.02, mu=0.95, weight_decay=0.0, scale=1.0):
-        """After step(): the experts' weights by momentum and orthogonal updates, w_gate_up [H, 2I] and w_down [I, H] of each expert by
-        themselves; with scores the bias too.  scale: of the orthogonal matrices, or "fan": max(1, fan_out / fan_in)^0.5 of each (weights are
-        [in, out])."""
-        pairs = ((self.w_gate_up, self.dw_gate_up), (self.w_down, self.dw_down))
+    def update(self, lr=0.02, mu=0.95, weight_decay=0.0, scale=1.0, apart=False):
+        """After step(): the experts' weights by momentum and orthogonal updates; with scores the bias too.
+
+        apart: each expert's gate and up matrices [H, I] by themselves, else [H, 2I] as one matrix, as they are stored; w_down [I, H] by itself.
+        scale: of the orthogonal matrices, or "fan": max(1, fan_out / fan_in)^0.5 of each (weights are [in, out]).  Momentum belongs to the form
+        of the first call."""
+        E, H, I = self.E, self.H, self.shape.I
+        halves = (2 * E, H, I)
         if self.momentum is None:
-            self.momentum = [torch.zeros(w.shape, device=w.device) for w, _ in pairs]
-            self.ws_update = [moe.alloc_muon_workspace(*w.shape, w.dtype, w.device) for w, _ in pairs]
-        for (w, dw), m, ws in zip(pairs, self.momentum, self.ws_update):
+            sizes = (halves if apart else tuple(self.w_gate_up.shape), tuple(self.w_down.shape))
+            self.momentum = [torch.zeros(n, device=self.w_down.device) for n in sizes]
+            self.ws_update = [moe.alloc_muon_workspace(*n, self.w_down.dtype, self.w_down.device) for n in sizes]
+            if apart:
+                self.w_halves, self.dw_halves = (torch.empty(halves, dtype=self.w_down.dtype, device=self.w_down.device) for _ in range(2))
+        elif (self.momentum[0].shape == halves) != bool(apart):
+            raise ValueError("apart: the momentum is that of the other form")
+        w1, dw1 = self.w_gate_up, self.dw_gate_up
+        if apart:                                                    # [E, H, 2, I] with gate and up in front
+            w1, dw1 = self.w_halves, self.dw_halves
+            for half, whole in ((w1, self.w_gate_up), (dw1, self.dw_gate_up)):
+                half.view(2, E, H, I).copy_(whole.view(E, H, 2, I).permute(2, 0, 1, 3))
+        for w, dw, m, ws in zip((w1, self.w_down), (dw1, self.dw_down), self.momentum, self.ws_update):
             fan_in, fan_out = w.shape[1:]
             s = max(1.0, fan_out / fan_in) ** 0.5 if scale == "fan" else scale
             moe.moe_muon_step(dw, m, w, m, w, ws, lr=lr, mu=mu, weight_decay=weight_decay, scale=s)
+        if apart:
+            self.w_gate_up.view(E, H, 2, I).copy_(w1.view(2, E, H, I).permute(1, 2, 0, 3))
         if self.scores is not None:
             moe.moe_bias_update(self.counts, self.rate, self.bias, self.bias)
 
@@ -167,7 +182,7 @@ def main():
     timed(f"training step, {a.tokens} tokens", lambda: block.step(x, dout, dz))
     print(f"balance loss {block.loss.item():.5f} ({block.coef} if even), busiest expert {block.counts[:-1].max().item()} of "
           f"{a.tokens * a.top_k // a.experts} selections on average")
-    timed("update of the experts", lambda: block.update(scale="fan"))
+    timed("update of the experts, gate and up apart", lambda: block.update(scale="fan", apart=True))
     block.quantize()
     for n in (1, 32):
         timed(f"decode step, {n} tokens, 4-bit experts", lambda: block.decode(x[:n]))
