@@ -488,9 +488,11 @@ int moe_router_project_backward(int32_t T, int32_t H, int32_t E, int dtype, cons
  * which leaves the singular vectors of u and takes every singular value s of X0 through a s + b s^3 + c s^5: close to 1 after five
  * steps with the usual coefficients, unless it is a very small part of the whole.
  * Products on the matrix cores with fp32 sums, their operands in bf16 storage rounded to 11 bits, in fp32 storage to 22.  A rounding's share
- * grows by up to a per later step: of the result's norm, five steps leave about 2e-3 (bf16; its own rounding included) and 5e-6
- * (fp32), where the singular values reach down to a hundredth of the largest.  A matrix of zeros stays zeros; one with a NaN or
- * an infinity becomes NaN and touches no other.  Sums have a fixed order.
+ * grows by up to a per later step: of the result's norm, five steps leave 2e-3 to 5e-3 (bf16; its own rounding, 1.7e-3, included) and
+ * up to 5e-6 (fp32), where the singular values reach down to a hundredth of the largest.  A matrix of zeros stays zeros; one with a NaN or
+ * an infinity becomes NaN in every value and touches no other.  Sums have a fixed order, the same for the same call; with another B, or at another
+ * place among the B, a matrix may go through other tiles, some of which add up a long sum in shares: the same bits, or within these
+ * roundings.
  *   steps    1 .. 16;  eps > 0, finite
  *   coefs    host, [steps][3] a, b, c, read before the call returns; NULL: 3.4445, -4.7750, 2.0315 in each.  MOE_ERR_INVALID_ARG
  *            where they let singular values grow beyond 32 (from at most 1), or |a + b s^2 + c s^4| beyond 1024 on the way
