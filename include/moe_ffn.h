@@ -462,7 +462,8 @@ int moe_bias_update(int32_t E, const int32_t* d_counts, float rate, const float*
 /* ---- The router's projection ----
  * logits = x W in fp32 from hidden rows in either storage type, and its backward, with fp32 sums in a fixed order.  The products under
  * them are exact where x is bf16, off by less than 2^-21 where both sides are fp32 (2^-24 on average), and by less than 2^-13 in dx in
- * bf16, ahead of its rounding.  An infinity in x, W or dlogits gives NaN in the sums that it takes part in.
+ * bf16, ahead of its rounding.  Of fp32 values below 2^-109 in magnitude only the multiples of 2^-133 in them count (x in bf16: all of it).  An
+ * infinity in x, W or dlogits gives NaN in the sums that it takes part in.
  * 1 <= H <= 262144, 1 <= E <= 256, T / 128 * max(H, E) / 64 (both rounded up) below 2^24.
  *   d_x [T,H] dtype;  d_w [H,E] f32;  d_logits, d_dlogits [T,E] f32
  *   d_workspace  >= moe_router_project_workspace_bytes(T, H, E), which does not fall as T grows: one of the largest T serves all

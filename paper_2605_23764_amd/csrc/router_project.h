@@ -4,7 +4,7 @@
 // and the rest (below 2^-15).  A product of two sums is the sum of the pieces' products: three MFMAs where x is bf16 (one piece against
 // three, nothing left out), six where both sides are fp32 (left out: below 2 * 2^-7 * 2^-15 of the product); dx in bf16 takes two pieces
 // of each side, three products (left out: below 2^-14 + 2 * 2^-15), in front of a rounding of 2^-8.  At 16 times the rate of fp32 MFMA
-// that is 5 and 2.7 times as fast.  (An infinity has NaN pieces.)
+// that is 5 and 2.7 times as fast.  (An infinity has NaN pieces.  The last bit of a piece is 2^-133 at least, so of values below 2^-109 bits are lost.)
 //
 // One form, C[i,j] = sum over k of P(i,k) Q(j,k), with either operand k-contiguous or row-contiguous in memory.  Tiles of 128 x 128 by
 // four waves of 64 x 64, of 128 x 64 by four of 32 x 64, of 128 x 32 by four of 32 x 32; k steps of 64: a step's values are fetched into

@@ -41,8 +41,8 @@ def _hold(got, P, Q, products, left, add, half, what):
     elements = _block_norms(torch.ones_like(want)) ** 2
     factor = torch.where(elements < 64, 4.0, 2.0)
     allowed = factor * (U * n ** 0.5 * size + left / 2 * (size + _block_norms(sums))) + (half + 2 * U) * _block_norms(want)
-    worst = (err / allowed).max().item()
-    print(f"{what}: {err.norm() / _block_norms(want).norm():.2e} of the norm, worst block {worst:.2f} of what is allowed", flush=True)
+    worst = torch.where(err == 0, 0.0, err / allowed).max().item()             # nothing but zeros: nothing is allowed
+    print(f"{what}: {err.norm():.2e} against {_block_norms(want).norm():.2e}, worst block {worst:.2f} of what is allowed", flush=True)
     return worst
 
 
@@ -84,3 +84,24 @@ def test_the_measure_sees_a_missing_piece(T, H, E, dtype):
     for name, wrong in (("logits", (x.double() @ _high(w, 2).double()).float()), ("dw", (x.double().t().contiguous() @ _high(d, 2).double()).float())):
         P, Q, products, left, add, half = cases[name]
         assert _hold(wrong, P, Q, products, left, add, half, f"planted, {name}") > 1, name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("power", [-100, -110, -115, -120, -125, -130, -140])
+def test_values_near_the_least(power, dtype):
+    """Of fp32 values below 2^-109 the multiples of 2^-133 in them count, here of W and dlogits (times large ones, so that sums are ordinary)."""
+    T, H, E = 40, 96, 24
+    x, w, d, _ = _inputs(T, H, E, dtype)
+    x = (x.float() * 2.0 ** 60).to(TORCH[dtype])
+    large = w * 2.0 ** 60
+    w, d = ((t.double() * 2.0 ** power).float() for t in (w, d))
+    cut = lambda v: torch.where(v.abs() < 2.0 ** -109, torch.trunc(v.double() * 2.0 ** 133) * 2.0 ** -133, v.double())  # noqa: E731
+    logits, dx, dw = torch.empty(T, E, device="cuda"), torch.empty_like(x), torch.empty(H, E, device="cuda")
+    ws = moe.alloc_router_project_workspace(T, H, E)
+    moe.moe_router_project(x, w, logits, ws)
+    moe.moe_router_project_backward(d, x, large, None, None, dw, ws)
+    moe.moe_router_project_backward(d, x, large, None, dx, None, ws)
+    f32 = dtype == "f32"
+    for got, P, Q, left, half in ((logits, x, cut(w), 2.0 ** -24 * f32, 0.0), (dw, x.t(), cut(d), 2.0 ** -24 * f32, 0.0),
+                                  (dx, cut(d), large.t(), 2.0 ** -24 if f32 else 2.0 ** -13, HALF[dtype])):
+        assert _hold(got, P, Q, 6 if f32 else 3, left, None, half, f"2^{power} {dtype}") <= 1
