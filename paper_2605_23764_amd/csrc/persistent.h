@@ -271,15 +271,16 @@ __device__ __forceinline__ void sched_trigger(const SchedParams<BF16>& sp, int e
 
 // A routing without counters and task tables: a single launch behind it finds no task, or every share drawn, and says so in the status word
 // instead of running an earlier routing's tasks or whatever the workspace held.  It loads no more for that than it does anyway.  By the workgroup's
-// last wave, ahead of the routing, which waits for others.
+// last wave, beside wave 0's tile map.
 template <bool BF16>
 __device__ __forceinline__ void leave_out_tables(const SchedParams<BF16>& sp) {
   const int i = (int)threadIdx.x - ((int)blockDim.x - kWave);
-  if (i >= 0 && i < kNumXcd) {
-    sp.meta[kMetaQueueCount0 + i] = -1;
-    sp.events[kEvNotPrepared + i] = kNotPrepared;
+  if (sp.no_tasks) {                       // the launch as streams
+    if (i >= 0 && i < kNumXcd) sp.events[kEvNotPrepared + i] = kNotPrepared;
+  } else {
+    if (i >= 0 && i < kNumXcd) sp.meta[kMetaQueueCount0 + i] = -1;
+    if (i == kNumXcd) sp.meta[kMetaGemm2Total] = -1;
   }
-  if (i == kNumXcd) sp.meta[kMetaGemm2Total] = -1;
 }
 
 constexpr int kTableRows = 1024;
@@ -422,11 +423,14 @@ __global__ __launch_bounds__(kScanWaves * kWave) void sched_prepare_kernel(Sched
   __shared__ int32_t s_lds[kScanLds];
   static_assert(kRankThreads == kScanWaves * kWave, "workgroup 0 scans with all its waves");
   if (blockIdx.x == 0) {
-    if (sp.skip_tables) leave_out_tables(sp);
     scan_all(sp.route, s_lds, s_lds + kMaxE + 64);
+    if (sp.skip_tables) {
+      leave_out_tables(sp);
+      return;
+    }
     __threadfence_block();
     __syncthreads();   // tile map (written by wave 0) complete before every wave reads it
-    if (!sp.skip_tables) build_task_tables<BF16>(sp);
+    build_task_tables<BF16>(sp);
     return;
   }
   const int rank_wgs = (sp.route.n_sub + sp.route.subs - 1) / sp.route.subs;
@@ -445,8 +449,8 @@ template <bool BF16>
 __global__ __launch_bounds__(kRankThreads) void sched_prepare_copy_kernel(SchedParams<BF16> sp, int tokens) {
   __shared__ int32_t s_lds[kScanLds];
   if (blockIdx.x == 0) {
-    leave_out_tables(sp);
     scan_all(sp.route, s_lds, s_lds + kMaxE + 64);
+    leave_out_tables(sp);
     return;
   }
   rank_tokens(sp.route, ((int)blockIdx.x - 1) * sp.route.subs * tokens, tokens, [&](int t, int rowv) __attribute__((always_inline)) {
@@ -463,9 +467,11 @@ __device__ __forceinline__ void route_one_launch(const SchedParams<BF16>& sp, co
       sp.zero_dst[i] = make_uint4(0, 0, 0, 0);
     return;
   }
-  if (sp.skip_tables) leave_out_tables(sp);
   route_one(sp.route, select);
-  if (sp.skip_tables) return;
+  if (sp.skip_tables) {
+    leave_out_tables(sp);
+    return;
+  }
   __threadfence_block();
   __syncthreads();   // tile map (written by wave 0) complete before every wave reads it
   build_task_tables<BF16>(sp);
