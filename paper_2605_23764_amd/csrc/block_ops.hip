@@ -351,13 +351,13 @@ int moe_route_scores_backward(int32_t T, int32_t E, int32_t k, const MoeScores* 
   if (!good(d_logits) || !good(d_topk_idx) || !good(d_dtopk_w) || !aligned(d_dadd) || !good(d_dlogits)) return MOE_ERR_INVALID_ARG;
   ScoresBackwardParams p{};
   p.logits = d_logits; p.topk_idx = d_topk_idx; p.dtopk_w = d_dtopk_w; p.dadd = d_dadd; p.dlogits = d_dlogits;
-  p.sigmoid = scores->score == MOE_SCORE_SIGMOID; p.renorm = scores->renormalize; p.scale = scores->scale;
+  p.renorm = scores->renormalize; p.scale = scores->scale;
   p.T = T; p.E = E; p.k = k;
   hipStream_t s = static_cast<hipStream_t>(stream);
   with_token_form(E, [&](auto lanes, auto tail) {
     const int want = ceil_div(T, kRouterThreads / lanes.value);
     const dim3 grid(want < 2048 ? want : 2048);
-    if (p.sigmoid) hipLaunchKernelGGL((scores_backward_kernel<lanes.value, tail.value, false>), grid, dim3(kRouterThreads), 0, s, p);
+    if (scores->score == MOE_SCORE_SIGMOID) hipLaunchKernelGGL((scores_backward_kernel<lanes.value, tail.value, false>), grid, dim3(kRouterThreads), 0, s, p);
     else hipLaunchKernelGGL((scores_backward_kernel<lanes.value, tail.value, true>), grid, dim3(kRouterThreads), 0, s, p);
   });
   return launched();

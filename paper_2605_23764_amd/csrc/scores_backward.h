@@ -18,13 +18,13 @@ struct ScoresBackwardParams {
   const float* dtopk_w;          // [T, k]
   const float* dadd;             // [T, E] or null; may be dlogits
   float* dlogits;                // [T, E]; may be logits
-  int sigmoid, renorm;
+  int renorm;
   float scale;
   int T, E, k;
 };
 
 template <int L, bool TAIL, bool FULL> __global__ __launch_bounds__(kRouterThreads) void scores_backward_kernel(ScoresBackwardParams p) {
-  // FULL: the row's maximum (and, not renormalised, its sum) is needed: softmax
+  // FULL: softmax, which needs the row's maximum (and, not renormalised, its sum); else sigmoid
   constexpr int kPer = kRouterThreads / L, kSlots = RouterToken<L>::kSlots;
   __shared__ float s_row[kPer][4 * L];
   const int g = threadIdx.x / L, l = threadIdx.x & (L - 1), e0 = l * 4;
@@ -78,7 +78,7 @@ template <int L, bool TAIL, bool FULL> __global__ __launch_bounds__(kRouterThrea
     double ps[kSlots], total = 0.0, dot = 0.0;
 #pragma unroll
     for (int j = 0; j < kSlots; ++j) {
-      ps[j] = id[j] < 0 ? 0.0 : up * (p.sigmoid ? sigmoid64(lv[j]) : exp_below(lv[j], m));
+      ps[j] = id[j] < 0 ? 0.0 : up * (FULL ? exp_below(lv[j], m) : sigmoid64(lv[j]));
       total += ps[j];
       dot += ps[j] * (double)dw[j];
     }
@@ -88,7 +88,7 @@ template <int L, bool TAIL, bool FULL> __global__ __launch_bounds__(kRouterThrea
       dot += __shfl_xor(dot, o);
     }
     // w'[j] = ps[j] * norm
-    const double norm = p.renorm ? (total > 0.0 ? 1.0 / total : 0.0) : p.sigmoid ? 1.0 : (sum > 0.f ? 1.0 / (double)sum : 0.0);
+    const double norm = p.renorm ? (total > 0.0 ? 1.0 / total : 0.0) : !FULL ? 1.0 : (sum > 0.f ? 1.0 / (double)sum : 0.0);
     dot *= norm;                                                 // sum of w' dw
 #pragma unroll
     for (int i = 0; i < 4; ++i) row[e0 + i] = 0.f;
@@ -97,7 +97,7 @@ template <int L, bool TAIL, bool FULL> __global__ __launch_bounds__(kRouterThrea
     for (int j = 0; j < kSlots; ++j)
       if (id[j] >= 0) {
         double v = (double)p.scale * ps[j] * norm * ((double)dw[j] - (p.renorm ? dot : 0.0));
-        if (p.sigmoid) v *= sigmoid64(-lv[j]);
+        if (!FULL) v *= sigmoid64(-lv[j]);
         __hip_atomic_fetch_add(row + id[j], (float)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);   // an expert may be there twice
       }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
