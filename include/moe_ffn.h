@@ -430,7 +430,8 @@ typedef struct MoeScores {
  * near ones); the weights are rounded once.  The bias takes part in the selection alone.  A logit of NaN counts as -inf, as in
  * moe_route.  An expert whose logit or key is -inf (or whose key is NaN) comes behind all others, with weight 0 where it is selected
  * all the same (logit -inf); in a group's score it counts 0 beside a living one.  Several logits of +inf share a softmax's probability
- * evenly.  Keys beyond +-1e300 are equal.
+ * evenly.  Keys beyond +-1e300 are equal.  A group's score is the sum of its two best for either kind of score; there is no form that takes
+ * its best key alone.
  *   d_logits [T,E] f32;  d_bias [E] f32 or NULL: 0
  *   saved, d_workspace   filled as by moe_route: moe_dispatch_to_combine, moe_dispatch_to_combine_w4 or the stage entry points
  *                        follow, then moe_ffn_backward, and moe_route_scores_backward on its d_dtopk_w

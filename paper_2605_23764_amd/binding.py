@@ -572,7 +572,7 @@ def make_scores(score="sigmoid", n_group: int = 1, topk_group: int = 1, renormal
 
 def moe_route_scores(shape, scores, logits, bias, saved: Saved, workspace, mode: int = MODE_SERIALIZED, stream=None) -> None:
     """moe_route by scores: fills the routing results of `saved` and the workspace; bias [E] or None.  mode: that of the
-    moe_dispatch_to_combine that follows."""
+    moe_dispatch_to_combine that follows (which, with MODE_PERSISTENT behind MODE_SERIALIZED, computes nothing: moe_ffn_last_status)."""
     sv = saved.c_struct()
     logits, = _args((shape.T, shape.E), torch.float32, "logits", logits)
     bias, = _args((shape.E,), torch.float32, "bias", bias)

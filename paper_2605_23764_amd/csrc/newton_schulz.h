@@ -131,7 +131,8 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
   asm volatile("" : "+v"(lane));           // see store_block_via_lds
   const int l32 = lane & 31, lh = lane >> 5;
   const lds_ptr base = (lds_ptr)region;
-  // Fused by hand, here and below, so that a matrix's result is the same bits whichever tiles it goes through.
+  // Fused by hand, here and below, so that a matrix's result is the same bits whichever tiles it goes through (shares of a tile's sum, which depend
+  // on the matrices beside it, add up in another order).
   auto value = [&](int nt, int q, int x) __attribute__((always_inline)) {
     return acc[nt][q * 4 + x];
   };
@@ -162,7 +163,7 @@ __device__ __forceinline__ void ns_block(const NsGemmParams& p, const f32x16 (&a
     const int cols_valid = p.cols - c0;    // a multiple of 64
     const int r = lane / kLanes, ch = lane % kLanes;
     // Of a symmetric matrix: the blocks of 64 x 64 on the diagonal and above it, the latter also as those below (sums with the operands exchanged
-    // differ by a last bit now and then: that way the matrix is symmetric, and the same whichever tiles it is made of).
+    // differ by a last bit now and then: that way the matrix is symmetric, and the same whichever tiles it is made of, but for shares).
     constexpr bool SYM = ns_symmetric(EPI);
     const bool col_ok = ch * 8 < cols_valid && (!SYM || (c0 + ch * 8) >> 6 >= r0 >> 6);
     // bytes from a matrix's first to element (row, col) of 8-column chunk `col`, col a multiple of 8

@@ -217,7 +217,7 @@ template <typename OUT> struct ProjRows {
 };
 struct ProjNoRows {};
 
-// NP, NQ: pieces of a value of each side.  TN: columns of a tile, 128 or 32.  OUT: storage of the result of dx, void: partial sums in fp32.
+// NP, NQ: pieces of a value of each side.  TN: columns of a tile, 128, 64 or 32 (with OUT 64).  OUT: storage of the result of dx, void: partial sums in fp32.
 // Two workgroups to a CU where their LDS allows it (all but fp32's pairs of three pieces): they cover each other's waits (dx, 8192 x 7168 x 256, 260
 // registers and one workgroup: 312 us).
 template <typename TP, bool KCP, int NP, typename TQ, bool KCQ, int NQ, int TN, typename OUT>

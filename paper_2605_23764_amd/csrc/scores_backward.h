@@ -11,7 +11,7 @@ namespace moe {
 //   softmax               dl[e] = scale * s[e] * ([e selected] dw - d)
 // plus dadd.  Slots in 64 bits (a lane has one, or up to four where a token has fewer than 16 lanes); the softmax over all E, whose
 // result is rounded to 32 bits anyway, in 32.  Bound by dadd and dlogits (and the softmax's logits) as router_backward_kernel is: 8192 tokens of
-// 256 experts, sigmoid, 5.7 us.
+// 256 experts, sigmoid 6.0 us, softmax 7.0 (from a graph).
 struct ScoresBackwardParams {
   const float* logits;           // [T, E]
   const int32_t* topk_idx;       // [T, k]

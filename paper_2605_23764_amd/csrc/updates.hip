@@ -147,6 +147,7 @@ template <int EPI, bool SPLIT, typename T, bool QUARTERS> void run_tiles128(NsGe
 // product, whose launches wait for each other's latency and not for the matrix cores, as tiles of 64 x 64 as long as two to a CU hold all (all steps
 // of one matrix in bf16: 200 x 330 105 us with 128 x 128, 71 with 64 x 64; 512 x 512 146 and 87; 1024 x 1024 233 and 132; 1408 x 1408 277 and 160; but
 // 4 of 1024 x 2048, 544 tiles for A, 279 and 335), unless the sums are long and so few that shares of them pay (256 x 4096: 113 and 147).
+// Tiles count as whole ones however much of them lies past a matrix's sides: many matrices of sides below 256 go through 256 x 256 all the same.
 template <int EPI, typename T> void run_product(NsGemmParams p, int cus, hipStream_t s) {
   constexpr bool SPLIT = sizeof(T) == 4, SYM = ns_symmetric(EPI);
   auto tiles = [&](int side) {
