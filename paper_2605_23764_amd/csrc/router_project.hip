@@ -12,7 +12,7 @@ using namespace moe;
 namespace {
 
 constexpr int kProjMaxE = 256;
-constexpr int kProjCUs = 256;
+constexpr int kProjCUs = 256;              // the card's, not asked for: workspace sizes follow from it, whichever device is current when they are asked
 constexpr int kProjTiles = 48;             // of 128 columns, at least
 constexpr int kProjMaxSplits = 256;
 
